@@ -352,6 +352,55 @@ SR_API sr_status sr_attention_colsums(const sr_config* cfg, int32_t S, const voi
 SR_API sr_status sr_select_topk_scores(const sr_config* cfg, int32_t K, const float* planes,
                                 int32_t parts, int32_t* idx, void* stream);
 
+/* Eight-bit activations.
+ * Tokens and activations held as signed 8-bit codes, the linear layer that multiplies such codes, and
+ * the weight gradient that reads them.  These calls take their sizes and sr_dtype directly (no sr_config).
+ *
+ * SR_Q8_ROW, for the operands of sr_linear8 (the tokens, or a weight's rows: one scale per token, one
+ *   per output channel).  Per row with a = max |x|:  q = 127 x / a to the nearest integer, halves to
+ *   the even one, of the exact quotient; scale = a / 127 in fp32 (value: q * scale).  A row of zeros has
+ *   q = 0, scale = 0.  A row with an Inf or NaN has q = 0 and scale = NaN.
+ * SR_Q8_BLOCK, for activations kept from a forward for its backward: a power of two 2^e per 32
+ *   channels, e the smallest integer in [-126, 121] with max |x| <= 127 2^e, kept as the byte e + 127;
+ *   q = x 2^-e to the nearest integer, halves to even, within +-127 (which only a block with values
+ *   above 1.98 * 2^127 meets).  The value q * 2^e is exact in bf16 and fp32.  A block with an Inf or
+ *   NaN has the byte 255 and q = 0, and reads back as NaN. */
+typedef enum { SR_Q8_ROW = 0, SR_Q8_BLOCK = 1 } sr_q8_kind;
+
+typedef enum { SR_ACT_NONE = 0, SR_ACT_GELU = 1 } sr_act;
+
+/* x [M,N] (storage type) -> q [M,N] int8 and scale: fp32 [M] (SR_Q8_ROW) or bytes [M,N/32]
+ * (SR_Q8_BLOCK).  M >= 1, N % 64 == 0, M*N*elt < 2^31 bytes. */
+SR_API sr_status sr_quantize8(int32_t q8_kind, int32_t dtype, int32_t M, int32_t N, const void* x, int8_t* q,
+                       void* scale, void* stream);
+
+/* The values that q and scale stand for -> x [M,N] storage type (SR_Q8_ROW: one rounding to it;
+ * SR_Q8_BLOCK: exact).  Sizes as above. */
+SR_API sr_status sr_dequantize8(int32_t q8_kind, int32_t dtype, int32_t M, int32_t N, const int8_t* q,
+                         const void* scale, void* x, void* stream);
+
+/* Linear layer on SR_Q8_ROW operands (nn.Linear layout):
+ *   y[m,n] = act( xs[m] ws[n] sum_k xq[m,k] wq[n,k] + bias[n] )
+ * with an exact int32 sum, the rest in fp32 and one rounding to the storage type.
+ *   xq [M,K], xs [M]: the tokens;  wq [N,K], ws [N]: the weight;  bias [N] storage type or NULL;
+ *   y [M,N] storage type out;  act: sr_act (the exact GELU).
+ * M >= 1, N % 8 == 0, K % 64 == 0, K <= 65536; M*K, N*K and M*N*elt < 2^31 bytes. */
+SR_API sr_status sr_linear8(int32_t dtype, int32_t act, int32_t M, int32_t N, int32_t K, const int8_t* xq,
+                     const float* xs, const int8_t* wq, const float* ws, const void* bias, void* y,
+                     void* stream);
+
+/* Weight and bias gradient of a linear layer from the SR_Q8_BLOCK checkpoint of its input:
+ *   dw[n,k] = sum_m dy[m,n] xhat[m,k],   db[n] = sum_m dy[m,n]
+ *   dy [M,N] storage type;  xq [M,K], xe [M,K/32]: the checkpoint, read in 8 bits;
+ *   dw [N,K] fp32 and db [N] fp32 (or NULL), overwritten.  Every product is exact and sums are fp32,
+ *   in a fixed order (deterministic).  scratch: sr_weight_grad8_scratch_bytes bytes (NULL when 0).
+ * M >= 1, N % 8 == 0, K % 64 == 0; M*N*elt, M*K and N*K*4 < 2^31 bytes. */
+SR_API sr_status sr_weight_grad8_scratch_bytes(int32_t dtype, int32_t M, int32_t N, int32_t K,
+                                        size_t* scratch_bytes);
+SR_API sr_status sr_weight_grad8(int32_t dtype, int32_t M, int32_t N, int32_t K, const void* dy, const int8_t* xq,
+                          const uint8_t* xe, float* dw, float* db, void* scratch, size_t scratch_bytes,
+                          void* stream);
+
 /* Launch timing for measurement (not needed by the method).  After
  * sr_profile_start, every library launch group whose name contains `name_filter`
  * ("" or NULL = all) is timed with HIP events bound to its first and last kernel at launch
@@ -367,7 +416,7 @@ SR_API sr_status sr_select_topk_scores(const sr_config* cfg, int32_t K, const fl
  * scatter_delta, gather_f32, scatter_f32, ln_fwd, ln_bwd,
  * gemm_<op> (qkv, o, fc1, fc2, dx_fc2, dx_fc1, dx_o, dx_qkv, dw_<op>), attn_fwd,
  * attn_bwd_dkv, attn_bwd_dq, attn_bwd_f32 (both passes of fp32 storage), attn_bwd_delta, reduce,
- * colsum, convert, mod.  Where few workgroups make dK/dV and dQ one launch (bf16, head dim 64),
+ * colsum, convert, mod, quantize8, dequantize8, linear8, weight_grad8.  Where few workgroups make dK/dV and dQ one launch (bf16, head dim 64),
  * attn_bwd_dkv holds both passes. */
 SR_API sr_status sr_profile_start(const char* name_filter);
 SR_API sr_status sr_profile_stop(char* out, size_t out_bytes, size_t* needed);

@@ -17,6 +17,8 @@ SR_OK, SR_EINVAL, SR_ESHAPE, SR_EDTYPE, SR_EALIGN, SR_EWORKSPACE, SR_EUNSUPPORTE
 SR_F32, SR_BF16 = 0, 1
 SR_BLOCK_PRELN, SR_BLOCK_ADALN = 0, 1
 SR_SEL_RANDOM, SR_SEL_TOPK_DIFFNORM = 0, 1
+SR_Q8_ROW, SR_Q8_BLOCK = 0, 1
+SR_ACT_NONE, SR_ACT_GELU = 0, 1
 
 PARAM_FIELDS = ("ln1_w", "ln1_b", "w_qkv", "b_qkv", "w_o", "b_o", "ln2_w", "ln2_b",
                 "w_fc1", "b_fc1", "w_fc2", "b_fc2", "w_ada", "b_ada")
@@ -27,6 +29,7 @@ EXPORTS = ("sr_last_error", "sr_version", "sr_workspace_bytes", "sr_select_scrat
            "sr_attention_colsums", "sr_select_topk_scores", "sr_routed_blocks_fwd", "sr_routed_blocks_bwd",
            "sr_cross_attention_fwd", "sr_cross_attention_bwd",
            "sr_edm_workspace_bytes", "sr_edm_blocks_fwd", "sr_edm_blocks_bwd",
+           "sr_quantize8", "sr_dequantize8", "sr_linear8", "sr_weight_grad8", "sr_weight_grad8_scratch_bytes",
            "sr_profile_start", "sr_profile_stop", "sr_probe_mfma_rate")
 
 
@@ -104,6 +107,11 @@ def lib(path: str = LIB_PATH):
         "sr_edm_workspace_bytes": ([CP, I32, ctypes.POINTER(SZ), ctypes.POINTER(SZ)], I32),
         "sr_edm_blocks_fwd": ([CP, I32, P, P, P, P, P, P, SZ, P], I32),
         "sr_edm_blocks_bwd": ([CP, I32, P, P, P, P, SZ, P, P, P, P, P, P, SZ, P], I32),
+        "sr_quantize8": ([I32, I32, I32, I32, P, P, P, P], I32),
+        "sr_dequantize8": ([I32, I32, I32, I32, P, P, P, P], I32),
+        "sr_linear8": ([I32, I32, I32, I32, I32, P, P, P, P, P, P, P], I32),
+        "sr_weight_grad8_scratch_bytes": ([I32, I32, I32, I32, ctypes.POINTER(SZ)], I32),
+        "sr_weight_grad8": ([I32, I32, I32, I32, P, P, P, P, P, P, SZ, P], I32),
         "sr_profile_start": ([ctypes.c_char_p], I32),
         "sr_profile_stop": ([ctypes.c_char_p, SZ, ctypes.POINTER(SZ)], I32),
         "sr_probe_mfma_rate": ([P, ctypes.POINTER(ctypes.c_double), P], I32),
@@ -259,6 +267,29 @@ def sr_attention_colsums(cfg, S, saved, block, colsum, stream=None):
 
 def sr_select_topk_scores(cfg, K, planes, parts, idx, stream=None):
     _check(lib().sr_select_topk_scores(ctypes.byref(cfg), K, _p(planes), parts, _p(idx), _stream(stream)))
+
+
+def sr_quantize8(q8_kind, dtype, M, N, x, q, scale, stream=None):
+    _check(lib().sr_quantize8(q8_kind, dtype, M, N, _p(x), _p(q), _p(scale), _stream(stream)))
+
+
+def sr_dequantize8(q8_kind, dtype, M, N, q, scale, x, stream=None):
+    _check(lib().sr_dequantize8(q8_kind, dtype, M, N, _p(q), _p(scale), _p(x), _stream(stream)))
+
+
+def sr_linear8(dtype, act, M, N, K, xq, xs, wq, ws, bias, y, stream=None):
+    _check(lib().sr_linear8(dtype, act, M, N, K, _p(xq), _p(xs), _p(wq), _p(ws), _p(bias), _p(y), _stream(stream)))
+
+
+def sr_weight_grad8_scratch_bytes(dtype: int, M: int, N: int, K: int) -> int:
+    a = ctypes.c_size_t()
+    _check(lib().sr_weight_grad8_scratch_bytes(dtype, M, N, K, ctypes.byref(a)))
+    return a.value
+
+
+def sr_weight_grad8(dtype, M, N, K, dy, xq, xe, dw, db, scratch, stream=None):
+    _check(lib().sr_weight_grad8(dtype, M, N, K, _p(dy), _p(xq), _p(xe), _p(dw), _p(db), _p(scratch),
+                                 _nbytes(scratch), _stream(stream)))
 
 
 def sr_profile_start(name_filter: str = "") -> None:

@@ -11,6 +11,7 @@
 #include "../../include/sr.h"
 #include "edm.h"
 #include "profile.h"
+#include "quant8.h"
 #include "stack.h"
 
 static_assert(SR_SELECT_NOALLOC_MAX_TOKENS == sr::kSelStaticScores,
@@ -555,6 +556,122 @@ sr_status sr_edm_blocks_bwd(const sr_config* cfg, int32_t S, const sr_edm_block_
   return hip_status(sr::edm_bwd(edm_dims(cfg, S), params, e, zc, (const char*)saved, dh_out, dh_in, grads, dzc, de,
                                 (char*)scratch, (hipStream_t)stream),
                     "edm_blocks_bwd");
+}
+
+namespace {
+// The eight-bit calls take sizes and the storage type directly.
+sr_status check_q8(int32_t dtype, int32_t M, int32_t N, const char* cols) {
+  SR_CHECK(dtype == SR_F32 || dtype == SR_BF16, SR_EDTYPE, "unknown dtype %d", dtype);
+  SR_CHECK(M >= 1 && N >= 1, SR_EINVAL, "sizes must be positive (M=%d %s=%d)", M, cols, N);
+  SR_CHECK(N % 64 == 0, SR_EUNSUPPORTED, "%s=%d must be a multiple of 64", cols, N);
+  return SR_OK;
+}
+bool fits31(int64_t a, int64_t b, int64_t elt) { return a * b < ((1ll << 31) + elt - 1) / elt; }
+
+sr_status check_quant(int32_t kind, int32_t dtype, int32_t M, int32_t N) {
+  sr_status s = check_q8(dtype, M, N, "N");
+  if (s != SR_OK) return s;
+  SR_CHECK(kind == SR_Q8_ROW || kind == SR_Q8_BLOCK, SR_EINVAL, "unknown 8-bit kind %d", kind);
+  SR_CHECK(fits31(M, N, (int64_t)elt_of(dtype)), SR_EUNSUPPORTED, "tensors beyond 2 GiB are not supported (M=%d N=%d)",
+           M, N);
+  return SR_OK;
+}
+
+sr_status check_product8(int32_t dtype, int32_t M, int32_t N, int32_t K) {
+  sr_status s = check_q8(dtype, M, K, "K");
+  if (s != SR_OK) return s;
+  SR_CHECK(N >= 1, SR_EINVAL, "sizes must be positive (N=%d)", N);
+  SR_CHECK(N % 8 == 0, SR_EUNSUPPORTED, "N=%d must be a multiple of 8", N);
+  SR_CHECK(fits31(M, K, 1) && fits31(M, N, (int64_t)elt_of(dtype)), SR_EUNSUPPORTED,
+           "tensors beyond 2 GiB are not supported (M=%d N=%d K=%d)", M, N, K);
+  return SR_OK;
+}
+
+sr_status check_wgrad8(int32_t dtype, int32_t M, int32_t N, int32_t K) {
+  sr_status s = check_product8(dtype, M, N, K);
+  if (s != SR_OK) return s;
+  SR_CHECK(fits31(N, K, 4), SR_EUNSUPPORTED, "a gradient beyond 2 GiB is not supported (N=%d K=%d)", N, K);
+  return SR_OK;
+}
+}  // namespace
+
+sr_status sr_quantize8(int32_t q8_kind, int32_t dtype, int32_t M, int32_t N, const void* x, int8_t* q, void* scale,
+                       void* stream) {
+  sr_status s = check_quant(q8_kind, dtype, M, N);
+  if (s != SR_OK) return s;
+  SR_PTR(x, "x");
+  SR_PTR(q, "q");
+  SR_PTR(scale, "scale");
+  hipStream_t st = (hipStream_t)stream;
+  sr::ProfScope ps("quantize8", 0, (double)M * N * (elt_of(dtype) + 1), st);
+  return hip_status(sr::launch_quantize8(q8_kind, dtype == SR_BF16 ? sr::kBF16 : sr::kF32, M, N, x, q, scale, st),
+                    "quantize8");
+}
+
+sr_status sr_dequantize8(int32_t q8_kind, int32_t dtype, int32_t M, int32_t N, const int8_t* q, const void* scale,
+                         void* x, void* stream) {
+  sr_status s = check_quant(q8_kind, dtype, M, N);
+  if (s != SR_OK) return s;
+  SR_PTR(q, "q");
+  SR_PTR(scale, "scale");
+  SR_PTR(x, "x");
+  hipStream_t st = (hipStream_t)stream;
+  sr::ProfScope ps("dequantize8", 0, (double)M * N * (elt_of(dtype) + 1), st);
+  return hip_status(sr::launch_dequantize8(q8_kind, dtype == SR_BF16 ? sr::kBF16 : sr::kF32, M, N, q, scale, x, st),
+                    "dequantize8");
+}
+
+sr_status sr_linear8(int32_t dtype, int32_t act, int32_t M, int32_t N, int32_t K, const int8_t* xq, const float* xs,
+                     const int8_t* wq, const float* ws, const void* bias, void* y, void* stream) {
+  sr_status s = check_product8(dtype, M, N, K);
+  if (s != SR_OK) return s;
+  SR_CHECK(act == SR_ACT_NONE || act == SR_ACT_GELU, SR_EINVAL, "unknown activation %d", act);
+  SR_CHECK(K <= 65536, SR_EUNSUPPORTED, "K=%d > 65536", K);
+  SR_CHECK(fits31(N, K, 1), SR_EUNSUPPORTED, "a weight beyond 2 GiB is not supported (N=%d K=%d)", N, K);
+  SR_PTR(xq, "xq");
+  SR_PTR(xs, "xs");
+  SR_PTR(wq, "wq");
+  SR_PTR(ws, "ws");
+  if (bias) SR_CHECK(aligned16(bias), SR_EALIGN, "bias is not 16-byte aligned");
+  SR_PTR(y, "y");
+  hipStream_t st = (hipStream_t)stream;
+  sr::Linear8 a;
+  a.M = M; a.N = N; a.K = K;
+  a.xq = xq; a.xs = xs; a.wq = wq; a.ws = ws; a.bias = bias; a.y = y; a.act = act;
+  sr::ProfScope ps("linear8", 2.0 * M * N * K, (double)M * K + (double)N * K + (double)M * N * elt_of(dtype), st);
+  return hip_status(sr::launch_linear8(dtype == SR_BF16 ? sr::kBF16 : sr::kF32, a, st), "linear8");
+}
+
+sr_status sr_weight_grad8_scratch_bytes(int32_t dtype, int32_t M, int32_t N, int32_t K, size_t* scratch_bytes) {
+  sr_status s = check_wgrad8(dtype, M, N, K);
+  if (s != SR_OK) return s;
+  SR_CHECK(scratch_bytes != nullptr, SR_EINVAL, "scratch_bytes is NULL");
+  *scratch_bytes = sr::wgrad8_scratch(dtype == SR_BF16 ? sr::kBF16 : sr::kF32, M, N, K);
+  return SR_OK;
+}
+
+sr_status sr_weight_grad8(int32_t dtype, int32_t M, int32_t N, int32_t K, const void* dy, const int8_t* xq,
+                          const uint8_t* xe, float* dw, float* db, void* scratch, size_t scratch_bytes, void* stream) {
+  sr_status s = check_wgrad8(dtype, M, N, K);
+  if (s != SR_OK) return s;
+  SR_PTR(dy, "dy");
+  SR_PTR(xq, "xq");
+  SR_PTR(xe, "xe");
+  SR_PTR(dw, "dw");
+  if (db) SR_CHECK(aligned16(db), SR_EALIGN, "db is not 16-byte aligned");
+  const int dt = dtype == SR_BF16 ? sr::kBF16 : sr::kF32;
+  const size_t need = sr::wgrad8_scratch(dt, M, N, K);
+  if (need) {
+    SR_PTR(scratch, "scratch");
+    SR_CHECK(scratch_bytes >= need, SR_EWORKSPACE, "scratch buffer has %zu bytes, needs %zu", scratch_bytes, need);
+  }
+  hipStream_t st = (hipStream_t)stream;
+  sr::Wgrad8 a;
+  a.M = M; a.N = N; a.K = K;
+  a.dy = dy; a.xq = xq; a.xe = xe; a.dw = dw; a.db = db; a.scratch = (float*)scratch;
+  sr::ProfScope ps("weight_grad8", 2.0 * M * N * K,
+                   (double)M * N * elt_of(dtype) + (double)M * K * 33 / 32 + (double)N * K * 4, st);
+  return hip_status(sr::launch_wgrad8(dt, a, st), "weight_grad8");
 }
 
 sr_status sr_probe_mfma_rate(float* sink, double* tflops, void* stream) {

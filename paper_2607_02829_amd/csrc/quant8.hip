@@ -1,0 +1,223 @@
+// Eight-bit activations: rows of the storage type to signed 8-bit codes and back.
+//
+// SR_Q8_ROW (operands of the int8 products; one fp32 scale per row, a = max |x| of the row):
+//   q = nearest integer to 127 x / a, halves to the even one, of the exact quotient;  scale = a / 127.
+// SR_Q8_BLOCK (what a forward keeps for its backward; a power of two per 32 channels):
+//   e = the smallest integer with max |x| <= 127 2^e inside [-126, 121], kept as the byte e + 127;
+//   q = nearest integer to x 2^-e, halves to even, within +-127.  The value q 2^e has at most seven
+//   significant bits, so it is exact in bf16 and fp32: what reads a checkpoint rounds nothing.
+//
+// Both are bound by memory: 3 bytes per bf16 element (5 per fp32 one) each way.
+#include "common.h"
+#include "quant8.h"
+#include "sr_internal.h"
+
+namespace sr {
+
+namespace {
+
+constexpr uint32_t kInfBits = 0x7F800000u;
+
+SR_DEV uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+// Eight consecutive elements as fp32.
+SR_DEV void load8(const bf16_t* p, float v[8]) {
+  const i32x4 w = *reinterpret_cast<const i32x4*>(p);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    v[2 * j] = __uint_as_float((uint32_t)w[j] << 16);
+    v[2 * j + 1] = __uint_as_float((uint32_t)w[j] & 0xFFFF0000u);
+  }
+}
+SR_DEV void load8(const float* p, float v[8]) {
+  const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    v[j] = a[j];
+    v[4 + j] = b[j];
+  }
+}
+SR_DEV void store8(bf16_t* p, const float v[8]) {
+  i32x4 w;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) w[j] = (int)f2bf2(v[2 * j], v[2 * j + 1]);
+  *reinterpret_cast<i32x4*>(p) = w;
+}
+SR_DEV void store8(float* p, const float v[8]) {
+  f32x4 a, b;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    a[j] = v[j];
+    b[j] = v[4 + j];
+  }
+  reinterpret_cast<f32x4*>(p)[0] = a;
+  reinterpret_cast<f32x4*>(p)[1] = b;
+}
+
+SR_DEV uint32_t wave_umax(uint32_t v) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
+  return v;
+}
+
+// Adding 1.5 2^23 to |v| < 2^22 rounds v to an integer (halves to even), whose two's complement
+// is then in the low bits of the sum.
+constexpr float kMagic = 12582912.0f;
+SR_DEV uint32_t low_bytes(float a, float b, float c, float d) {
+  return (__float_as_uint(a) & 0xFFu) | (__float_as_uint(b) & 0xFFu) << 8 | (__float_as_uint(c) & 0xFFu) << 16 |
+         __float_as_uint(d) << 24;
+}
+
+// 127 x / a to the nearest integer for the elements of one row.
+//  bf16: with x and a scaled by the power of two that brings a into [0.5, 1), 127 x is exact in
+//    fp32 and the quotient, corrected once, is within an ulp; a quotient that is no tie lies more than
+//    2^-18 from every tie (both sides are multiples of 2^-16 over a), and a tie is hit exactly.
+//  fp32: the same in fp64, where 127 x is exact and the distance at least 2^-33.
+template <typename T>
+struct RowCode;
+template <>
+struct RowCode<bf16_t> {
+  float a, inv;
+  int ex;
+  SR_DEV explicit RowCode(float amax) {
+    ex = __builtin_amdgcn_frexp_expf(amax);
+    a = __builtin_amdgcn_ldexpf(amax, -ex);
+    inv = __fdiv_rn(1.0f, a);
+  }
+  SR_DEV float code(float x) const {
+    const float t = 127.0f * __builtin_amdgcn_ldexpf(x, -ex);
+    const float v = t * inv;
+    return __fadd_rn(fmaf(fmaf(-v, a, t), inv, v), kMagic);
+  }
+};
+template <>
+struct RowCode<float> {
+  double a, inv;
+  SR_DEV explicit RowCode(float amax) {
+    a = amax;
+    inv = 1.0 / a;
+  }
+  SR_DEV float code(float x) const {
+    const double t = 127.0 * (double)x;
+    const double v = t * inv;
+    return __fadd_rn((float)__builtin_rint(fma(fma(-v, a, t), inv, v)), kMagic);
+  }
+};
+
+// One wave per row: the row's maximum, then its codes.
+template <typename T>
+__global__ __launch_bounds__(256) void quant_rows_kernel(const T* __restrict__ x, int M, int N, int8_t* __restrict__ q,
+                                                         float* __restrict__ scale) {
+  const int row = blockIdx.x * 4 + wave_index(), lane = threadIdx.x & 63;
+  if (row >= M) return;
+  const T* xr = x + (size_t)row * N;
+  uint32_t m = 0;
+  for (int c = lane * 8; c < N; c += 512) {
+    float v[8];
+    load8(xr + c, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = max(m, abs_bits(v[j]));
+  }
+  m = wave_umax(m);
+  const bool ok = m < kInfBits;   // the order of magnitudes is that of the bits, NaN above Inf
+  const float amax = __uint_as_float(m);
+  if (lane == 0) scale[row] = ok ? __fdiv_rn(amax, 127.0f) : __uint_as_float(0x7FC00000u);
+  const RowCode<T> rc(ok && m ? amax : 1.0f);
+  for (int c = lane * 8; c < N; c += 512) {
+    float v[8];
+    load8(xr + c, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = rc.code(v[j]);
+    i32x2 w;
+    w[0] = ok ? (int)low_bytes(v[0], v[1], v[2], v[3]) : 0;
+    w[1] = ok ? (int)low_bytes(v[4], v[5], v[6], v[7]) : 0;
+    *reinterpret_cast<i32x2*>(q + (size_t)row * N + c) = w;
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void dequant_rows_kernel(const int8_t* __restrict__ q, const float* __restrict__ scale,
+                                                           size_t n8, int N8, T* __restrict__ x) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n8) return;
+  const i32x2 w = reinterpret_cast<const i32x2*>(q)[i];
+  const float s = scale[i / (size_t)N8];
+  float v[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = (float)(int8_t)((uint32_t)w[j >> 2] >> (8 * (j & 3))) * s;
+  store8(x + i * 8, v);
+}
+
+// Eight elements per lane, four lanes per block of 32 channels.
+template <typename T>
+__global__ __launch_bounds__(256) void quant_blocks_kernel(const T* __restrict__ x, size_t n8, int8_t* __restrict__ q,
+                                                           uint8_t* __restrict__ e) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n8) return;   // n8 is a multiple of 8: the four lanes of a block leave together
+  float v[8];
+  load8(x + i * 8, v);
+  uint32_t m = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) m = max(m, abs_bits(v[j]));
+  m = max(m, (uint32_t)__shfl_xor((int)m, 1, 64));
+  m = max(m, (uint32_t)__shfl_xor((int)m, 2, 64));
+  const uint32_t E = block_exponent(m);
+  const float inv = __uint_as_float((254u - min(E, 253u)) << 23);   // 2^-e
+#pragma unroll
+  for (int j = 0; j < 8; ++j)   // the upper limit is met only by a block whose 2^e is at its largest
+    v[j] = __builtin_amdgcn_fmed3f(fmaf(v[j], inv, kMagic), kMagic - 127.0f, kMagic + 127.0f);
+  i32x2 w;
+  w[0] = E == 255u ? 0 : (int)low_bytes(v[0], v[1], v[2], v[3]);
+  w[1] = E == 255u ? 0 : (int)low_bytes(v[4], v[5], v[6], v[7]);
+  reinterpret_cast<i32x2*>(q)[i] = w;
+  if ((threadIdx.x & 3) == 0) e[i >> 2] = (uint8_t)E;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void dequant_blocks_kernel(const int8_t* __restrict__ q, const uint8_t* __restrict__ e,
+                                                             size_t n8, T* __restrict__ x) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n8) return;
+  const i32x2 w = reinterpret_cast<const i32x2*>(q)[i];
+  const float s = block_scale(e[i >> 2]);
+  float v[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = (float)(int8_t)((uint32_t)w[j >> 2] >> (8 * (j & 3))) * s;
+  store8(x + i * 8, v);
+}
+
+template <typename T>
+hipError_t quant(int kind, int M, int N, const void* x, int8_t* q, void* scale, hipStream_t st) {
+  if (kind == SR_Q8_ROW) {
+    SR_LAUNCH(quant_rows_kernel<T>, dim3((unsigned)((M + 3) / 4)), dim3(256), 0, st, (const T*)x, M, N, q,
+              (float*)scale);
+  } else {
+    const size_t n8 = (size_t)M * N / 8;
+    SR_LAUNCH(quant_blocks_kernel<T>, dim3((unsigned)((n8 + 255) / 256)), dim3(256), 0, st, (const T*)x, n8, q,
+              (uint8_t*)scale);
+  }
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t dequant(int kind, int M, int N, const int8_t* q, const void* scale, void* x, hipStream_t st) {
+  const size_t n8 = (size_t)M * N / 8;
+  const dim3 grid((unsigned)((n8 + 255) / 256));
+  if (kind == SR_Q8_ROW)
+    SR_LAUNCH(dequant_rows_kernel<T>, grid, dim3(256), 0, st, q, (const float*)scale, n8, N / 8, (T*)x);
+  else
+    SR_LAUNCH(dequant_blocks_kernel<T>, grid, dim3(256), 0, st, q, (const uint8_t*)scale, n8, (T*)x);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_quantize8(int kind, int dtype, int M, int N, const void* x, int8_t* q, void* scale, hipStream_t st) {
+  return dtype == kBF16 ? quant<bf16_t>(kind, M, N, x, q, scale, st) : quant<float>(kind, M, N, x, q, scale, st);
+}
+hipError_t launch_dequantize8(int kind, int dtype, int M, int N, const int8_t* q, const void* scale, void* x,
+                              hipStream_t st) {
+  return dtype == kBF16 ? dequant<bf16_t>(kind, M, N, q, scale, x, st) : dequant<float>(kind, M, N, q, scale, x, st);
+}
+
+}  // namespace sr

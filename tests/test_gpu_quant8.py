@@ -1,0 +1,165 @@
+"""The eight-bit calls on the GPU against the fp64 oracle: codes, scales and exponents exactly, the
+products and gradients within what their roundings allow."""
+import numpy as np
+import pytest
+
+from oracle import quant8 as oq
+from oracle.numerics import storage_to_f64
+from paper_2607_02829_amd import abi, device, inputs
+
+pytestmark = pytest.mark.gpu
+
+GUARD = 64   # elements behind an output that must keep their value
+DT = {"bf16": abi.SR_BF16, "f32": abi.SR_F32}
+
+
+def _guarded(shape, dtype, fill):
+    """A tensor of `shape` at the front of a longer buffer, and the buffer."""
+    import torch
+    n = int(np.prod(shape))
+    buf = torch.full((n + GUARD,), fill, dtype=dtype, device="cuda")
+    return buf[:n].view(shape), buf
+
+
+def _storage(dtype):
+    import torch
+    return torch.bfloat16 if dtype == "bf16" else torch.float32
+
+
+def _rows(M, N, dtype, seed):
+    """Rows with ties of the row rounding, zeros, subnormal and huge values among ordinary ones."""
+    rng = np.random.default_rng([M, N, seed])
+    x = (rng.standard_normal((M, N)) * np.exp(rng.standard_normal((M, 1)))).astype(np.float32)
+    if M > 2:
+        x[1] = 1.984375 * rng.integers(-127, 128, N) / 254.0      # every code a multiple of one half
+        x[1, 3] = 1.984375
+        x[2] = 0.0
+    if M > 6:
+        x[3] *= np.float32(2.0 ** -140)                              # subnormal
+        x[4] = np.clip(x[4].astype(np.float64) * 2.0 ** 126, -3.3e38, 3.3e38)
+        x[5, :] = 0.0
+        x[5, N - 1] = -7.0
+    return inputs.to_storage(x, dtype)
+
+
+def _quant(kind, x, dtype):
+    import torch
+    M, N = x.shape
+    xd = device.to_device(x)
+    q, qb = _guarded((M, N), torch.int8, 77)
+    s, sb = _guarded((M,), torch.float32, -3.0) if kind == abi.SR_Q8_ROW else _guarded((M, N // 32), torch.uint8, 99)
+    abi.sr_quantize8(kind, DT[dtype], M, N, xd, q, s)
+    back, bb = _guarded((M, N), _storage(dtype), -5.0)
+    abi.sr_dequantize8(kind, DT[dtype], M, N, q, s, back)
+    torch.cuda.synchronize()
+    assert bool((qb[M * N:] == 77).all()) and bool((bb[M * N:] == -5.0).all())
+    assert bool((sb[s.numel():] == (-3.0 if kind == abi.SR_Q8_ROW else 99)).all())
+    return q.cpu().numpy(), s.cpu().numpy(), storage_to_f64(device.to_host(back))
+
+
+SIZES = [(1, 64), (3, 64), (7, 192), (33, 1024), (130, 4096), (9, 4160), (2, 8192), (1025, 320)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,N", SIZES)
+def test_row_format_is_exact(M, N, dtype):
+    x = _rows(M, N, dtype, 1)
+    q, s, back = _quant(abi.SR_Q8_ROW, x, dtype)
+    wq, ws = oq.quant_rows(storage_to_f64(x))
+    assert np.array_equal(q, wq)
+    assert np.array_equal(s, ws)
+    want = oq.rows_value(wq, ws)
+    if dtype == "bf16":   # one rounding to bf16 of a fp32 product: half a step of each, and the floor of the subnormals
+        assert np.all(np.abs(back - want) <= np.abs(want) * (2.0 ** -8 + 2.0 ** -24) + 2.0 ** -134)
+    else:
+        assert np.array_equal(back.astype(np.float32), want.astype(np.float32))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,N", SIZES)
+def test_block_format_is_exact(M, N, dtype):
+    x = _rows(M, N, dtype, 2)
+    q, e, back = _quant(abi.SR_Q8_BLOCK, x, dtype)
+    wq, we = oq.quant_blocks(storage_to_f64(x))
+    assert np.array_equal(e, we)
+    assert np.array_equal(q, wq)
+    assert np.array_equal(back, oq.blocks_value(wq, we))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_block_format_at_its_borders(dtype):
+    # maxima on and next to 127 2^e, at the largest finite value, and the halves of the code grid
+    top = 3.3895313892515355e38 if dtype == "bf16" else 3.4028234663852886e38
+    x = np.zeros((1, 64 * 6), np.float32)
+    x[0, 0], x[0, 1:9] = 127.0, [0.5, 1.5, 2.5, -0.5, -1.5, -126.5, 63.5, 0.25]
+    x[0, 32], x[0, 33] = 127.5, 64.0
+    x[0, 64], x[0, 65:68] = top, [-top, 2.0 ** 120, 2.0 ** 121]
+    x[0, 96], x[0, 97] = 1.984375 * 2.0 ** 127, 2.0 ** 127
+    x[0, 128], x[0, 129] = 2.0 ** -126, 2.0 ** -133
+    x[0, 160] = 2.0 ** -133
+    x[0, 192], x[0, 193] = 127 * 2.0 ** -126, 0.5 * 2.0 ** -126
+    x[0, 224], x[0, 225] = np.inf, 1.0
+    x[0, 256], x[0, 288] = np.nan, -np.inf
+    x[0, 320:352] = -0.0
+    x = inputs.to_storage(x, dtype)
+    q, e, back = _quant(abi.SR_Q8_BLOCK, x, dtype)
+    wq, we = oq.quant_blocks(storage_to_f64(x))
+    assert np.array_equal(e, we) and np.array_equal(q, wq)
+    assert np.array_equal(back, oq.blocks_value(wq, we), equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+def test_row_format_keeps_non_finite_rows_apart(dtype, bad):
+    x = _rows(9, 128, dtype, 3)
+    f = storage_to_f64(x).astype(np.float32)
+    f[8, 77] = bad
+    f[0, 0] = bad
+    x = inputs.to_storage(f, dtype)
+    q, s, back = _quant(abi.SR_Q8_ROW, x, dtype)
+    wq, ws = oq.quant_rows(storage_to_f64(x))
+    assert np.array_equal(q, wq) and np.array_equal(s, ws, equal_nan=True)
+    assert np.isnan(back[[0, 8]]).all() and np.isfinite(back[1:8]).all()
+
+
+def test_near_ties_of_fp32_rows():
+    # quotients one unit in the last place of x on either side of k + 1/2, which a division in fp32 rounds onto it
+    rng = np.random.default_rng(8)
+    N = 1024
+    a = np.float32(1.0) + rng.random(64, dtype=np.float32)
+    x = np.zeros((64, N), np.float32)
+    for r in range(64):
+        k = rng.integers(0, 126, N)
+        v = ((k + 0.5) * np.float64(a[r]) / 127.0).astype(np.float32)
+        x[r] = np.where(rng.random(N) < 0.5, np.nextafter(v, np.float32(0)), np.where(rng.random(N) < 0.5, v, np.nextafter(v, np.float32(9))))
+        x[r, 0] = a[r]
+    q, s, _ = _quant(abi.SR_Q8_ROW, x, "f32")
+    wq, ws = oq.quant_rows(x.astype(np.float64))
+    assert np.array_equal(q, wq) and np.array_equal(s, ws)
+
+
+@pytest.mark.parametrize("kind", [abi.SR_Q8_ROW, abi.SR_Q8_BLOCK])
+def test_largest_tensor(kind):
+    # 2 GiB less one row of bf16: offsets up to the limit of the call
+    import torch
+    N = 4096
+    M = (1 << 31) // (2 * N) - 1
+    print(f"[quant8 largest] kind={kind} M={M} N={N}", flush=True)
+    x = torch.randn((64, N), device="cuda").to(torch.bfloat16).repeat(M // 64 + 1, 1)[:M].contiguous()
+    x *= torch.arange(1, M + 1, device="cuda").remainder(7).add(1).to(torch.bfloat16)[:, None]
+    q = torch.empty((M, N), dtype=torch.int8, device="cuda")
+    s = torch.empty((M,), dtype=torch.float32, device="cuda") if kind == abi.SR_Q8_ROW else torch.empty(
+        (M, N // 32), dtype=torch.uint8, device="cuda")
+    back = torch.full_like(x, 7.0)
+    abi.sr_quantize8(kind, abi.SR_BF16, M, N, x, q, s)
+    abi.sr_dequantize8(kind, abi.SR_BF16, M, N, q, s, back)
+    torch.cuda.synchronize()
+    for lo in (0, M // 2, M - 70):
+        xs = storage_to_f64(device.to_host(x[lo:lo + 70]))
+        wq, ws = (oq.quant_rows if kind == abi.SR_Q8_ROW else oq.quant_blocks)(xs)
+        assert np.array_equal(q[lo:lo + 70].cpu().numpy(), wq)
+        assert np.array_equal(s[lo:lo + 70].cpu().numpy(), ws)
+    step = x.abs().amax(1) if kind == abi.SR_Q8_ROW else None
+    err = (back.float() - x.float()).abs().amax(1)
+    limit = (step.float() if step is not None else x.float().abs().amax(1)) * (1 / 64)   # a half step of the coarser format
+    assert bool((err <= limit).all())

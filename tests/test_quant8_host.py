@@ -1,0 +1,106 @@
+"""Host-side refusals of the eight-bit calls: every bad argument is rejected before any launch."""
+import ctypes
+
+import pytest
+
+from paper_2607_02829_amd import abi
+
+pytestmark = pytest.mark.cpu
+
+FAKE = 1 << 40          # aligned, never dereferenced: validation fails first
+BF, F32 = abi.SR_BF16, abi.SR_F32
+
+
+def _lib():
+    try:
+        return abi.lib()
+    except abi.SrLibraryMissing as e:
+        pytest.skip(str(e))
+
+
+@pytest.mark.parametrize("kind,dtype,M,N,status", [
+    (2, BF, 4, 64, abi.SR_EINVAL), (-1, BF, 4, 64, abi.SR_EINVAL), (0, 5, 4, 64, abi.SR_EDTYPE),
+    (0, BF, 0, 64, abi.SR_EINVAL), (1, BF, 4, 0, abi.SR_EINVAL), (1, F32, -3, 64, abi.SR_EINVAL),
+    (0, BF, 4, 32, abi.SR_EUNSUPPORTED), (1, BF, 4, 100, abi.SR_EUNSUPPORTED),
+    (0, BF, 1 << 20, 1024, abi.SR_EUNSUPPORTED),       # exactly 2 GiB
+    (1, F32, 1 << 19, 1024, abi.SR_EUNSUPPORTED),
+    (0, BF, 2147483647, 2147483584, abi.SR_EUNSUPPORTED),
+])
+def test_quantize_sizes(kind, dtype, M, N, status):
+    L = _lib()
+    assert L.sr_quantize8(kind, dtype, M, N, FAKE, FAKE, FAKE, None) == status
+    assert L.sr_dequantize8(kind, dtype, M, N, FAKE, FAKE, FAKE, None) == status
+    assert abi.sr_last_error()
+
+
+def test_quantize_pointers():
+    L = _lib()
+    for bad, status in ((None, abi.SR_EINVAL), (FAKE + 8, abi.SR_EALIGN)):
+        for k in range(3):
+            p = [FAKE] * 3
+            p[k] = bad
+            assert L.sr_quantize8(0, BF, 4, 64, *p, None) == status
+            assert L.sr_dequantize8(1, F32, 4, 64, *p, None) == status
+
+
+@pytest.mark.parametrize("dtype,act,M,N,K,status", [
+    (9, 0, 4, 8, 64, abi.SR_EDTYPE), (BF, 2, 4, 8, 64, abi.SR_EINVAL), (BF, 0, 0, 8, 64, abi.SR_EINVAL),
+    (BF, 0, 4, 0, 64, abi.SR_EINVAL), (BF, 0, 4, 8, 0, abi.SR_EINVAL), (BF, 0, 4, 12, 64, abi.SR_EUNSUPPORTED),
+    (BF, 0, 4, 8, 96, abi.SR_EUNSUPPORTED), (BF, 0, 4, 8, 65600, abi.SR_EUNSUPPORTED),
+    (BF, 0, 1 << 21, 8, 1024, abi.SR_EUNSUPPORTED), (F32, 0, 1 << 19, 1024, 64, abi.SR_EUNSUPPORTED),
+    (BF, 0, 1, 1 << 21, 1024, abi.SR_EUNSUPPORTED),
+])
+def test_linear_sizes(dtype, act, M, N, K, status):
+    assert _lib().sr_linear8(dtype, act, M, N, K, FAKE, FAKE, FAKE, FAKE, None, FAKE, None) == status
+
+
+def test_linear_pointers():
+    L = _lib()
+    for bad, status in ((None, abi.SR_EINVAL), (FAKE + 4, abi.SR_EALIGN)):
+        for k in range(6):
+            if k == 4 and bad is None:
+                continue   # the bias is optional
+            p = [FAKE] * 6
+            p[k] = bad
+            assert L.sr_linear8(BF, 0, 4, 8, 64, *p, None) == status, k
+
+
+@pytest.mark.parametrize("dtype,M,N,K,status", [
+    (3, 4, 8, 64, abi.SR_EDTYPE), (BF, 0, 8, 64, abi.SR_EINVAL), (BF, 4, 8, -64, abi.SR_EINVAL),
+    (BF, 4, 4, 64, abi.SR_EUNSUPPORTED), (BF, 4, 8, 32, abi.SR_EUNSUPPORTED),
+    (BF, 1, 1 << 16, 1 << 13, abi.SR_EUNSUPPORTED),    # a 2 GiB gradient
+    (BF, 1 << 20, 1024, 64, abi.SR_EUNSUPPORTED), (BF, 1 << 21, 8, 1024, abi.SR_EUNSUPPORTED),
+])
+def test_weight_grad_sizes(dtype, M, N, K, status):
+    L = _lib()
+    n = ctypes.c_size_t()
+    assert L.sr_weight_grad8_scratch_bytes(dtype, M, N, K, ctypes.byref(n)) == status
+    assert L.sr_weight_grad8(dtype, M, N, K, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 1 << 40, None) == status
+
+
+def test_weight_grad_pointers_and_scratch():
+    L = _lib()
+    assert L.sr_weight_grad8_scratch_bytes(BF, 4, 8, 64, None) == abi.SR_EINVAL
+    for bad, status in ((None, abi.SR_EINVAL), (FAKE + 2, abi.SR_EALIGN)):
+        for k in range(5):
+            if k == 4 and bad is None:
+                continue   # db is optional
+            p = [FAKE] * 5
+            p[k] = bad
+            assert L.sr_weight_grad8(BF, 4, 8, 64, *p, FAKE, 1 << 40, None) == status, k
+    n = abi.sr_weight_grad8_scratch_bytes(BF, 16200, 1024, 1024)
+    if n:
+        p = [FAKE] * 5
+        assert L.sr_weight_grad8(BF, 16200, 1024, 1024, *p, None, 0, None) == abi.SR_EINVAL
+        assert L.sr_weight_grad8(BF, 16200, 1024, 1024, *p, FAKE, n - 1, None) == abi.SR_EWORKSPACE
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("N,K", [(8, 64), (256, 1024), (1024, 1024), (4096, 1024), (1024, 4096)])
+def test_weight_grad_scratch_never_falls_with_tokens(dtype, N, K):
+    _lib()
+    last = 0
+    for M in (*range(1, 600, 7), *range(600, 16400, 61)):
+        n = abi.sr_weight_grad8_scratch_bytes(dtype, M, N, K)
+        assert n >= last, (M, last, n)
+        last = n
