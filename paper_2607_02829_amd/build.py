@@ -24,7 +24,7 @@ NO_CONTRACT = {"select.hip", "routing.hip"}
 NO_NANS = {"attention.hip"}
 # Files whose kernels read LDS fragments with inline assembly: their gfx950 assembly is kept
 # and checked (isa_scan) for registers touched while such a read is in flight.
-ASYNC_READS = {"attention.hip", "gemm.hip"}
+ASYNC_READS = {"attention.hip", "gemm.hip", "linear8.hip"}
 
 HIPCC = os.environ.get("HIPCC", shutil.which("hipcc") or "/opt/rocm/bin/hipcc")
 FLAGS = [

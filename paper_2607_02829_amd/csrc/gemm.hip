@@ -34,6 +34,7 @@
 #include "common.h"
 #include "epilogue.h"
 #include "sr_internal.h"
+#include "tiles.h"
 
 namespace sr {
 
@@ -208,26 +209,6 @@ SR_DEV void fill_issue(const uint32_t* off, __amdgpu_buffer_rsrc_t rs, bf16_t* l
     __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr_t*)(lds + (wid * BPW + i) * 512), 16, off[i] + delta, 0, 0,
                                              0);
 }
-
-// Workgroups are handed to the eight XCDs round-robin by linear id.  Renumber them so that each
-// XCD owns a contiguous range of tiles, and walk tiles in groups of GM tile rows (column by
-// column within a group), so the tiles that one XCD runs together share A rows and B columns in
-// its L2.  Split-K index outermost.
-constexpr int GM = 8;
-SR_DEV void tile_coords(int bid, int nwg, int tiles_m, int tiles_n, int& tm, int& tn, int& split) {
-  const int x = bid & 7, q = nwg >> 3, rem = nwg & 7;
-  const int t = x * q + min(x, rem) + (bid >> 3);
-  const int per = tiles_m * tiles_n;
-  split = t / per;
-  const int u = t - split * per;
-  const int grp = u / (GM * tiles_n);
-  const int first = grp * GM;
-  const int gm = min(GM, tiles_m - first);
-  const int v = u - first * tiles_n;
-  tm = first + v % gm;
-  tn = v / gm;
-}
-
 
 // Per-lane LDS byte addresses of one operand's fragments (stage 0, k-step 0 for r-major).
 //  k-major: rows rb + 32 p + lane % 32 (p = 0, 1; rows 64 apart share the swizzle), one address
