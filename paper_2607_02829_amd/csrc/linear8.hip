@@ -51,14 +51,14 @@ SR_DEV Cols load_cols(const Linear8& a, int n) {
   return c;
 }
 template <int ACT, typename T>
-SR_DEV void finish4(const Linear8& a, int m, int n, float xs, const Cols& c, i32x4 acc) {
+SR_DEV f32x4 finish4(float xs, const Cols& c, i32x4 acc) {
   f32x4 v;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     v[q] = fmaf((float)acc[q] * xs, c.ws[q], c.bias[q]);
     if constexpr (ACT == SR_ACT_GELU) v[q] = gelu_f<gelu_deg<T>()>(v[q]);
   }
-  store4<T>(a.y, (size_t)m * a.N + n, v);
+  return v;
 }
 
 // ---------------------------------------------------------------- tiles through LDS
@@ -158,7 +158,8 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear8_tile_kernel(Li
     for (int i = 0; i < MI; ++i)
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(ua[ks][i], ub[ks][j], acc[i][j], 0, 0, 0);
+        acc[i][j] = KG == 1 ? __builtin_amdgcn_mfma_i32_32x32x32_i8(ub[ks][j], ua[ks][i], acc[i][j], 0, 0, 0)
+                            : __builtin_amdgcn_mfma_i32_32x32x32_i8(ua[ks][i], ub[ks][j], acc[i][j], 0, 0, 0);
   };
 
   static_for<NST>([&](auto s) { fill(s.value, s.value); });
@@ -193,7 +194,62 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear8_tile_kernel(Li
   wait_vm_lgkm0<0>();
   __syncthreads();
 
-  // epilogue in MI passes of PR rows: pass p stages block p of every wave row in LDS, one plane per group; each
+  if constexpr (KG == 1) {
+    // one group: the weight is the first operand, so that a lane has four consecutive channels of one token in each
+    // register quad (register r: channel 8 (r/4) + 4 h + r%4, token lane % 32) and finishes them where they are
+    float* sc = reinterpret_cast<float*>(smem);   // the tile's channel scales, then its biases
+    for (int i = threadIdx.x; i < BN; i += NT) {
+      const bool in = n0 + i < a.N;
+      sc[i] = in ? a.ws[n0 + i] : 0.f;
+      sc[BN + i] = in && a.bias ? to_f32<T>(((const T*)a.bias)[n0 + i]) : 0.f;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int nb = wn * (BN / WN) + 32 * j;
+      Cols cols[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        cols[q].ws = *reinterpret_cast<const f32x4*>(sc + nb + 8 * q + 4 * h);
+        cols[q].bias = *reinterpret_cast<const f32x4*>(sc + BN + nb + 8 * q + 4 * h);
+      }
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        const int m = m0 + wm * (BM / WM) + 32 * i + (lane & 31);
+        const float xs = m < a.M ? a.xs[m] : 0.f;
+        f32x4 v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          v[q] = finish4<ACT, T>(xs, cols[q], i32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2],
+                                                    acc[i][j][4 * q + 3]});
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int n = n0 + nb + 8 * q + 4 * h;
+            if (m < a.M && n < a.N) store4<float>(a.y, (size_t)m * a.N + n, v[q]);
+          }
+        } else {
+          // the halves of the wave trade quads: each lane stores eight consecutive channels
+#pragma unroll
+          for (int q = 0; q < 4; q += 2) {
+            i32x4 w;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const auto r = __builtin_amdgcn_permlane32_swap(f2bf2(v[q][2 * e], v[q][2 * e + 1]),
+                                                              f2bf2(v[q + 1][2 * e], v[q + 1][2 * e + 1]), false, false);
+              w[e] = (int)r[0];
+              w[2 + e] = (int)r[1];
+            }
+            const int n = n0 + nb + 8 * q + 8 * h;
+            if (m < a.M && n < a.N) *reinterpret_cast<i32x4*>((bf16_t*)a.y + (size_t)m * a.N + n) = w;
+          }
+        }
+      }
+    }
+    return;
+  }
+
+  // more groups: epilogue in MI passes of PR rows: pass p stages block p of every wave row in LDS, one plane per group; each
   // thread then finishes NB chunks of four columns (register r of a 32 x 32 tile: row 8 (r/4) + 4 h + r%4, column
   // lane % 32)
   int* stg = reinterpret_cast<int*>(smem);
@@ -234,7 +290,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear8_tile_kernel(Li
         i32x4 v = *reinterpret_cast<const i32x4*>(stg + lr * LD + c4);
 #pragma unroll
         for (int g = 1; g < KG; ++g) v += *reinterpret_cast<const i32x4*>(stg + (g * PR + lr) * LD + c4);
-        finish4<ACT, T>(a, m, n, xs[p][q], cols, v);
+        store4<T>(a.y, (size_t)m * a.N + n, finish4<ACT, T>(xs[p][q], cols, v));
       }
     }
   }
@@ -282,7 +338,7 @@ __global__ __launch_bounds__(64 * W) void linear8_few_kernel(Linear8 a) {
     i32x4 v = *reinterpret_cast<const i32x4*>(&stg[0][lr][c4]);
 #pragma unroll
     for (int g = 1; g < W; ++g) v += *reinterpret_cast<const i32x4*>(&stg[g][lr][c4]);
-    finish4<ACT, T>(a, m, n, a.xs[m], load_cols<T>(a, n), v);
+    store4<T>(a.y, (size_t)m * a.N + n, finish4<ACT, T>(a.xs[m], load_cols<T>(a, n), v));
   }
 }
 
