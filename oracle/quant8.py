@@ -53,7 +53,7 @@ def gelu(v):
 
 def linear(xq, xs, wq, ws, bias=None, act_gelu=False):
     """y (M, N) fp64 = act(xs ws (xq wq^T) + bias)."""
-    v = (xq.astype(np.int64) @ wq.astype(np.int64).T) * xs.astype(np.float64)[:, None] * ws.astype(np.float64)[None, :]
+    v = (xq.astype(np.float64) @ wq.astype(np.float64).T) * xs.astype(np.float64)[:, None] * ws.astype(np.float64)[None, :]
     if bias is not None:
         v = v + bias[None, :]
     return gelu(v) if act_gelu else v

@@ -16,8 +16,6 @@ namespace {
 
 typedef __attribute__((__vector_size__(16 * sizeof(int)))) int i32x16;
 
-constexpr int KB = 64;   // bytes (and channels) of k in an operand tile: K is a multiple of it
-
 // Columns n .. n + 3: the channels' scales and bias.
 struct Cols {
   f32x4 ws, bias;
@@ -63,43 +61,55 @@ SR_DEV f32x4 finish4(float xs, const Cols& c, i32x4 acc) {
 
 // ---------------------------------------------------------------- tiles through LDS
 
-// Operand tile of R rows x KB bytes: row r at 64 r, its four 16-byte chunks at positions c ^ (r / 4) % 4,
-// so that the 16 rows of a fragment read's quarter wave cover the 64 banks once.  It is filled by whole 1 KB
-// blocks of 16 rows, straight from memory (buffer_load ... lds): lane l lands at byte 16 l of its block
-// and fetches the chunk that the swizzle places there.
-SR_DEV int bswz(int r) { return (r >> 2) & 3; }
-template <int BPW>
-SR_DEV void fill_offsets(uint32_t* off, int r0, int K, int lane, int wid) {
-#pragma unroll
-  for (int i = 0; i < BPW; ++i) {
-    const int row = (wid * BPW + i) * 16 + (lane >> 2);
-    off[i] = (uint32_t)(r0 + row) * (uint32_t)K + (uint32_t)(((lane & 3) ^ bswz(row)) * 16);
-  }
+// Operand tile of R rows x KB bytes (64 or 128): row r at KB r, its 16-byte chunks at positions c ^ bswz(r), so
+// that the 16 rows of a fragment read's quarter wave cover the 64 banks once.  It is filled by whole 1 KB blocks,
+// straight from memory (buffer_load ... lds): lane l lands at byte 16 l of its block and fetches the chunk that
+// the swizzle places there.
+template <int KB>
+SR_DEV int bswz(int r) {
+  return (r / (256 / KB)) & (KB / 16 - 1);
 }
+template <int KB, int BPW>
+struct Fill {
+  uint32_t off[BPW];
+  uint32_t upper = 0;   // bit i: load i fetches the second 64 bytes of the tile
+  SR_DEV void init(int r0, int K, int lane, int wid) {
+    constexpr int CH = KB / 16, RPB = 64 / CH;
+#pragma unroll
+    for (int i = 0; i < BPW; ++i) {
+      const int row = (wid * BPW + i) * RPB + lane / CH, c = (lane % CH) ^ bswz<KB>(row);
+      off[i] = (uint32_t)(r0 + row) * (uint32_t)K + (uint32_t)(c * 16);
+      upper |= (uint32_t)(c >> 2) << i;
+    }
+  }
+};
 // delta: the tile's byte offset in a row, or 2^31 past the last tile, which keeps the count of fills in flight
 // uniform: those of rows of the operand then lie past its end and read zeros.  (A row past the operand's last
-// one may wrap into the operand; what it holds reaches no output that is stored.)
+// one may wrap into the operand; what it holds reaches no output that is stored.)  half: the row ends after
+// 64 bytes of the tile, and what would be its second half reads zeros.
 template <int BPW>
-SR_DEV void fill_tile(const uint32_t* off, __amdgpu_buffer_rsrc_t rs, char* lds, int wid, uint32_t delta) {
+SR_DEV void fill_tile(const uint32_t* off, uint32_t upper, __amdgpu_buffer_rsrc_t rs, char* lds, int wid, uint32_t delta,
+                      bool half) {
 #pragma unroll
-  for (int i = 0; i < BPW; ++i)
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr_t*)(lds + (wid * BPW + i) * 1024), 16, off[i] + delta, 0, 0,
-                                             0);
+  for (int i = 0; i < BPW; ++i) {
+    const uint32_t d = half && (upper >> i & 1u) ? 0x80000000u : delta;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr_t*)(lds + (wid * BPW + i) * 1024), 16, off[i] + d, 0, 0, 0);
+  }
 }
 
 // BM x BN workgroup tile on WM x WN waves, each MI x NJ tiles of v_mfma_i32_32x32x32_i8; KG such groups of
 // waves share the tile, each with a run of the k range and LDS stages of its own.  NST stages; fills run
 // NST - 1 k-tiles ahead; fragment reads are explicit (lds_read16), so none waits for a fill it does not need.
-// Per k-tile: the second half's fragments are read, the first half multiplied; then the wait for the next tile's
-// fill and the barrier, after which this tile's stage is filled anew and the next tile's first fragments are read
-// under the second half's products.  OCC workgroups per CU.
-template <int BM, int BN, int WM, int WN, int KG, int NST, int OCC, int ACT, typename T>
+// Per k-tile: a k-step's products with the next one's fragment reads under them; before the last k-step's the wait
+// for the next tile's fill and the barrier, after which this tile's stage is filled anew and the next tile's first
+// fragments are read.  OCC workgroups per CU.
+template <int BM, int BN, int KB, int WM, int WN, int KG, int NST, int OCC, int ACT, typename T>
 __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear8_tile_kernel(Linear8 a, int tiles_m, int tiles_n) {
   constexpr int NW = WM * WN, NT = 64 * NW * KG;
   constexpr int MI = BM / (32 * WM), NJ = BN / (32 * WN);
   constexpr int SB = (BM + BN) * KB;               // bytes of a stage: the token tile, then the weight tile
-  constexpr int APW = BM / 16 / NW, BPW = BN / 16 / NW, LPT = APW + BPW;
-  static_assert(MI * 32 * WM == BM && NJ * 32 * WN == BN && APW * 16 * NW == BM && BPW * 16 * NW == BN, "whole tiles");
+  constexpr int RPB = 1024 / KB, APW = BM / RPB / NW, BPW = BN / RPB / NW, LPT = APW + BPW, KS = KB / 32;
+  static_assert(MI * 32 * WM == BM && NJ * 32 * WN == BN && APW * RPB * NW == BM && BPW * RPB * NW == BN, "whole tiles");
   static_assert(NST >= 2 && NST <= 4 && (NST - 1) * LPT < 64 && MI + NJ < 16, "counter ranges");
   __shared__ __attribute__((aligned(1024))) char smem[KG * NST * SB];
 
@@ -109,7 +119,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear8_tile_kernel(Li
   int tm, tn, split;
   tile_coords(blockIdx.x, gridDim.x, tiles_m, tiles_n, tm, tn, split);
   const int m0 = tm * BM, n0 = tn * BN;
-  const int all = a.K / KB, ntile = (all + KG - 1) / KG;   // every group runs ntile, the missing ones on zeros
+  const int all = (a.K + KB - 1) / KB, ntile = (all + KG - 1) / KG;   // every group runs ntile, the missing ones on zeros
   const int t0 = grp * ntile, nmine = min(ntile, all - t0);
   const __amdgpu_buffer_rsrc_t ra = make_rsrc(a.xq, (uint32_t)a.M * (uint32_t)a.K);
   const __amdgpu_buffer_rsrc_t rb = make_rsrc(a.wq, (uint32_t)a.N * (uint32_t)a.K);
@@ -122,67 +132,82 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear8_tile_kernel(Li
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
 
-  uint32_t offa[APW], offb[BPW];
-  fill_offsets<APW>(offa, m0, a.K, lane, wid);
-  fill_offsets<BPW>(offb, n0, a.K, lane, wid);
+  Fill<KB, APW> fla;
+  Fill<KB, BPW> flb;
+  fla.init(m0, a.K, lane, wid);
+  flb.init(n0, a.K, lane, wid);
   auto fill = [&](int t, int s) {
     char* st = smem + (grp * NST + s) * SB;
-    const uint32_t delta = t < nmine ? (uint32_t)((t0 + t) * KB) : 0x80000000u;
-    fill_tile<APW>(offa, ra, st, wid, delta);
-    fill_tile<BPW>(offb, rb, st + BM * KB, wid, delta);
+    const int k0 = (t0 + t) * KB;
+    const uint32_t delta = t < nmine ? (uint32_t)k0 : 0x80000000u;
+    const bool half = KB > 64 && k0 + KB > a.K;
+    fill_tile<APW>(fla.off, fla.upper, ra, st, wid, delta, half);
+    fill_tile<BPW>(flb.off, flb.upper, rb, st + BM * KB, wid, delta, half);
   };
   // fragment of rows r .. r + 31 at k-step ks: lane's row r + lane % 32, chunk 2 ks + lane / 32; rows 16 apart
   // share the swizzle
   const uint32_t sbase = lds_addr(smem) + (uint32_t)(grp * NST * SB);
-  uint32_t fa[2], fb[2];
+  uint32_t fa[KS], fb[KS];
 #pragma unroll
-  for (int ks = 0; ks < 2; ++ks) {
-    const int r = lane & 31, c = ((2 * ks + h) ^ bswz(r)) * 16;
+  for (int ks = 0; ks < KS; ++ks) {
+    const int r = lane & 31, c = ((2 * ks + h) ^ bswz<KB>(r)) * 16;
     fa[ks] = sbase + (uint32_t)((wm * (BM / WM) + r) * KB + c);
     fb[ks] = sbase + (uint32_t)(BM * KB + (wn * (BN / WN) + r) * KB + c);
   }
   i32x4 ua[2][MI], ub[2][NJ];
-  auto read = [&](auto sidx, auto ksv) {
-    constexpr int S = decltype(sidx)::value, ks = decltype(ksv)::value;
-    static_for<MI>([&](auto i) { ua[ks][i.value] = rd16<S * SB + i.value * 32 * KB>(fa[ks]); });
-    static_for<NJ>([&](auto j) { ub[ks][j.value] = rd16<S * SB + j.value * 32 * KB>(fb[ks]); });
+  // fragment F of k-step ks of stage S: the MI token fragments, then the NJ weight fragments
+  auto read1 = [&](auto sidx, auto ksv, auto fv) {
+    constexpr int S = decltype(sidx)::value, ks = decltype(ksv)::value, F = decltype(fv)::value;
+    if constexpr (F < MI) ua[ks & 1][F] = rd16<S * SB + F * 32 * KB>(fa[ks]);
+    else ub[ks & 1][F - MI] = rd16<S * SB + (F - MI) * 32 * KB>(fb[ks]);
   };
   auto settle = [&](int ks) {
 #pragma unroll
-    for (int i = 0; i < MI; ++i) pin(ua[ks][i]);
+    for (int i = 0; i < MI; ++i) pin(ua[ks & 1][i]);
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) pin(ub[ks][j]);
+    for (int j = 0; j < NJ; ++j) pin(ub[ks & 1][j]);
   };
-  auto mfmas = [&](int ks) {
-#pragma unroll
-    for (int i = 0; i < MI; ++i)
-#pragma unroll
-      for (int j = 0; j < NJ; ++j)
-        acc[i][j] = KG == 1 ? __builtin_amdgcn_mfma_i32_32x32x32_i8(ub[ks][j], ua[ks][i], acc[i][j], 0, 0, 0)
-                            : __builtin_amdgcn_mfma_i32_32x32x32_i8(ua[ks][i], ub[ks][j], acc[i][j], 0, 0, 0);
+  // the products of one k-step, with issue(X) after product X: what it issues goes out under the products
+  auto mfmas = [&](auto ksv, auto&& issue) {
+    constexpr int ks = decltype(ksv)::value & 1;
+    static_for<MI * NJ>([&](auto x) {
+      constexpr int i = decltype(x)::value / NJ, j = decltype(x)::value % NJ;
+      acc[i][j] = KG == 1 ? __builtin_amdgcn_mfma_i32_32x32x32_i8(ub[ks][j], ua[ks][i], acc[i][j], 0, 0, 0)
+                          : __builtin_amdgcn_mfma_i32_32x32x32_i8(ua[ks][i], ub[ks][j], acc[i][j], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      issue(x);
+      __builtin_amdgcn_sched_barrier(0);
+    });
   };
+  // the share of NF fragment reads that goes out after product X of NX
+  constexpr int NF = MI + NJ, NX = MI * NJ;
 
   static_for<NST>([&](auto s) { fill(s.value, s.value); });
   wait_vm_lgkm0<(NST - 1) * LPT>();
   lds_barrier();
-  read(IC<0>{}, IC<0>{});
+  static_for<NF>([&](auto f) { read1(IC<0>{}, IC<0>{}, f); });
   auto body = [&](int t, auto sidx) {
     constexpr int S = decltype(sidx)::value;
-    read(sidx, IC<1>{});
-    lgkm_wait<MI + NJ>();   // the first half's fragments, read one step earlier, have arrived
-    settle(0);
-    __builtin_amdgcn_sched_barrier(0);
-    mfmas(0);
-    __builtin_amdgcn_sched_barrier(0);
+    static_for<KS - 1>([&](auto ksv) {
+      constexpr int ks = decltype(ksv)::value;
+      lgkm_wait<0>();
+      settle(ks);
+      __builtin_amdgcn_sched_barrier(0);
+      mfmas(ksv, [&](auto x) {
+        constexpr int X = decltype(x)::value, F0 = X * NF / NX, F1 = (X + 1) * NF / NX;
+        static_for<F1 - F0>([&](auto f) { read1(sidx, IC<ks + 1>{}, IC<F0 + decltype(f)::value>{}); });
+      });
+    });
     // the next tile is resident (its fill is the oldest in flight), and every wave is done with this one's stage
     wait_vm_lgkm0<(NST - 2) * LPT>();
     lds_barrier();
-    settle(1);
-    fill(t + NST, S);
-    read(IC<(S + 1) % NST>{}, IC<0>{});   // unused past the last tile
+    settle(KS - 1);
     __builtin_amdgcn_sched_barrier(0);
-    mfmas(1);
-    __builtin_amdgcn_sched_barrier(0);
+    mfmas(IC<KS - 1>{}, [&](auto x) {   // reads of the next tile: unused past the last one
+      constexpr int X = decltype(x)::value, F0 = X * NF / NX, F1 = (X + 1) * NF / NX;
+      static_for<F1 - F0>([&](auto f) { read1(IC<(S + 1) % NST>{}, IC<0>{}, IC<F0 + decltype(f)::value>{}); });
+      if constexpr (X == (NX > 1 ? 1 : 0)) fill(t + NST, S);
+    });
   };
   for (int t = 0; t < ntile; t += NST)
     static_for<NST>([&](auto s) {
@@ -246,51 +271,49 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear8_tile_kernel(Li
         }
       }
     }
-    return;
-  }
-
-  // more groups: epilogue in MI passes of PR rows: pass p stages block p of every wave row in LDS, one plane per group; each
-  // thread then finishes NB chunks of four columns (register r of a 32 x 32 tile: row 8 (r/4) + 4 h + r%4, column
-  // lane % 32)
-  int* stg = reinterpret_cast<int*>(smem);
-  constexpr int PR = 32 * WM, LD = BN + 8, CPR = BN / 4, NB = (PR * CPR + NT - 1) / NT;
-  static_assert(NT % CPR == 0 && (NB * NT == PR * CPR || NB == 1), "a thread's chunks share their columns");
-  static_assert(KG * PR * LD * 4 <= KG * NST * SB, "staging fits the stages");
-  const bool active = PR * CPR >= NT || (int)threadIdx.x < PR * CPR;
-  const int c4 = (threadIdx.x % CPR) * 4, n = n0 + c4;
-  const bool ok = active && n < a.N;
-  auto row_of = [&](int p, int q) {
-    const int lr = (threadIdx.x + NT * q) / CPR;
-    return m0 + (lr >> 5) * (BM / WM) + p * 32 + (lr & 31);
-  };
-  Cols cols{};
-  if (ok) cols = load_cols<T>(a, n);
-  float xs[MI][NB];
+  } else {
+    // more groups: MI passes of PR rows.  Pass p stages block p of every wave row in LDS, one plane per group; each
+    // thread then finishes NB chunks of four columns (register r: row 8 (r/4) + 4 h + r%4, column lane % 32)
+    int* stg = reinterpret_cast<int*>(smem);
+    constexpr int PR = 32 * WM, LD = BN + 8, CPR = BN / 4, NB = (PR * CPR + NT - 1) / NT;
+    static_assert(NT % CPR == 0 && (NB * NT == PR * CPR || NB == 1), "a thread's chunks share their columns");
+    static_assert(KG * PR * LD * 4 <= KG * NST * SB, "staging fits the stages");
+    const bool active = PR * CPR >= NT || (int)threadIdx.x < PR * CPR;
+    const int c4 = (threadIdx.x % CPR) * 4, n = n0 + c4;
+    const bool ok = active && n < a.N;
+    auto row_of = [&](int p, int q) {
+      const int lr = (threadIdx.x + NT * q) / CPR;
+      return m0 + (lr >> 5) * (BM / WM) + p * 32 + (lr & 31);
+    };
+    Cols cols{};
+    if (ok) cols = load_cols<T>(a, n);
+    float xs[MI][NB];
 #pragma unroll
-  for (int p = 0; p < MI; ++p)
+    for (int p = 0; p < MI; ++p)
 #pragma unroll
-    for (int q = 0; q < NB; ++q) {
-      const int m = row_of(p, q);
-      xs[p][q] = m < a.M && ok ? a.xs[m] : 0.f;
-    }
+      for (int q = 0; q < NB; ++q) {
+        const int m = row_of(p, q);
+        xs[p][q] = m < a.M && ok ? a.xs[m] : 0.f;
+      }
 #pragma unroll
-  for (int p = 0; p < MI; ++p) {
-    if (p) __syncthreads();
+    for (int p = 0; p < MI; ++p) {
+      if (p) __syncthreads();
 #pragma unroll
-    for (int j = 0; j < NJ; ++j)
+      for (int j = 0; j < NJ; ++j)
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        stg[(grp * PR + wm * 32 + 8 * (r >> 2) + 4 * h + (r & 3)) * LD + wn * (BN / WN) + j * 32 + (lane & 31)] =
-            acc[p][j][r];
-    __syncthreads();
+        for (int r = 0; r < 16; ++r)
+          stg[(grp * PR + wm * 32 + 8 * (r >> 2) + 4 * h + (r & 3)) * LD + wn * (BN / WN) + j * 32 + (lane & 31)] =
+              acc[p][j][r];
+      __syncthreads();
 #pragma unroll
-    for (int q = 0; q < NB; ++q) {
-      const int lr = (threadIdx.x + NT * q) / CPR, m = row_of(p, q);
-      if (m < a.M && ok) {
-        i32x4 v = *reinterpret_cast<const i32x4*>(stg + lr * LD + c4);
+      for (int q = 0; q < NB; ++q) {
+        const int lr = (threadIdx.x + NT * q) / CPR, m = row_of(p, q);
+        if (m < a.M && ok) {
+          i32x4 v = *reinterpret_cast<const i32x4*>(stg + lr * LD + c4);
 #pragma unroll
-        for (int g = 1; g < KG; ++g) v += *reinterpret_cast<const i32x4*>(stg + (g * PR + lr) * LD + c4);
-        store4<T>(a.y, (size_t)m * a.N + n, finish4<ACT, T>(xs[p][q], cols, v));
+          for (int g = 1; g < KG; ++g) v += *reinterpret_cast<const i32x4*>(stg + (g * PR + lr) * LD + c4);
+          store4<T>(a.y, (size_t)m * a.N + n, finish4<ACT, T>(xs[p][q], cols, v));
+        }
       }
     }
   }
@@ -298,13 +321,13 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear8_tile_kernel(Li
 
 // ---------------------------------------------------------------- few tokens
 
-// R x R tile (16 or 32) on W waves that share the k range, fragments straight from memory: with few tiles a
-// launch is as long as its slowest chain of loads, and here a wave's whole run is in flight at once (8 k-steps
-// of 64 bytes at R = 16, 32 at R = 32, then the next 8).  The waves' sums meet in LDS.
+// R x R tile on W waves that share the k range, fragments straight from memory (lane: row lane % R, 16 bytes of k):
+// with few tiles a launch is as long as its slowest chain of loads, and here a wave has its next eight k-steps in
+// flight at once.  The waves' sums meet in LDS.
 template <int R, int W, int ACT, typename T>
 __global__ __launch_bounds__(64 * W) void linear8_few_kernel(Linear8 a) {
-  constexpr int STEP = R == 16 ? 64 : 32, U = 8, NR = R * R / 64;
-  typedef __attribute__((__vector_size__(NR * sizeof(int)))) int accv;
+  static_assert(R == 16, "register layout of the 16 x 16 product");
+  constexpr int STEP = 64, U = 8;
   __shared__ int stg[W][R][R + 4];
   const int lane = threadIdx.x & 63, wave = wave_index(), r = lane % R, h = lane / R;
   const int m0 = blockIdx.y * R, n0 = blockIdx.x * R;
@@ -312,7 +335,7 @@ __global__ __launch_bounds__(64 * W) void linear8_few_kernel(Linear8 a) {
   const __amdgpu_buffer_rsrc_t rw = make_rsrc(a.wq, (uint32_t)a.N * (uint32_t)a.K);
   const uint32_t ox = (uint32_t)(m0 + r) * (uint32_t)a.K + 16u * h, ow = (uint32_t)(n0 + r) * (uint32_t)a.K + 16u * h;
   const int steps = a.K / STEP, per = (steps + W - 1) / W, s1 = min(steps, (wave + 1) * per);
-  accv acc = {};
+  i32x4 acc = {0, 0, 0, 0};
   for (int s = wave * per; s < s1; s += U) {
     i32x4 x[U], w[U];
 #pragma unroll
@@ -322,34 +345,31 @@ __global__ __launch_bounds__(64 * W) void linear8_few_kernel(Linear8 a) {
       w[u] = buf_load16(rw, ow + k);
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if constexpr (R == 16) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[u], w[u], acc, 0, 0, 0);
-      else acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[u], w[u], acc, 0, 0, 0);
-    }
+    for (int u = 0; u < U; ++u) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[u], w[u], acc, 0, 0, 0);
   }
-  // register i: row 8 (i/4) + 4 h + i%4 at R = 32, 4 h + i at R = 16; column r
 #pragma unroll
-  for (int i = 0; i < NR; ++i) stg[wave][R == 16 ? 4 * h + i : 8 * (i >> 2) + 4 * h + (i & 3)][r] = acc[i];
+  for (int i = 0; i < 4; ++i) stg[wave][4 * h + i][r] = acc[i];   // register i: row 4 h + i, column r
   __syncthreads();
   constexpr int CPR = R / 4;
-  for (int c = threadIdx.x; c < R * CPR; c += 64 * W) {
-    const int lr = c / CPR, c4 = c % CPR * 4, m = m0 + lr, n = n0 + c4;
-    if (m >= a.M || n >= a.N) continue;
-    i32x4 v = *reinterpret_cast<const i32x4*>(&stg[0][lr][c4]);
+  if ((int)threadIdx.x < R * CPR) {
+    const int lr = threadIdx.x / CPR, c4 = threadIdx.x % CPR * 4, m = m0 + lr, n = n0 + c4;
+    if (m < a.M && n < a.N) {
+      i32x4 v = *reinterpret_cast<const i32x4*>(&stg[0][lr][c4]);
 #pragma unroll
-    for (int g = 1; g < W; ++g) v += *reinterpret_cast<const i32x4*>(&stg[g][lr][c4]);
-    store4<T>(a.y, (size_t)m * a.N + n, finish4<ACT, T>(a.xs[m], load_cols<T>(a, n), v));
+      for (int g = 1; g < W; ++g) v += *reinterpret_cast<const i32x4*>(&stg[g][lr][c4]);
+      store4<T>(a.y, (size_t)m * a.N + n, finish4<ACT, T>(a.xs[m], load_cols<T>(a, n), v));
+    }
   }
 }
 
 // ---------------------------------------------------------------- dispatch
 
-enum Shape { kFew16, kFew32, k32x32g8, k64x64g2, k64x128, k128x128, k256x128, k256x256 };
+enum Shape { kFew16, k32x32g8, k64x64g2, k64x128, k128x128, k128x128x2, k256x256 };
 
-template <int BM, int BN, int WM, int WN, int KG, int NST, int OCC, int ACT, typename T>
+template <int BM, int BN, int KB, int WM, int WN, int KG, int NST, int OCC, int ACT, typename T>
 hipError_t run_tile(const Linear8& a, hipStream_t st) {
   const int tm = (a.M + BM - 1) / BM, tn = (a.N + BN - 1) / BN;
-  SR_LAUNCH((linear8_tile_kernel<BM, BN, WM, WN, KG, NST, OCC, ACT, T>), dim3((unsigned)(tm * tn)),
+  SR_LAUNCH((linear8_tile_kernel<BM, BN, KB, WM, WN, KG, NST, OCC, ACT, T>), dim3((unsigned)(tm * tn)),
             dim3(64 * WM * WN * KG), 0, st, a, tm, tn);
   return hipGetLastError();
 }
@@ -363,25 +383,45 @@ hipError_t run_few(const Linear8& a, hipStream_t st) {
 template <int ACT, typename T>
 hipError_t run_shape(int shape, const Linear8& a, hipStream_t st) {
   switch (shape) {
-    case kFew16: return a.K > 1024 ? run_few<16, 16, ACT, T>(a, st) : run_few<16, 4, ACT, T>(a, st);
-    case kFew32: return a.K > 1024 ? run_few<32, 16, ACT, T>(a, st) : run_few<32, 4, ACT, T>(a, st);
-    case k32x32g8: return run_tile<32, 32, 1, 1, 8, 4, 1, ACT, T>(a, st);
-    case k64x64g2: return run_tile<64, 64, 2, 2, 2, 4, 1, ACT, T>(a, st);
-    case k64x128: return run_tile<64, 128, 2, 2, 1, 4, 1, ACT, T>(a, st);
-    case k128x128: return run_tile<128, 128, 2, 2, 1, 4, 2, ACT, T>(a, st);
-    case k256x128: return run_tile<256, 128, 2, 2, 1, 3, 2, ACT, T>(a, st);
-    case k256x256: return run_tile<256, 256, 2, 4, 1, 4, 1, ACT, T>(a, st);
+    case kFew16: return run_few<16, 4, ACT, T>(a, st);
+    case k32x32g8: return run_tile<32, 32, 64, 1, 1, 8, 4, 1, ACT, T>(a, st);
+    case k64x64g2:
+      // longer rows in whole lines (512 x 1024 x 4096 12.0 -> 10.8 us; 1024 x 512 x 2048 6.9, 7.7)
+      return a.K > 2048 ? run_tile<64, 64, 128, 2, 2, 2, 4, 1, ACT, T>(a, st)
+                        : run_tile<64, 64, 64, 2, 2, 2, 4, 1, ACT, T>(a, st);
+    case k64x128: return run_tile<64, 128, 128, 2, 4, 1, 4, 1, ACT, T>(a, st);
+    case k128x128: return run_tile<128, 128, 128, 2, 4, 1, 4, 1, ACT, T>(a, st);
+    case k128x128x2: return run_tile<128, 128, 128, 2, 4, 1, 2, 2, ACT, T>(a, st);
+    case k256x256:
+      // GELU's vector work on four waves per SIMD instead of two: 4050 x 4096 x 1024 30.7 -> 29.0 us, 16200 112 ->
+      // 108; without it eight waves are ahead (8192 x 4096 x 1024 52.0, 57.6)
+      if constexpr (ACT == SR_ACT_GELU) return run_tile<256, 256, 128, 4, 4, 1, 2, 1, ACT, T>(a, st);
+      else return run_tile<256, 256, 128, 2, 4, 1, 2, 1, ACT, T>(a, st);
   }
   return hipErrorInvalidValue;
 }
 
+// The smallest tile whose grid is one round of workgroups on the 256 CUs; past one round of 128 x 128 the largest,
+// once its own grid is most of a round.  us, bf16 without activation, M x N x K:
+//   fragments straight from memory, up to one 16 x 16 tile per CU and K <= 1024 (or as much work in more, shorter
+//   tiles):  1 x 4096 x 1024 4.0 (32 x 32 in eight groups 4.9), 64 x 1024 x 1024 4.5 (5.1), 2048 x 64 x 64 3.5
+//   (64 x 64 4.4);  past it 128 x 1024 x 1024 5.5 (5.2), 1 x 1024 x 4096 6.3 (6.1)
+//   32 x 32, eight groups of waves:  128 x 1024 x 4096 6.9 (64 x 64 8.1);  K = 256 4.9 (4.6)
+//   64 x 64, two groups:  1024 x 1024 x 1024 6.2 (64 x 128 7.3);  64 x 128:  2048 x 1024 x 1024 7.7 (8.7, 128 x 128 9.7)
+//   128 x 128, four stages, one workgroup per CU:  4050 x 1024 x 4096 25.5 (two 28.7);  with shorter rows two
+//   workgroups are ahead: 4050 x 1024 x 1024 11.9 (14.6), 16200 x 256 x 1024 12.3 (14.4)
+//   256 x 256:  16200 x 1024 x 1024 27.6 (128 x 128 31.6), 4050 x 4096 x 1024 27.9 (32.5);  with half a round of
+//   them 8192 x 1024 x 4096 45 (42)
+// Tiles of 256 x 128 lie between the two throughout.
 int pick_shape(const Linear8& a) {
   auto tiles = [&](int bm, int bn) { return (long)((a.M + bm - 1) / bm) * ((a.N + bn - 1) / bn); };
-  if (tiles(32, 32) <= 512) return tiles(16, 16) <= 512 ? kFew16 : kFew32;
+  const long t16 = tiles(16, 16);
+  if (a.K <= 1024 && (t16 <= 256 || t16 * a.K <= 1 << 17)) return kFew16;
+  if (a.K >= 512 && tiles(32, 32) <= 256) return k32x32g8;
   if (tiles(64, 64) <= 256) return k64x64g2;
   if (tiles(64, 128) <= 256) return k64x128;
-  if (tiles(128, 128) <= 512) return k128x128;
-  return k256x128;
+  if (a.K >= 2048 && tiles(128, 128) <= 256) return k128x128;
+  return tiles(256, 256) >= 200 ? k256x256 : k128x128x2;
 }
 
 template <typename T>

@@ -86,6 +86,17 @@ def test_linear_on_many_tokens(M, N, K):
         assert bool(((y.double() - want).abs() <= tol).all())
 
 
+@pytest.mark.parametrize("dtype,act", [("bf16", 0), ("bf16", 1), ("f32", 0), ("f32", 1)])
+@pytest.mark.parametrize("M,N,K", [
+    # sizes on either side of every border between tile shapes, ragged in rows, columns and the last 64 of k
+    (600, 600, 192), (600, 600, 576), (500, 1032, 2112), (1500, 1032, 448), (2050, 1032, 2112), (4050, 1000, 320),
+    (4100, 3336, 1088), (3500, 4104, 64), (2040, 64, 64), (2064, 64, 64), (250, 250 * 8, 1024),
+])
+def test_linear_on_every_tile_shape(M, N, K, dtype, act):
+    data = _data(M, N, K, dtype, seed=1)
+    _check(_run(M, N, K, dtype, data, act, True), M, N, K, dtype, data, act, True)
+
+
 @pytest.mark.parametrize("M", [1, 40, 300])
 def test_largest_sums_are_exact(M):
     # codes of 126 and 127 over the longest K: sums near 2^30, beyond what fp32 holds exactly
