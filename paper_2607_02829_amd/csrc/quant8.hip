@@ -54,12 +54,6 @@ SR_DEV void store8(float* p, const float v[8]) {
   reinterpret_cast<f32x4*>(p)[1] = b;
 }
 
-SR_DEV uint32_t wave_umax(uint32_t v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
-  return v;
-}
-
 // Adding 1.5 2^23 to |v| < 2^22 rounds v to an integer (halves to even), whose two's complement
 // is then in the low bits of the sum.
 constexpr float kMagic = 12582912.0f;
@@ -68,11 +62,12 @@ SR_DEV uint32_t low_bytes(float a, float b, float c, float d) {
          __float_as_uint(d) << 24;
 }
 
-// 127 x / a to the nearest integer for the elements of one row.
-//  bf16: with x and a scaled by the power of two that brings a into [0.5, 1), 127 x is exact in
-//    fp32 and the quotient, corrected once, is within an ulp; a quotient that is no tie lies more than
-//    2^-18 from every tie (both sides are multiples of 2^-16 over a), and a tie is hit exactly.
-//  fp32: the same in fp64, where 127 x is exact and the distance at least 2^-33.
+// 127 x / a to the nearest integer for the elements of one row; x and a are first scaled by the power of two that
+// brings a into [0.5, 1).
+//  bf16: 127 x is exact in fp32 and the quotient, corrected once, is within an ulp; a quotient that is no tie
+//    lies more than 2^-18 from every tie (both sides are multiples of 2^-16 over a), and a tie is hit exactly.
+//  fp32: x (127 / a) is within 3e-5 of the quotient, which decides the code unless it lies that near a tie; the few
+//    waves that see such an element take the quotient in fp64, where 127 x is exact and the distance at least 2^-33.
 template <typename T>
 struct RowCode;
 template <>
@@ -84,54 +79,104 @@ struct RowCode<bf16_t> {
     a = __builtin_amdgcn_ldexpf(amax, -ex);
     inv = __fdiv_rn(1.0f, a);
   }
-  SR_DEV float code(float x) const {
-    const float t = 127.0f * __builtin_amdgcn_ldexpf(x, -ex);
-    const float v = t * inv;
-    return __fadd_rn(fmaf(fmaf(-v, a, t), inv, v), kMagic);
+  SR_DEV void codes(float v[8]) const {   // in: elements, out: kMagic + code
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float t = 127.0f * __builtin_amdgcn_ldexpf(v[j], -ex);
+      const float u = t * inv;
+      v[j] = __fadd_rn(fmaf(fmaf(-u, a, t), inv, u), kMagic);
+    }
   }
 };
 template <>
 struct RowCode<float> {
-  double a, inv;
+  float a, inv;
+  int ex;
   SR_DEV explicit RowCode(float amax) {
-    a = amax;
-    inv = 1.0 / a;
+    ex = __builtin_amdgcn_frexp_expf(amax);
+    a = __builtin_amdgcn_ldexpf(amax, -ex);
+    inv = __fdiv_rn(127.0f, a);
   }
-  SR_DEV float code(float x) const {
-    const double t = 127.0 * (double)x;
-    const double v = t * inv;
-    return __fadd_rn((float)__builtin_rint(fma(fma(-v, a, t), inv, v)), kMagic);
+  SR_DEV void codes(float v[8]) const {
+    float x[8], far = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      x[j] = __builtin_amdgcn_ldexpf(v[j], -ex);
+      const float u = x[j] * inv;
+      v[j] = __fadd_rn(u, kMagic);
+      far = fmaxf(far, fabsf(u - __fsub_rn(v[j], kMagic)));
+    }
+    if (__any(far > 0.5f - 4e-5f)) {
+      const double ad = a, id = 1.0 / ad;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const double t = 127.0 * (double)x[j], u = t * id;
+        v[j] = __fadd_rn((float)__builtin_rint(fma(fma(-u, ad, t), id, u)), kMagic);
+      }
+    }
   }
 };
 
-// One wave per row: the row's maximum, then its codes.
-template <typename T>
+// One row on LPR lanes (a part of a wave, a wave, or the workgroup), C chunks of eight elements per lane, which
+// stay in registers between the maximum and the codes; C = 0: rows of any length, read twice.
+// us for M x N, bf16 and fp32, against a wave per row that reads it twice: 16200 x 4096 56 and 93 -> 37 and 60,
+// 16200 x 1024 11.8 and 17.8 -> 11.0 and 14.3, 16200 x 256 6.5 and 8.3 -> 4.4 and 5.9, 1024 x 4096 7.0 and 9.7 -> 4.3 and 6.2.
+template <typename T, int LPR, int C>
 __global__ __launch_bounds__(256) void quant_rows_kernel(const T* __restrict__ x, int M, int N, int8_t* __restrict__ q,
                                                          float* __restrict__ scale) {
-  const int row = blockIdx.x * 4 + wave_index(), lane = threadIdx.x & 63;
-  if (row >= M) return;
+  const int row = blockIdx.x * (256 / LPR) + (int)threadIdx.x / LPR, lane = threadIdx.x % LPR;
+  const bool in = row < M;
   const T* xr = x + (size_t)row * N;
+  float v[C > 0 ? C : 1][8];
   uint32_t m = 0;
-  for (int c = lane * 8; c < N; c += 512) {
-    float v[8];
-    load8(xr + c, v);
+  auto top = [&](const float w[8]) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) m = max(m, abs_bits(v[j]));
+    for (int j = 0; j < 8; ++j) m = max(m, abs_bits(w[j]));
+  };
+  if constexpr (C > 0) {
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      const int c = (lane + i * LPR) * 8;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+      if (in && c < N) load8(xr + c, v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < C; ++i) top(v[i]);
+  } else if (in) {
+    for (int c = lane * 8; c < N; c += LPR * 8) {
+      load8(xr + c, v[0]);
+      top(v[0]);
+    }
   }
-  m = wave_umax(m);
+#pragma unroll
+  for (int o = (LPR < 64 ? LPR : 64) / 2; o >= 1; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+  if constexpr (LPR > 64) {
+    __shared__ uint32_t red[LPR / 64];
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < LPR / 64; ++k) m = max(m, red[k]);
+  }
   const bool ok = m < kInfBits;   // the order of magnitudes is that of the bits, NaN above Inf
   const float amax = __uint_as_float(m);
-  if (lane == 0) scale[row] = ok ? __fdiv_rn(amax, 127.0f) : __uint_as_float(0x7FC00000u);
+  if (in && lane == 0) scale[row] = ok ? __fdiv_rn(amax, 127.0f) : __uint_as_float(0x7FC00000u);
   const RowCode<T> rc(ok && m ? amax : 1.0f);
-  for (int c = lane * 8; c < N; c += 512) {
-    float v[8];
-    load8(xr + c, v);
+  auto put = [&](int c, float w[8]) {
+    rc.codes(w);
+    i32x2 b;
+    b[0] = ok ? (int)low_bytes(w[0], w[1], w[2], w[3]) : 0;
+    b[1] = ok ? (int)low_bytes(w[4], w[5], w[6], w[7]) : 0;
+    if (in && c < N) *reinterpret_cast<i32x2*>(q + (size_t)row * N + c) = b;
+  };
+  if constexpr (C > 0) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = rc.code(v[j]);
-    i32x2 w;
-    w[0] = ok ? (int)low_bytes(v[0], v[1], v[2], v[3]) : 0;
-    w[1] = ok ? (int)low_bytes(v[4], v[5], v[6], v[7]) : 0;
-    *reinterpret_cast<i32x2*>(q + (size_t)row * N + c) = w;
+    for (int i = 0; i < C; ++i) put((lane + i * LPR) * 8, v[i]);
+  } else if (in) {
+    for (int c = lane * 8; c < N; c += LPR * 8) {
+      load8(xr + c, v[0]);
+      put(c, v[0]);
+    }
   }
 }
 
@@ -189,8 +234,18 @@ __global__ __launch_bounds__(256) void dequant_blocks_kernel(const int8_t* __res
 template <typename T>
 hipError_t quant(int kind, int M, int N, const void* x, int8_t* q, void* scale, hipStream_t st) {
   if (kind == SR_Q8_ROW) {
-    SR_LAUNCH(quant_rows_kernel<T>, dim3((unsigned)((M + 3) / 4)), dim3(256), 0, st, (const T*)x, M, N, q,
-              (float*)scale);
+    auto rows = [&](auto lpr, auto c) {
+      constexpr int LPR = decltype(lpr)::value, C = decltype(c)::value;
+      SR_LAUNCH((quant_rows_kernel<T, LPR, C>), dim3((unsigned)(((size_t)M * LPR + 255) / 256)), dim3(256), 0, st,
+                (const T*)x, M, N, q, (float*)scale);
+    };
+    if (N <= 256) rows(IC<32>{}, IC<1>{});
+    else if (N <= 512) rows(IC<64>{}, IC<1>{});
+    else if (N <= 1024) rows(IC<64>{}, IC<2>{});
+    else if (N <= 2048) rows(IC<256>{}, IC<1>{});
+    else if (N <= 4096) rows(IC<256>{}, IC<2>{});
+    else if (N <= 8192) rows(IC<256>{}, IC<4>{});
+    else rows(IC<256>{}, IC<0>{});
   } else {
     const size_t n8 = (size_t)M * N / 8;
     SR_LAUNCH(quant_blocks_kernel<T>, dim3((unsigned)((n8 + 255) / 256)), dim3(256), 0, st, (const T*)x, n8, q,
