@@ -112,6 +112,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear8_tile_kernel(Li
   static_assert(MI * 32 * WM == BM && NJ * 32 * WN == BN && APW * RPB * NW == BM && BPW * RPB * NW == BN, "whole tiles");
   static_assert(NST >= 2 && NST <= 4 && (NST - 1) * LPT < 64 && MI + NJ < 16, "counter ranges");
   __shared__ __attribute__((aligned(1024))) char smem[KG * NST * SB];
+  __shared__ __attribute__((aligned(16))) float sc[KG == 1 ? 2 * BN : 4];   // the tile's channel scales, then its biases
 
   const int lane = threadIdx.x & 63, wave = wave_index();
   const int grp = wave / NW, wid = wave % NW;
@@ -124,6 +125,13 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear8_tile_kernel(Li
   const __amdgpu_buffer_rsrc_t ra = make_rsrc(a.xq, (uint32_t)a.M * (uint32_t)a.K);
   const __amdgpu_buffer_rsrc_t rb = make_rsrc(a.wq, (uint32_t)a.N * (uint32_t)a.K);
 
+  if constexpr (KG == 1) {
+    for (int i = threadIdx.x; i < BN; i += NT) {
+      const bool in = n0 + i < a.N;
+      sc[i] = in ? a.ws[n0 + i] : 0.f;
+      sc[BN + i] = in && a.bias ? to_f32<T>(((const T*)a.bias)[n0 + i]) : 0.f;
+    }
+  }
   i32x16 acc[MI][NJ];
 #pragma unroll
   for (int i = 0; i < MI; ++i)
@@ -221,54 +229,43 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear8_tile_kernel(Li
 
   if constexpr (KG == 1) {
     // one group: the weight is the first operand, so that a lane has four consecutive channels of one token in each
-    // register quad (register r: channel 8 (r/4) + 4 h + r%4, token lane % 32) and finishes them where they are
-    float* sc = reinterpret_cast<float*>(smem);   // the tile's channel scales, then its biases
-    for (int i = threadIdx.x; i < BN; i += NT) {
-      const bool in = n0 + i < a.N;
-      sc[i] = in ? a.ws[n0 + i] : 0.f;
-      sc[BN + i] = in && a.bias ? to_f32<T>(((const T*)a.bias)[n0 + i]) : 0.f;
-    }
-    __syncthreads();
+    // register quad (register r: channel 8 (r/4) + 4 h + r%4, token lane % 32) and finishes them where they are.  The
+    // results go through LDS, IPP blocks of every wave row at a time, so that memory sees whole rows of the tile
+    // (16200 x 4096 x 1024: 105 us in 32-byte pieces from the registers, 95 in rows).
+    constexpr int E = sizeof(T), LDB = BN * E + 16, PR = 32 * WM;
+    constexpr int FIT = NST * SB / (PR * LDB), IPP = FIT >= MI ? MI : FIT >= 2 && MI % 2 == 0 ? 2 : 1;
+    static_assert(IPP * PR * LDB <= NST * SB && MI % IPP == 0, "staging fits the stages");
+    constexpr int CPR = BN * E / 16, NB = IPP * PR * CPR / NT;
+    static_assert(NB * NT == IPP * PR * CPR, "whole rounds");
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const int nb = wn * (BN / WN) + 32 * j;
-      Cols cols[4];
+    for (int p = 0; p < MI; p += IPP) {
+      if (p) __syncthreads();
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        cols[q].ws = *reinterpret_cast<const f32x4*>(sc + nb + 8 * q + 4 * h);
-        cols[q].bias = *reinterpret_cast<const f32x4*>(sc + BN + nb + 8 * q + 4 * h);
-      }
-#pragma unroll
-      for (int i = 0; i < MI; ++i) {
-        const int m = m0 + wm * (BM / WM) + 32 * i + (lane & 31);
+      for (int i = 0; i < IPP; ++i) {
+        const int m = m0 + wm * (BM / WM) + 32 * (p + i) + (lane & 31);
         const float xs = m < a.M ? a.xs[m] : 0.f;
-        f32x4 v[4];
+        char* row = smem + ((i * WM + wm) * 32 + (lane & 31)) * LDB;
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          v[q] = finish4<ACT, T>(xs, cols[q], i32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2],
-                                                    acc[i][j][4 * q + 3]});
-        if constexpr (sizeof(T) == 4) {
+        for (int j = 0; j < NJ; ++j) {
+          const int nb = wn * (BN / WN) + 32 * j;
+          f32x4 v[4];
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            const int n = n0 + nb + 8 * q + 4 * h;
-            if (m < a.M && n < a.N) store4<float>(a.y, (size_t)m * a.N + n, v[q]);
-          }
-        } else {
-          // the halves of the wave trade quads: each lane stores eight consecutive channels
-#pragma unroll
-          for (int q = 0; q < 4; q += 2) {
-            i32x4 w;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const auto r = __builtin_amdgcn_permlane32_swap(f2bf2(v[q][2 * e], v[q][2 * e + 1]),
-                                                              f2bf2(v[q + 1][2 * e], v[q + 1][2 * e + 1]), false, false);
-              w[e] = (int)r[0];
-              w[2 + e] = (int)r[1];
-            }
-            const int n = n0 + nb + 8 * q + 8 * h;
-            if (m < a.M && n < a.N) *reinterpret_cast<i32x4*>((bf16_t*)a.y + (size_t)m * a.N + n) = w;
+            const Cols c = {*reinterpret_cast<const f32x4*>(sc + nb + 8 * q + 4 * h),
+                            *reinterpret_cast<const f32x4*>(sc + BN + nb + 8 * q + 4 * h)};
+            v[q] = finish4<ACT, T>(xs, c, i32x4{acc[p + i][j][4 * q], acc[p + i][j][4 * q + 1], acc[p + i][j][4 * q + 2],
+                                                acc[p + i][j][4 * q + 3]});
+            store4<T>(row, nb + 8 * q + 4 * h, v[q]);
           }
         }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const int c = threadIdx.x + NT * b, lr = c / CPR, col = c % CPR * (16 / E), blk = lr >> 5;
+        const int m = m0 + blk % WM * (BM / WM) + 32 * (p + blk / WM) + (lr & 31), n = n0 + col;
+        if (m < a.M && n < a.N)
+          *reinterpret_cast<i32x4*>((T*)a.y + (size_t)m * a.N + n) = *reinterpret_cast<const i32x4*>(smem + lr * LDB + col * E);
       }
     }
   } else {
@@ -392,27 +389,25 @@ hipError_t run_shape(int shape, const Linear8& a, hipStream_t st) {
     case k64x128: return run_tile<64, 128, 128, 2, 4, 1, 4, 1, ACT, T>(a, st);
     case k128x128: return run_tile<128, 128, 128, 2, 4, 1, 4, 1, ACT, T>(a, st);
     case k128x128x2: return run_tile<128, 128, 128, 2, 4, 1, 2, 2, ACT, T>(a, st);
-    case k256x256:
-      // GELU's vector work on four waves per SIMD instead of two: 4050 x 4096 x 1024 30.7 -> 29.0 us, 16200 112 ->
-      // 108; without it eight waves are ahead (8192 x 4096 x 1024 52.0, 57.6)
-      if constexpr (ACT == SR_ACT_GELU) return run_tile<256, 256, 128, 4, 4, 1, 2, 1, ACT, T>(a, st);
-      else return run_tile<256, 256, 128, 2, 4, 1, 2, 1, ACT, T>(a, st);
+    case k256x256: return run_tile<256, 256, 128, 2, 4, 1, 2, 1, ACT, T>(a, st);
   }
   return hipErrorInvalidValue;
 }
 
-// The smallest tile whose grid is one round of workgroups on the 256 CUs; past one round of 128 x 128 the largest,
-// once its own grid is most of a round.  us, bf16 without activation, M x N x K:
+// The smallest tile whose grid is one round of workgroups on the 256 CUs; past one round of 128 x 128 those, two
+// workgroups per CU (one's epilogue under the other's products), or with long rows 256 x 256, once its own grid is most
+// of a round.  us, bf16, M x N x K:
 //   fragments straight from memory, up to one 16 x 16 tile per CU and K <= 1024 (or as much work in more, shorter
 //   tiles):  1 x 4096 x 1024 4.0 (32 x 32 in eight groups 4.9), 64 x 1024 x 1024 4.5 (5.1), 2048 x 64 x 64 3.5
 //   (64 x 64 4.4);  past it 128 x 1024 x 1024 5.5 (5.2), 1 x 1024 x 4096 6.3 (6.1)
 //   32 x 32, eight groups of waves:  128 x 1024 x 4096 6.9 (64 x 64 8.1);  K = 256 4.9 (4.6)
 //   64 x 64, two groups:  1024 x 1024 x 1024 6.2 (64 x 128 7.3);  64 x 128:  2048 x 1024 x 1024 7.7 (8.7, 128 x 128 9.7)
-//   128 x 128, four stages, one workgroup per CU:  4050 x 1024 x 4096 25.5 (two 28.7);  with shorter rows two
-//   workgroups are ahead: 4050 x 1024 x 1024 11.9 (14.6), 16200 x 256 x 1024 12.3 (14.4)
-//   256 x 256:  16200 x 1024 x 1024 27.6 (128 x 128 31.6), 4050 x 4096 x 1024 27.9 (32.5);  with half a round of
-//   them 8192 x 1024 x 4096 45 (42)
-// Tiles of 256 x 128 lie between the two throughout.
+//   128 x 128, four stages, one workgroup per CU:  4050 x 1024 x 4096 22.9 (two 26.1);  with shorter rows two
+//   workgroups are level or ahead: 4050 x 1024 x 1024 10.9 (10.5), 16200 x 256 x 1024 12.3 (14.4)
+//   256 x 256:  16200 x 4096 x 1024 95 (106), 16200 x 1024 x 4096 67 (80), 16200 x 2048 x 512 36 (32);  with half a
+//   round of them 8192 x 1024 x 4096 45 (42);  with GELU, whose vector work wants the second workgroup,
+//   16200 x 2048 x 2048 88 (94), 16200 x 4096 x 1024 123 (122), 8192 x 4096 x 1024 62 (57)
+// Tiles of 256 x 128 and sixteen waves lie within 4 % of these.
 int pick_shape(const Linear8& a) {
   auto tiles = [&](int bm, int bn) { return (long)((a.M + bm - 1) / bm) * ((a.N + bn - 1) / bn); };
   const long t16 = tiles(16, 16);
@@ -421,7 +416,7 @@ int pick_shape(const Linear8& a) {
   if (tiles(64, 64) <= 256) return k64x64g2;
   if (tiles(64, 128) <= 256) return k64x128;
   if (a.K >= 2048 && tiles(128, 128) <= 256) return k128x128;
-  return tiles(256, 256) >= 200 ? k256x256 : k128x128x2;
+  return a.K >= (a.act == SR_ACT_GELU ? 2048 : 1024) && tiles(256, 256) >= 200 ? k256x256 : k128x128x2;
 }
 
 template <typename T>

@@ -5,8 +5,8 @@ make them wait for global-to-LDS fills in flight; the compiler then does not kno
 registers are written.  The kernels wait (s_waitcnt lgkmcnt) before using them, which is only
 sound if no instruction -- a copy, a spill, another use, or the kernel's own consumer -- touches a
 destination register between the read and the wait that retires it.  This scan checks exactly
-that on the compiled code: LDS reads retire in issue order, s_waitcnt lgkmcnt(N) leaves the last N
-in flight, and any vector instruction reading or writing a register of a read still in flight is
+that on the compiled code: LDS reads and writes retire in issue order, s_waitcnt lgkmcnt(N) leaves the
+last N in flight, and any vector instruction reading or writing a register of a read still in flight is
 reported.
 
 The check follows the control flow: the function is split into basic blocks (labels, branches,
@@ -92,6 +92,12 @@ def _run(block: list[str], pending: list, count: bool):
             pending = pending[-_MAXLEN:]
             continue
         if op.startswith("s_"):
+            continue
+        if op.startswith("ds_write") or op.startswith("ds_store"):   # retires in order with the reads
+            if count and set().union(*(_regs(x) for x in ops)) & live:
+                hits.append(t)
+            pending.append(frozenset())
+            pending = pending[-_MAXLEN:]
             continue
         touched = set().union(*(_regs(x) for x in ops)) if ops else set()
         if count and touched & live:

@@ -104,3 +104,29 @@ def test_weight_grad_scratch_never_falls_with_tokens(dtype, N, K):
         n = abi.sr_weight_grad8_scratch_bytes(dtype, M, N, K)
         assert n >= last, (M, last, n)
         last = n
+
+
+def test_scan_counts_lds_writes():
+    # an LDS write behind a read takes its place in the counter: lgkmcnt(1) then retires the read; a write of a
+    # register that a read is still filling is a hazard
+    from paper_2607_02829_amd.isa_scan import kernel_hazards
+    asm = """_Zkept:
+\tds_read_b128 v[0:3], v9 offset:0
+\tds_write_b64 v10, v[20:21] offset:0
+\ts_waitcnt lgkmcnt(1)
+\tv_add_u32 v11, v0, v1
+.Lfunc_end0:
+_Zearly:
+\tds_read_b128 v[0:3], v9 offset:0
+\tds_read_b128 v[4:7], v9 offset:64
+\tds_write_b64 v10, v[20:21] offset:0
+\ts_waitcnt lgkmcnt(2)
+\tv_add_u32 v11, v0, v4
+.Lfunc_end1:
+_Zstore:
+\tds_read_b128 v[0:3], v9 offset:0
+\tds_write_b64 v10, v[2:3] offset:0
+\ts_waitcnt lgkmcnt(0)
+.Lfunc_end2:
+"""
+    assert kernel_hazards(asm) == {"_Zkept": 0, "_Zearly": 1, "_Zstore": 1}
