@@ -394,7 +394,7 @@ SR_API sr_status sr_linear8(int32_t dtype, int32_t act, int32_t M, int32_t N, in
  *   dy [M,N] storage type;  xq [M,K], xe [M,K/32]: the checkpoint, read in 8 bits;
  *   dw [N,K] fp32 and db [N] fp32 (or NULL), overwritten.  Every product is exact and sums are fp32,
  *   in a fixed order (deterministic).  scratch: sr_weight_grad8_scratch_bytes bytes (NULL when 0).
- * M >= 1, N % 8 == 0, K % 64 == 0; M*N*elt, M*K and N*K*4 < 2^31 bytes. */
+ * M >= 1, N % 8 == 0, K % 64 == 0, K <= 65536; M*N*elt, M*K and N*K*4 < 2^31 bytes. */
 SR_API sr_status sr_weight_grad8_scratch_bytes(int32_t dtype, int32_t M, int32_t N, int32_t K,
                                         size_t* scratch_bytes);
 SR_API sr_status sr_weight_grad8(int32_t dtype, int32_t M, int32_t N, int32_t K, const void* dy, const int8_t* xq,

@@ -582,6 +582,7 @@ sr_status check_product8(int32_t dtype, int32_t M, int32_t N, int32_t K) {
   if (s != SR_OK) return s;
   SR_CHECK(N >= 1, SR_EINVAL, "sizes must be positive (N=%d)", N);
   SR_CHECK(N % 8 == 0, SR_EUNSUPPORTED, "N=%d must be a multiple of 8", N);
+  SR_CHECK(K <= 65536, SR_EUNSUPPORTED, "K=%d > 65536", K);
   SR_CHECK(fits31(M, K, 1) && fits31(M, N, (int64_t)elt_of(dtype)), SR_EUNSUPPORTED,
            "tensors beyond 2 GiB are not supported (M=%d N=%d K=%d)", M, N, K);
   return SR_OK;
@@ -626,7 +627,6 @@ sr_status sr_linear8(int32_t dtype, int32_t act, int32_t M, int32_t N, int32_t K
   sr_status s = check_product8(dtype, M, N, K);
   if (s != SR_OK) return s;
   SR_CHECK(act == SR_ACT_NONE || act == SR_ACT_GELU, SR_EINVAL, "unknown activation %d", act);
-  SR_CHECK(K <= 65536, SR_EUNSUPPORTED, "K=%d > 65536", K);
   SR_CHECK(fits31(N, K, 1), SR_EUNSUPPORTED, "a weight beyond 2 GiB is not supported (N=%d K=%d)", N, K);
   SR_PTR(xq, "xq");
   SR_PTR(xs, "xs");

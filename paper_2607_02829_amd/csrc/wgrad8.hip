@@ -1,59 +1,293 @@
 // Weight and bias gradient of a linear layer from the 8-bit checkpoint of its input:
 //   dw[n, k] = sum_m dy[m, n] xhat[m, k],   db[n] = sum_m dy[m, n],   xhat = q 2^e (SR_Q8_BLOCK).
+//
+// xhat is exact in bf16, so bf16 gradients take one product of v_mfma_f32_32x32x16_bf16 per term, exact before
+// the fp32 sum.  fp32 gradients are cut into three bf16 parts of eight significant bits each, dy = hi + mid + lo
+// without a remainder, and take three products per term: a third of the bf16 rate, which is five times
+// that of the fp32 matrix instructions.
+//
+// Both operands are token-major and the sum runs over tokens.  A workgroup takes 64 tokens at a time: each
+// thread loads 16-byte pieces of dy and of the codes into registers, one tile ahead, turns codes (and fp32
+// gradients) into bf16 and writes them to one of two LDS stages while the other is multiplied; fragments come
+// out of the transposing LDS reads.  The codes are a byte each on their way from memory and are decoded once per
+// workgroup.  Few output tiles are cut over tokens into planes that a second launch adds in order.
+#include <algorithm>
+
 #include "common.h"
 #include "quant8.h"
 #include "sr_internal.h"
+#include "tiles.h"
 
 namespace sr {
 
 namespace {
 
-// 64 x 64 tiles of dw in fp32, 16 tokens at a time through LDS; the tiles of the first column of
-// tiles also sum db.
+constexpr int TM = 64;   // tokens per tile
+
+// LDS tile of TM token rows of R values: the 16-byte chunk c of row m at position c ^ rowswz(m), so that
+// the four rows that a transposing read touches lie in different banks.
+template <int R>
+SR_DEV int rowswz(int m) {
+  return R >= 128 ? (m & 3) << 2 : R == 64 ? ((m >> 1) & 1) << 2 : 0;
+}
+
+// The upper halves of two fp32 values as a pair of bf16 (truncated).
+SR_DEV uint32_t upper2(float lo, float hi) {
+  return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+}
+SR_DEV float truncated(float v) { return __uint_as_float(__float_as_uint(v) & 0xFFFF0000u); }
+
+// Eight gradients of one token in flight: raw[0 ..) and their P bf16 parts.
 template <typename T>
-__global__ __launch_bounds__(256) void wgrad8_kernel(Wgrad8 a) {
-  __shared__ float sy[16][64], sx[16][64];
-  const int n0 = blockIdx.y * 64, k0 = blockIdx.x * 64, t = threadIdx.x;
-  const int tn = (t >> 4) * 4, tk = (t & 15) * 4;
-  float acc[4][4] = {}, sum = 0.f;
-  for (int m0 = 0; m0 < a.M; m0 += 16) {
-    for (int i = t; i < 1024; i += 256) {
-      const int m = m0 + (i >> 6), c = i & 63;
-      const bool in = m < a.M;
-      sy[i >> 6][c] = in && n0 + c < a.N ? to_f32<T>(((const T*)a.dy)[(size_t)m * a.N + n0 + c]) : 0.f;
-      const size_t o = (size_t)m * a.K + k0 + c;
-      sx[i >> 6][c] = in ? (float)a.xq[o] * block_scale(a.xe[o / kQBlock]) : 0.f;
-    }
-    __syncthreads();
-#pragma unroll 4
-    for (int m = 0; m < 16; ++m) {
-      const f32x4 y = *reinterpret_cast<const f32x4*>(&sy[m][tn]), x = *reinterpret_cast<const f32x4*>(&sx[m][tk]);
+struct Grad8;
+template <>
+struct Grad8<bf16_t> {
+  static constexpr int P = 1;
+  i32x4 raw;
+  SR_DEV void load(__amdgpu_buffer_rsrc_t r, uint32_t off) { raw = buf_load16(r, off); }
+  SR_DEV void parts(i32x4 p[P]) const { p[0] = raw; }
+  SR_DEV void add(float* s) const {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(y[i], x[j], acc[i][j]);
-      if (t < 64) sum += sy[m][t];
+    for (int j = 0; j < 4; ++j) {
+      s[2 * j] += __uint_as_float((uint32_t)raw[j] << 16);
+      s[2 * j + 1] += __uint_as_float((uint32_t)raw[j] & 0xFFFF0000u);
     }
-    __syncthreads();
   }
+};
+template <>
+struct Grad8<float> {
+  static constexpr int P = 3;
+  i32x4 raw[2];
+  SR_DEV void load(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+    raw[0] = buf_load16(r, off);
+    raw[1] = buf_load16(r, off + 16);
+  }
+  SR_DEV float at(int j) const { return __int_as_float(raw[j >> 2][j & 3]); }
+  // truncation leaves an exact remainder of the bits below: 24 = 8 + 8 + 8
+  SR_DEV void parts(i32x4 p[P]) const {
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (n0 + tn + i < a.N) {
-      const f32x4 v = {acc[i][0], acc[i][1], acc[i][2], acc[i][3]};
-      *reinterpret_cast<f32x4*>(a.dw + (size_t)(n0 + tn + i) * a.K + k0 + tk) = v;
+    for (int j = 0; j < 4; ++j) {
+      const float a = at(2 * j), b = at(2 * j + 1);
+      const float ra = a - truncated(a), rb = b - truncated(b);
+      p[0][j] = (int)upper2(a, b);
+      p[1][j] = (int)upper2(ra, rb);
+      p[2][j] = (int)upper2(ra - truncated(ra), rb - truncated(rb));
     }
-  if (a.db && blockIdx.x == 0 && t < 64 && n0 + t < a.N) a.db[n0 + t] = sum;
+  }
+  SR_DEV void add(float* s) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s[j] += at(j);
+  }
+};
+
+// BN x BK tile of dw on WN x WK waves.
+template <typename T, int BN, int BK, int WN, int WK, int OCC>
+__global__ __launch_bounds__(64 * WN * WK, OCC) void wgrad8_kernel(Wgrad8 a, int tiles_n, int tiles_k, int per_split) {
+  constexpr int NT = 64 * WN * WK, P = Grad8<T>::P;
+  constexpr int NI = BN / (32 * WN), KJ = BK / (32 * WK);
+  constexpr int STAGE = TM * (P * BN + BK);                        // bf16 elements: the parts of dy, then xhat
+  constexpr int GR = NT / (BN / 8), GL = TM / GR;                  // dy: rows per round of loads, rounds
+  constexpr int XR = NT / (BK / 16), XL = TM / XR;                 // codes
+  static_assert(GL * GR == TM && XL * XR == TM, "whole rounds of loads");
+  __shared__ __attribute__((aligned(1024))) bf16_t smem[2 * STAGE];
+  const int lane = threadIdx.x & 63, wave = wave_index(), h = lane >> 5;
+  const int wn = wave / WK, wk = wave % WK;
+  int tn, tk, split;
+  tile_coords(blockIdx.x, gridDim.x, tiles_n, tiles_k, tn, tk, split);
+  const int n0 = tn * BN, k0 = tk * BK, mbeg = split * per_split, mend = min(a.M, mbeg + per_split);
+  const int ntile = mbeg < mend ? (mend - mbeg + TM - 1) / TM : 0;
+  const __amdgpu_buffer_rsrc_t ry = make_rsrc(a.dy, (uint32_t)((size_t)a.M * a.N * sizeof(T)));
+  const __amdgpu_buffer_rsrc_t rx = make_rsrc(a.xq, (uint32_t)((size_t)a.M * a.K));
+  const __amdgpu_buffer_rsrc_t re = make_rsrc(a.xe, (uint32_t)((size_t)a.M * (a.K / kQBlock)));
+
+  // this thread's pieces: dy chunk gc of rows gr + i GR, codes 16 xc .. of rows xr + i XR
+  const int gc = threadIdx.x % (BN / 8), gr = threadIdx.x / (BN / 8);
+  const int xc = threadIdx.x % (BK / 16), xr = threadIdx.x / (BK / 16);
+  const bool gin = n0 + gc * 8 < a.N, xin = k0 + xc * 16 < a.K;
+  Grad8<T> g[GL];
+  i32x4 xv[XL];
+  uint32_t xe[XL];
+  auto load = [&](int t) {   // rows past the last token lie past the operands: zeros
+#pragma unroll
+    for (int i = 0; i < GL; ++i) {
+      const uint32_t m = (uint32_t)(mbeg + t * TM + gr + i * GR);
+      g[i].load(ry, t < ntile && gin ? (m * (uint32_t)a.N + (uint32_t)(n0 + gc * 8)) * (uint32_t)sizeof(T) : 0x80000000u);
+    }
+#pragma unroll
+    for (int i = 0; i < XL; ++i) {
+      const uint32_t m = (uint32_t)(mbeg + t * TM + xr + i * XR), k = (uint32_t)(k0 + xc * 16);
+      const bool in = t < ntile && xin;
+      xv[i] = buf_load16(rx, in ? m * (uint32_t)a.K + k : 0x80000000u);
+      xe[i] = __builtin_amdgcn_raw_buffer_load_b8(re, in ? m * (uint32_t)(a.K / kQBlock) + k / kQBlock : 0x80000000u, 0, 0);
+    }
+  };
+  const bool want_db = a.db && tk == 0;
+  float dbv[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  auto write = [&](bf16_t* st) {
+#pragma unroll
+    for (int i = 0; i < GL; ++i) {
+      const int m = gr + i * GR;
+      i32x4 p[P];
+      g[i].parts(p);
+#pragma unroll
+      for (int q = 0; q < P; ++q)
+        *reinterpret_cast<i32x4*>(st + q * TM * BN + m * BN + ((gc ^ rowswz<BN>(m)) << 3)) = p[q];
+      if (want_db) g[i].add(dbv);
+    }
+#pragma unroll
+    for (int i = 0; i < XL; ++i) {
+      const int m = xr + i * XR;
+      const float s = block_scale(xe[i]);
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        i32x4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int b = xv[i][2 * c + (j >> 1)] >> (16 * (j & 1));
+          w[j] = (int)f2bf2((float)(int8_t)b * s, (float)(int8_t)(b >> 8) * s);
+        }
+        *reinterpret_cast<i32x4*>(st + P * TM * BN + m * BK + (((2 * xc + c) ^ rowswz<BK>(m)) << 3)) = w;
+      }
+    }
+  };
+
+  // fragment of columns cb .. cb + 31 (lane: column lane % 32) at tokens 16 ks + 8 h .. + 7: two reads of four tokens
+  const int fm = 8 * (lane >> 5) + ((lane & 15) >> 2), fc = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+  auto frag = [&](const bf16_t* tile, auto rc, int cb, int ks) {
+    constexpr int R = decltype(rc)::value;
+    const int c = cb + fc;
+    const bf16_t* p = tile + (16 * ks + fm) * R + (((c >> 3) ^ rowswz<R>(fm)) << 3) + (c & 7);
+    i32x4 v;
+    const i32x2 lo = __builtin_bit_cast(i32x2, ds_tr(p)), hi = __builtin_bit_cast(i32x2, ds_tr(p + 4 * R));
+    v[0] = lo[0]; v[1] = lo[1]; v[2] = hi[0]; v[3] = hi[1];
+    return __builtin_bit_cast(bf16x8, v);
+  };
+  f32x16 acc[NI][KJ];
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+#pragma unroll
+    for (int j = 0; j < KJ; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+
+  load(0);
+  write(smem);
+  load(1);
+  for (int t = 0; t < ntile; ++t) {
+    const bf16_t* st = smem + (t & 1) * STAGE;
+    __syncthreads();   // tile t is written, and every wave is done with the other stage
+    write(smem + ((t + 1) & 1) * STAGE);
+    load(t + 2);
+#pragma unroll
+    for (int ks = 0; ks < TM / 16; ++ks) {
+      bf16x8 fx[KJ];
+#pragma unroll
+      for (int j = 0; j < KJ; ++j) fx[j] = frag(st + P * TM * BN, IC<BK>{}, wk * (BK / WK) + 32 * j, ks);
+#pragma unroll
+      for (int q = P - 1; q >= 0; --q)
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          const bf16x8 fg = frag(st + q * TM * BN, IC<BN>{}, wn * (BN / WN) + 32 * i, ks);
+#pragma unroll
+          for (int j = 0; j < KJ; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fg, fx[j], acc[i][j], 0, 0, 0);
+        }
+    }
+  }
+
+  const bool cut = per_split < a.M;
+  float* dw = cut ? a.scratch + (size_t)split * a.N * a.K : a.dw;
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+#pragma unroll
+    for (int j = 0; j < KJ; ++j) {
+      const int k = k0 + wk * (BK / WK) + 32 * j + (lane & 31);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {   // register r: row 8 (r/4) + 4 h + r%4
+        const int n = n0 + wn * (BN / WN) + 32 * i + 8 * (r >> 2) + 4 * h + (r & 3);
+        if (n < a.N && k < a.K) dw[(size_t)n * a.K + k] = acc[i][j][r];
+      }
+    }
+  if (want_db) {   // the threads of one chunk, in row order
+    __syncthreads();
+    float* red = reinterpret_cast<float*>(smem);   // [GR][BN]
+#pragma unroll
+    for (int e = 0; e < 8; ++e) red[gr * BN + gc * 8 + e] = dbv[e];
+    __syncthreads();
+    for (int c = threadIdx.x; c < BN; c += NT) {
+      float s = 0.f;
+      for (int r = 0; r < GR; ++r) s += red[r * BN + c];
+      const int n = n0 + c;
+      if (n < a.N) (cut ? a.scratch + (size_t)gridDim.x / (tiles_n * tiles_k) * a.N * a.K + (size_t)split * a.N : a.db)[n] = s;
+    }
+  }
+}
+
+// The planes of a cut sum, in order: four values of dw per thread, then those of db.
+__global__ __launch_bounds__(256) void wgrad8_sum_kernel(const float* __restrict__ part, int splits, size_t n4, size_t b4,
+                                                         float* __restrict__ dw, float* __restrict__ db) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n4 + b4) return;
+  const bool w = i < n4;
+  const f32x4* p = reinterpret_cast<const f32x4*>(part) + (w ? i : (size_t)splits * n4 + (i - n4));
+  const size_t step = w ? n4 : b4;
+  f32x4 s = p[0];
+  for (int z = 1; z < splits; ++z) s += p[(size_t)z * step];
+  (w ? reinterpret_cast<f32x4*>(dw)[i] : reinterpret_cast<f32x4*>(db)[i - n4]) = s;
+}
+
+enum Shape { k64x64, k128x128, k128x256 };
+struct Plan {
+  int shape, splits, per_split, tiles_n, tiles_k;
+};
+Plan plan(int dtype, int M, int N, int K) {
+  auto tiles = [&](int bn, int bk) { return (long)((N + bn - 1) / bn) * ((K + bk - 1) / bk); };
+  Plan p;
+  p.shape = tiles(128, 128) >= 128 ? k128x128 : k64x64;
+  const int bn = p.shape == k64x64 ? 64 : 128, bk = p.shape == k64x64 ? 64 : p.shape == k128x128 ? 128 : 256;
+  p.tiles_n = (N + bn - 1) / bn;
+  p.tiles_k = (K + bk - 1) / bk;
+  const long t = (long)p.tiles_n * p.tiles_k;
+  p.splits = (int)std::max(1l, std::min({512 / t, 8l, (long)M / 256}));
+  p.per_split = ((M + p.splits - 1) / p.splits + TM - 1) / TM * TM;
+  (void)dtype;
+  return p;
+}
+
+template <typename T, int BN, int BK, int WN, int WK, int OCC>
+hipError_t run(const Wgrad8& a, const Plan& p, hipStream_t st) {
+  const int n = p.splits > 1 ? (a.M + p.per_split - 1) / p.per_split : 1;
+  SR_LAUNCH((wgrad8_kernel<T, BN, BK, WN, WK, OCC>), dim3((unsigned)(p.tiles_n * p.tiles_k * n)), dim3(64 * WN * WK), 0,
+            st, a, p.tiles_n, p.tiles_k, n > 1 ? p.per_split : a.M);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || n == 1) return e;
+  const size_t n4 = (size_t)a.N * a.K / 4, b4 = a.db ? (size_t)a.N / 4 : 0;
+  SR_LAUNCH(wgrad8_sum_kernel, dim3((unsigned)((n4 + b4 + 255) / 256)), dim3(256), 0, st, a.scratch, n, n4, b4, a.dw,
+            a.db);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t dispatch(const Wgrad8& a, const Plan& p, hipStream_t st) {
+  constexpr bool F = sizeof(T) == 4;
+  switch (p.shape) {
+    case k64x64: return run<T, 64, 64, 2, 2, 2>(a, p, st);
+    case k128x128: return run<T, 128, 128, 2, 2, F ? 1 : 2>(a, p, st);
+    case k128x256: return run<T, 128, 256, 2, 4, 1>(a, p, st);
+  }
+  return hipErrorInvalidValue;
 }
 
 }  // namespace
 
-size_t wgrad8_scratch(int, int, int, int) { return 0; }
+size_t wgrad8_scratch(int dtype, int M, int N, int K) {
+  const Plan p = plan(dtype, M, N, K);
+  return p.splits > 1 ? (size_t)p.splits * ((size_t)N * K + N) * 4 : 0;
+}
 
 hipError_t launch_wgrad8(int dtype, const Wgrad8& a, hipStream_t st) {
-  const dim3 grid((unsigned)(a.K / 64), (unsigned)((a.N + 63) / 64));
-  if (dtype == kBF16) SR_LAUNCH(wgrad8_kernel<bf16_t>, grid, dim3(256), 0, st, a);
-  else SR_LAUNCH(wgrad8_kernel<float>, grid, dim3(256), 0, st, a);
-  return hipGetLastError();
+  const Plan p = plan(dtype, a.M, a.N, a.K);
+  return dtype == kBF16 ? dispatch<bf16_t>(a, p, st) : dispatch<float>(a, p, st);
 }
 
 }  // namespace sr
