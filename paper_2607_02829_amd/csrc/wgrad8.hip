@@ -7,10 +7,14 @@
 // that of the fp32 matrix instructions.
 //
 // Both operands are token-major and the sum runs over tokens.  A workgroup takes 64 tokens at a time: each
-// thread loads 16-byte pieces of dy and of the codes into registers, one tile ahead, turns codes (and fp32
+// thread loads 16-byte pieces of dy and of the codes into registers, two tiles ahead, turns codes (and fp32
 // gradients) into bf16 and writes them to one of two LDS stages while the other is multiplied; fragments come
 // out of the transposing LDS reads.  The codes are a byte each on their way from memory and are decoded once per
 // workgroup.  Few output tiles are cut over tokens into planes that a second launch adds in order.
+//
+// What bounds it: at 16200 x 1024 x 4096 the matrix pipes are busy 42 % of the time, the LDS 42 % and the vector
+// units 25 %; a wave issues in order, so fragment reads, decoding and writes are placed between its products
+// (256 x 128 tiles 177 us with the writes before the products, 157 so; 0.87 PFLOP/s).
 #include <algorithm>
 
 #include "common.h"
@@ -104,50 +108,60 @@ __global__ __launch_bounds__(64 * WN * WK, OCC) void wgrad8_kernel(Wgrad8 a, int
   const int gc = threadIdx.x % (BN / 8), gr = threadIdx.x / (BN / 8);
   const int xc = threadIdx.x % (BK / 16), xr = threadIdx.x / (BK / 16);
   const bool gin = n0 + gc * 8 < a.N, xin = k0 + xc * 16 < a.K;
-  Grad8<T> g[GL];
-  i32x4 xv[XL];
-  uint32_t xe[XL];
-  auto load = [&](int t) {   // rows past the last token lie past the operands: zeros
+  // pieces of a tile: GL of dy, then XL of codes, which are written in two halves; two tiles of them in flight
+  constexpr int NP = GL + XL, NWR = GL + 2 * XL;
+  Grad8<T> g[2][GL];
+  i32x4 xv[2][XL];
+  uint32_t xe[2][XL];
+  // byte offsets of the next tile's pieces.  Rows past the last token lie past the operands and read zeros, as do the
+  // offsets from 2^31 of channels past the last; tiles past the last read rows that nothing uses.
+  uint32_t go[GL], xo[XL], eo[XL];
 #pragma unroll
-    for (int i = 0; i < GL; ++i) {
-      const uint32_t m = (uint32_t)(mbeg + t * TM + gr + i * GR);
-      g[i].load(ry, t < ntile && gin ? (m * (uint32_t)a.N + (uint32_t)(n0 + gc * 8)) * (uint32_t)sizeof(T) : 0x80000000u);
-    }
+  for (int i = 0; i < GL; ++i)
+    go[i] = gin ? ((uint32_t)(mbeg + gr + i * GR) * (uint32_t)a.N + (uint32_t)(n0 + gc * 8)) * (uint32_t)sizeof(T) : 0x80000000u;
 #pragma unroll
-    for (int i = 0; i < XL; ++i) {
-      const uint32_t m = (uint32_t)(mbeg + t * TM + xr + i * XR), k = (uint32_t)(k0 + xc * 16);
-      const bool in = t < ntile && xin;
-      xv[i] = buf_load16(rx, in ? m * (uint32_t)a.K + k : 0x80000000u);
-      xe[i] = __builtin_amdgcn_raw_buffer_load_b8(re, in ? m * (uint32_t)(a.K / kQBlock) + k / kQBlock : 0x80000000u, 0, 0);
+  for (int i = 0; i < XL; ++i) {
+    const uint32_t m = (uint32_t)(mbeg + xr + i * XR), k = (uint32_t)(k0 + xc * 16);
+    xo[i] = xin ? m * (uint32_t)a.K + k : 0x80000000u;
+    eo[i] = xin ? m * (uint32_t)(a.K / kQBlock) + k / kQBlock : 0x80000000u;
+  }
+  const uint32_t gstep = gin ? (uint32_t)(TM * sizeof(T)) * (uint32_t)a.N : 0u, xstep = xin ? (uint32_t)(TM * a.K) : 0u;
+  auto load = [&](auto bv, auto pv) {
+    constexpr int B = decltype(bv)::value, p = decltype(pv)::value;
+    if constexpr (p < GL) {
+      g[B][p].load(ry, go[p]);
+      go[p] += gstep;
+    } else {
+      constexpr int i = p - GL;
+      xv[B][i] = buf_load16(rx, xo[i]);
+      xe[B][i] = __builtin_amdgcn_raw_buffer_load_b8(re, eo[i], 0, 0);
+      xo[i] += xstep;
+      eo[i] += xstep / kQBlock;
     }
   };
   const bool want_db = a.db && tk == 0;
   float dbv[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  auto write = [&](bf16_t* st) {
-#pragma unroll
-    for (int i = 0; i < GL; ++i) {
-      const int m = gr + i * GR;
+  auto write = [&](auto bv, auto wv, bf16_t* st, bool used) {
+    constexpr int B = decltype(bv)::value, w = decltype(wv)::value;
+    if constexpr (w < GL) {
+      const int m = gr + w * GR;
       i32x4 p[P];
-      g[i].parts(p);
+      g[B][w].parts(p);
 #pragma unroll
       for (int q = 0; q < P; ++q)
         *reinterpret_cast<i32x4*>(st + q * TM * BN + m * BN + ((gc ^ rowswz<BN>(m)) << 3)) = p[q];
-      if (want_db) g[i].add(dbv);
-    }
-#pragma unroll
-    for (int i = 0; i < XL; ++i) {
+      if (want_db && used) g[B][w].add(dbv);
+    } else {
+      constexpr int i = (w - GL) / 2, c = (w - GL) % 2;
       const int m = xr + i * XR;
-      const float s = block_scale(xe[i]);
+      const float s = block_scale(xe[B][i]);
+      i32x4 v;
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        i32x4 w;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int b = xv[i][2 * c + (j >> 1)] >> (16 * (j & 1));
-          w[j] = (int)f2bf2((float)(int8_t)b * s, (float)(int8_t)(b >> 8) * s);
-        }
-        *reinterpret_cast<i32x4*>(st + P * TM * BN + m * BK + (((2 * xc + c) ^ rowswz<BK>(m)) << 3)) = w;
+      for (int j = 0; j < 4; ++j) {
+        const int b = xv[B][i][2 * c + (j >> 1)] >> (16 * (j & 1));
+        v[j] = (int)f2bf2((float)(int8_t)b * s, (float)(int8_t)(b >> 8) * s);
       }
+      *reinterpret_cast<i32x4*>(st + P * TM * BN + m * BK + (((2 * xc + c) ^ rowswz<BK>(m)) << 3)) = v;
     }
   };
 
@@ -170,30 +184,57 @@ __global__ __launch_bounds__(64 * WN * WK, OCC) void wgrad8_kernel(Wgrad8 a, int
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
-  load(0);
-  write(smem);
-  load(1);
-  for (int t = 0; t < ntile; ++t) {
-    const bf16_t* st = smem + (t & 1) * STAGE;
+  static_for<NP>([&](auto p) { load(IC<0>{}, p); });
+  static_for<NP>([&](auto p) { load(IC<1>{}, p); });
+  static_for<NWR>([&](auto w) { write(IC<0>{}, w, smem, true); });
+  static_for<NP>([&](auto p) { load(IC<0>{}, p); });
+  // tile t, whose stage has parity S: its products, with the pieces of tile t + 1 written and those of t + 3
+  // fetched in between
+  constexpr int KS = TM / 16;
+  auto body = [&](int t, auto sidx) {
+    constexpr int S = decltype(sidx)::value;
+    const bf16_t* st = smem + S * STAGE;
+    bf16_t* next = smem + (1 - S) * STAGE;
     __syncthreads();   // tile t is written, and every wave is done with the other stage
-    write(smem + ((t + 1) & 1) * STAGE);
-    load(t + 2);
-#pragma unroll
-    for (int ks = 0; ks < TM / 16; ++ks) {
-      bf16x8 fx[KJ];
-#pragma unroll
-      for (int j = 0; j < KJ; ++j) fx[j] = frag(st + P * TM * BN, IC<BK>{}, wk * (BK / WK) + 32 * j, ks);
-#pragma unroll
-      for (int q = P - 1; q >= 0; --q)
-#pragma unroll
-        for (int i = 0; i < NI; ++i) {
-          const bf16x8 fg = frag(st + q * TM * BN, IC<BN>{}, wn * (BN / WN) + 32 * i, ks);
-#pragma unroll
-          for (int j = 0; j < KJ; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fg, fx[j], acc[i][j], 0, 0, 0);
+    // fragments of k-step ks: the KJ of xhat, then the NI of each part of dy
+    bf16x8 fx[2][KJ], fg[2][P * NI];
+    auto read = [&](auto ksv, auto fv) {
+      constexpr int ks = decltype(ksv)::value, f = decltype(fv)::value;
+      if constexpr (f < KJ) fx[ks & 1][f] = frag(st + P * TM * BN, IC<BK>{}, wk * (BK / WK) + 32 * f, ks);
+      else fg[ks & 1][f - KJ] = frag(st + (f - KJ) / NI * TM * BN, IC<BN>{}, wn * (BN / WN) + 32 * ((f - KJ) % NI), ks);
+    };
+    constexpr int NF = KJ + P * NI, NX = P * NI * KJ, SLOTS = KS * NX;
+    static_for<NF>([&](auto f) { read(IC<0>{}, f); });
+    static_for<KS>([&](auto ksv) {
+      constexpr int ks = decltype(ksv)::value;
+      static_for<NX>([&](auto xv_) {
+        constexpr int X = decltype(xv_)::value, qi = X / KJ, j = X % KJ, Y = ks * NX + X;
+        acc[qi % NI][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fg[ks & 1][qi], fx[ks & 1][j], acc[qi % NI][j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        // under this product: a share of the next k-step's fragment reads, of the next tile's writes and of the loads
+        if constexpr (ks + 1 < KS) {
+          constexpr int F0 = X * NF / NX, F1 = (X + 1) * NF / NX;
+          static_for<F1 - F0>([&](auto f) { read(IC<ks + 1>{}, IC<F0 + decltype(f)::value>{}); });
         }
-    }
+        constexpr int W0 = Y * NWR / SLOTS, W1 = (Y + 1) * NWR / SLOTS;
+        static_for<W1 - W0>([&](auto wv) {
+          constexpr int w = W0 + decltype(wv)::value;
+          write(IC<1 - S>{}, IC<w>{}, next, t + 1 < ntile);
+          if constexpr (w < GL) load(IC<1 - S>{}, IC<w>{});
+          else if constexpr ((w - GL) % 2 == 1) load(IC<1 - S>{}, IC<GL + (w - GL) / 2>{});
+        });
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    });
+  };
+  // whole pairs in the loop: a way around the second body would make the waits on the first one's loads those of
+  // the shorter way, with one tile in flight instead of two
+  int t = 0;
+  for (; t + 1 < ntile; t += 2) {
+    body(t, IC<0>{});
+    body(t + 1, IC<1>{});
   }
+  if (t < ntile) body(t, IC<0>{});
 
   const bool cut = per_split < a.M;
   float* dw = cut ? a.scratch + (size_t)split * a.N * a.K : a.dw;
@@ -223,34 +264,55 @@ __global__ __launch_bounds__(64 * WN * WK, OCC) void wgrad8_kernel(Wgrad8 a, int
   }
 }
 
-// The planes of a cut sum, in order: four values of dw per thread, then those of db.
-__global__ __launch_bounds__(256) void wgrad8_sum_kernel(const float* __restrict__ part, int splits, size_t n4, size_t b4,
-                                                         float* __restrict__ dw, float* __restrict__ db) {
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+// The planes of a cut sum, in order: four values of dw per thread, then those of db; four planes are fetched at
+// once.  One wave per workgroup, so that a small gradient spreads over the CUs.
+__global__ __launch_bounds__(64) void wgrad8_sum_kernel(const float* __restrict__ part, int splits, size_t n4, size_t b4,
+                                                        float* __restrict__ dw, float* __restrict__ db) {
+  const size_t i = (size_t)blockIdx.x * 64 + threadIdx.x;
   if (i >= n4 + b4) return;
   const bool w = i < n4;
   const f32x4* p = reinterpret_cast<const f32x4*>(part) + (w ? i : (size_t)splits * n4 + (i - n4));
   const size_t step = w ? n4 : b4;
-  f32x4 s = p[0];
-  for (int z = 1; z < splits; ++z) s += p[(size_t)z * step];
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  int z = 0;
+  for (; z + 4 <= splits; z += 4) {
+    f32x4 v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = p[(size_t)(z + u) * step];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) s += v[u];
+  }
+  for (; z < splits; ++z) s += p[(size_t)z * step];
   (w ? reinterpret_cast<f32x4*>(dw)[i] : reinterpret_cast<f32x4*>(db)[i - n4]) = s;
 }
 
-enum Shape { k64x64, k128x128, k128x256 };
+// Tile of dw and runs over tokens.  us on bf16 for M x N x K (tokens, rows and columns of dw), /runs:
+//   64 x 64 on four waves, runs up to a round of workgroups and of at least 256 tokens:  512 x 1024 x 1024 /1 8.5 (128 x
+//     128 10.6, /2 13.9), 2048 x 512 x 2048 /1 19.7 (/2 21.4; 128 x 128 /4 23.9), 1024 x 256 x 256 /4 8.7 (/1 10.9),
+//     16200 x 256 x 256 /16 16.8 (/8 21.3, /32 18.1; 128 x 128 20.2)
+//   128 x 128 on eight waves, where they fill half a round by themselves or many tokens fill it in runs:
+//     1024 x 1024 x 4096 /1 19.3 (64 x 64 26), 4050 x 1024 x 1024 /4 25.3 (64 x 64 /2 27.4), 16200 x 256 x 1024 /16
+//     23.8 (64 x 64 /8 27.2);  four waves of 64 x 64 each are behind: 22.7, 26.7, -
+//   256 x 128, over many tokens:  16200 x 1024 x 4096 /2 157 (128 x 128 /1 182), 16200 x 1024 x 1024 /8 51 (/4 56),
+//     8192 x 1024 x 1024 /8 35 (34);  128 x 256 has twice the codes to decode per thread: 161, 54
+// The scratch for more tokens is never less: every step above raises the planes' number.
+enum Shape { k64x64, k128x128, k256x128 };
 struct Plan {
   int shape, splits, per_split, tiles_n, tiles_k;
 };
 Plan plan(int dtype, int M, int N, int K) {
-  auto tiles = [&](int bn, int bk) { return (long)((N + bn - 1) / bn) * ((K + bk - 1) / bk); };
+  auto tiles = [&](int bn, int bk) { return ((N + bn - 1) / bn) * (long)((K + bk - 1) / bk); };
+  const long t128 = tiles(128, 128);
   Plan p;
-  p.shape = tiles(128, 128) >= 128 ? k128x128 : k64x64;
-  const int bn = p.shape == k64x64 ? 64 : 128, bk = p.shape == k64x64 ? 64 : p.shape == k128x128 ? 128 : 256;
+  if (dtype == kBF16 && M >= 8192 && tiles(256, 128) >= 32) p.shape = k256x128;
+  else if (t128 >= 128 || (t128 >= 32 && M >= 4096) || (t128 >= 16 && M >= 8192)) p.shape = k128x128;
+  else p.shape = k64x64;
+  const int bn = p.shape == k64x64 ? 64 : p.shape == k128x128 ? 128 : 256, bk = p.shape == k64x64 ? 64 : 128;
   p.tiles_n = (N + bn - 1) / bn;
   p.tiles_k = (K + bk - 1) / bk;
   const long t = (long)p.tiles_n * p.tiles_k;
-  p.splits = (int)std::max(1l, std::min({512 / t, 8l, (long)M / 256}));
+  p.splits = (int)std::max(1l, std::min({256 / t, (long)M / 256, 32l}));
   p.per_split = ((M + p.splits - 1) / p.splits + TM - 1) / TM * TM;
-  (void)dtype;
   return p;
 }
 
@@ -262,18 +324,19 @@ hipError_t run(const Wgrad8& a, const Plan& p, hipStream_t st) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || n == 1) return e;
   const size_t n4 = (size_t)a.N * a.K / 4, b4 = a.db ? (size_t)a.N / 4 : 0;
-  SR_LAUNCH(wgrad8_sum_kernel, dim3((unsigned)((n4 + b4 + 255) / 256)), dim3(256), 0, st, a.scratch, n, n4, b4, a.dw,
+  SR_LAUNCH(wgrad8_sum_kernel, dim3((unsigned)((n4 + b4 + 63) / 64)), dim3(64), 0, st, a.scratch, n, n4, b4, a.dw,
             a.db);
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t dispatch(const Wgrad8& a, const Plan& p, hipStream_t st) {
-  constexpr bool F = sizeof(T) == 4;
+  constexpr bool F = sizeof(T) == 4;   // three parts of dy fill the LDS of a workgroup per CU
   switch (p.shape) {
     case k64x64: return run<T, 64, 64, 2, 2, 2>(a, p, st);
-    case k128x128: return run<T, 128, 128, 2, 2, F ? 1 : 2>(a, p, st);
-    case k128x256: return run<T, 128, 256, 2, 4, 1>(a, p, st);
+    case k128x128: return run<T, 128, 128, 2, 4, F ? 1 : 2>(a, p, st);
+    case k256x128:
+      if constexpr (!F) return run<T, 256, 128, 4, 2, 1>(a, p, st);
   }
   return hipErrorInvalidValue;
 }

@@ -62,7 +62,12 @@ def test_weight_grad_matches_oracle(M, N, K, dtype):
 
 
 @pytest.mark.parametrize("dtype,M,N,K", [("bf16", 4050, 1024, 1024), ("bf16", 16200, 1024, 1024),
-                                         ("bf16", 8195, 4096, 1024), ("f32", 8195, 1024, 512)])
+                                         ("bf16", 8195, 4096, 1024), ("f32", 8195, 1024, 512),
+                                         # each tile shape with ragged rows, columns and tokens, with and without runs
+                                         ("bf16", 4101, 1032, 832), ("f32", 4101, 1032, 832), ("bf16", 67, 2056, 1088),
+                                         ("f32", 67, 2056, 1088), ("bf16", 8201, 1288, 832), ("bf16", 16333, 72, 192),
+                                         ("f32", 16333, 72, 192), ("bf16", 8200, 520, 960), ("f32", 9000, 264, 1088),
+                                         ("bf16", 8192, 4104, 2112)])
 def test_weight_grad_over_many_tokens(dtype, M, N, K):
     import torch
     gen = torch.Generator(device="cuda").manual_seed(M)
