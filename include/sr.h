@@ -92,6 +92,17 @@ typedef enum { SR_F32 = 0, SR_BF16 = 1 } sr_dtype;
  *   paper's EDM block, Sec. 2 "Generative forecasting"). */
 typedef enum { SR_BLOCK_PRELN = 0, SR_BLOCK_ADALN = 1 } sr_block_kind;
 
+/* Added to sr_config.kind (SR_BLOCK_PRELN | SR_BLOCK_SAVE8): the block calls keep a forward's activations for
+ * its backward in 8 bits (SR_Q8_BLOCK, below), 10.3 instead of 24.6 KB per token and block at D = 1024 in
+ * bf16, plus one block's worth of working buffers (34 KB per token, against 10).  The forward's output is bit
+ * for bit that without the flag; the gradients are those of the kept values (block inputs, q, k, v, attention
+ * output, residual and MLP pre-activation, each within half a step, 1/127 of the largest of its
+ * 32 neighbours), with the forward's LayerNorm statistics and row log-sum-exps.  sr_workspace_bytes, the
+ * sparse, dense and routed block calls take it, forward and backward alike (the same flag in both); a backward
+ * also writes the working part of `saved`, so calls on one `saved` must not overlap.  sr_attention_colsums
+ * returns SR_EUNSUPPORTED, and calls that do not read `kind` ignore it. */
+enum { SR_BLOCK_SAVE8 = 16 };
+
 /* Selectors.
  * SR_SEL_RANDOM: per sample, the K tokens with the smallest SplitMix64 keys
  *   key_i = mix(s_b + (i+1)*gamma), s_b = mix(s_step + (b+1)*gamma),
@@ -109,7 +120,7 @@ typedef enum { SR_SEL_RANDOM = 0, SR_SEL_TOPK_DIFFNORM = 1 } sr_select_kind;
 typedef struct {
   int32_t B, L, D, H, F, n_blocks;
   int32_t dtype;       /* sr_dtype */
-  int32_t kind;        /* sr_block_kind */
+  int32_t kind;        /* sr_block_kind, with SR_BLOCK_SAVE8 or without */
   float ln_eps;        /* LayerNorm epsilon (the paper leaves it unstated; 1e-6 here) */
   int32_t idx_shared;  /* 1: idx is [1,K], one index set for every sample (the
                           App. A.4 listing); 0: idx is [B,K], one set per sample */

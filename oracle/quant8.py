@@ -9,6 +9,8 @@ from __future__ import annotations
 import numpy as np
 from scipy.special import erfc
 
+from . import block as blk
+
 BLOCK = 32
 
 
@@ -63,3 +65,80 @@ def weight_grad(dy, q, eb):
     """dw (N, K), db (N,) fp64 from dy (M, N) and the block-format checkpoint of the layer's input."""
     dy = np.asarray(dy, np.float64)
     return dy.T @ blocks_value(q, eb), dy.sum(axis=0)
+
+
+def kept(t):
+    """The values that an activation (..., channels) has after being kept in the block format."""
+    t2 = t.reshape(-1, t.shape[-1])
+    return blocks_value(*quant_blocks(t2)).reshape(t.shape)
+
+
+def _kept_attention_bwd(q, k, v, O, lse, dO):
+    """dq, dk, dv (B, H, S, hd) with the probabilities exp(s - lse) of the kept q and k and the
+    forward's row log-sum-exps, and delta = rowsum(dO * O) of the kept O."""
+    scale = 1.0 / np.sqrt(q.shape[-1])
+    P = np.exp(q @ k.swapaxes(-1, -2) * scale - lse[..., None])
+    dS = P * (dO @ v.swapaxes(-1, -2) - (dO * O).sum(-1, keepdims=True))
+    return dS @ k * scale, dS.swapaxes(-1, -2) @ q * scale, P.swapaxes(-1, -2) @ dO
+
+
+def _shift(cache, n):
+    """The adaLN shift (B, 1, D) of LayerNorm n, from its output u = n (1 + scale) + shift."""
+    u, x = cache["u" if n == "1" else "u2"], cache["n" + n]
+    return (u - x * (1.0 + cache["sc" + n])).mean(axis=1, keepdims=True)
+
+
+def block_bwd_kept(dh_out, p, cache):
+    """oracle.block.block_bwd from a cache whose block input, q, k, v, attention output, residual,
+    MLP pre-activation (and adaLN branch outputs) were kept in the block format; LayerNorm
+    statistics and row log-sum-exps are the forward's."""
+    H, ada = cache["H"], cache["kind"] == "adaln"
+    B, S, D = cache["h"].shape
+    stats = {}
+    for n, x in (("1", cache["h"]), ("2", cache["h1"])):
+        mu = x.mean(axis=-1, keepdims=True)
+        rstd = cache["c_ln" + n][1]
+        xhat = (kept(x) - mu) * rstd
+        u = xhat * (1.0 + cache["sc" + n]) + _shift(cache, n) if ada else xhat * p[f"ln{n}_w"] + p[f"ln{n}_b"]
+        stats[n] = (xhat, rstd, u)
+    qkv = kept(np.concatenate([blk.merge_heads(cache[n]) for n in "qkv"], axis=-1))
+    q, k, v = (blk.split_heads(qkv[..., i * D:(i + 1) * D], H) for i in range(3))
+    s = cache["q"] @ cache["k"].swapaxes(-1, -2) / np.sqrt(D // H)
+    lse = np.log(np.exp(s - s.max(-1, keepdims=True)).sum(-1)) + s.max(-1)
+    O, z = kept(cache["O"]), kept(cache["z"])
+    flat = lambda t: t.reshape(-1, t.shape[-1])  # noqa: E731
+    g = {n: np.zeros_like(t) for n, t in p.items()}
+    dm, dgate2 = (dh_out * cache["g2"], (dh_out * kept(cache["m_out"])).sum(1)) if ada else (dh_out, None)
+    g["w_fc2"], g["b_fc2"] = flat(dm).T @ flat(blk.gelu(z)), flat(dm).sum(0)
+    dz = (dm @ p["w_fc2"]) * blk.gelu_grad(z)
+    g["w_fc1"], g["b_fc1"] = flat(dz).T @ flat(stats["2"][2]), flat(dz).sum(0)
+    du2 = dz @ p["w_fc1"]
+    if ada:
+        dscale2, dshift2 = (du2 * stats["2"][0]).sum(1), du2.sum(1)
+        dx = blk.ln_bwd(du2 * (1.0 + cache["sc2"]), stats["2"][:2], None)[0]
+    else:
+        dx, g["ln2_w"], g["ln2_b"] = blk.ln_bwd(du2, stats["2"][:2], p["ln2_w"])
+    dh1 = dh_out + dx
+    da, dgate1 = (dh1 * cache["g1"], (dh1 * kept(cache["a_out"])).sum(1)) if ada else (dh1, None)
+    g["w_o"], g["b_o"] = flat(da).T @ flat(O), flat(da).sum(0)
+    d3 = _kept_attention_bwd(q, k, v, blk.split_heads(O, H), lse, blk.split_heads(da @ p["w_o"], H))
+    dqkv = np.concatenate([blk.merge_heads(t) for t in d3], axis=-1)
+    g["w_qkv"], g["b_qkv"] = flat(dqkv).T @ flat(stats["1"][2]), flat(dqkv).sum(0)
+    du = dqkv @ p["w_qkv"]
+    dcond = None
+    if ada:
+        dmod = np.concatenate([du.sum(1), (du * stats["1"][0]).sum(1), dgate1, dshift2, dscale2, dgate2], axis=-1)
+        dx = blk.ln_bwd(du * (1.0 + cache["sc1"]), stats["1"][:2], None)[0]
+        g["w_ada"], g["b_ada"], dcond = dmod.T @ cache["cond"], dmod.sum(0), dmod @ p["w_ada"]
+    else:
+        dx, g["ln1_w"], g["ln1_b"] = blk.ln_bwd(du, stats["1"][:2], p["ln1_w"])
+    return dh1 + dx, g, dcond
+
+
+def stack_bwd_kept(dh, params64, caches):
+    """oracle.stack.stack_bwd with block_bwd_kept."""
+    grads, dcond = [None] * len(params64), None
+    for i in reversed(range(len(params64))):
+        dh, grads[i], dc = block_bwd_kept(dh, params64[i], caches[i])
+        dcond = dc if dcond is None or dc is None else dcond + dc
+    return dh, grads, dcond

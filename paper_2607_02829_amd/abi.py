@@ -16,6 +16,7 @@ LIB_PATH = os.path.join(HERE, "libsr.so")
 SR_OK, SR_EINVAL, SR_ESHAPE, SR_EDTYPE, SR_EALIGN, SR_EWORKSPACE, SR_EUNSUPPORTED, SR_EHIP = range(8)
 SR_F32, SR_BF16 = 0, 1
 SR_BLOCK_PRELN, SR_BLOCK_ADALN = 0, 1
+SR_BLOCK_SAVE8 = 16
 SR_SEL_RANDOM, SR_SEL_TOPK_DIFFNORM = 0, 1
 SR_Q8_ROW, SR_Q8_BLOCK = 0, 1
 SR_ACT_NONE, SR_ACT_GELU = 0, 1

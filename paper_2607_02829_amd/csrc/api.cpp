@@ -49,6 +49,9 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
     SR_CHECK(aligned16(p), SR_EALIGN, "%s is not 16-byte aligned", name); \
   } while (0)
 
+// cfg->kind without the flag for 8-bit saved activations
+int block_kind(const sr_config* c) { return c->kind & ~SR_BLOCK_SAVE8; }
+
 size_t elt_of(int dtype) { return dtype == SR_BF16 ? 2 : 4; }
 
 // Routing-only calls (selection, gather, scatter, index validation) touch [B, L, D] tensors, whose
@@ -58,7 +61,7 @@ size_t elt_of(int dtype) { return dtype == SR_BF16 ? 2 : 4; }
 sr_status check_cfg(const sr_config* c, bool routing_only = false, int64_t rows = 0) {
   SR_CHECK(c != nullptr, SR_EINVAL, "cfg is NULL");
   SR_CHECK(c->dtype == SR_F32 || c->dtype == SR_BF16, SR_EDTYPE, "unknown dtype %d", c->dtype);
-  SR_CHECK(c->kind == SR_BLOCK_PRELN || c->kind == SR_BLOCK_ADALN, SR_EINVAL, "unknown block kind %d", c->kind);
+  SR_CHECK(block_kind(c) == SR_BLOCK_PRELN || block_kind(c) == SR_BLOCK_ADALN, SR_EINVAL, "unknown block kind %d", c->kind);
   SR_CHECK(c->B >= 1 && c->L >= 1 && c->D >= 1 && c->H >= 1 && c->F >= 1 && c->n_blocks >= 0, SR_EINVAL,
            "sizes must be positive (B=%d L=%d D=%d H=%d F=%d n_blocks=%d)", c->B, c->L, c->D, c->H, c->F,
            c->n_blocks);
@@ -107,7 +110,8 @@ sr::Dims dims_of(const sr_config* c, int S) {
   d.B = c->B; d.L = c->L; d.D = c->D; d.H = c->H; d.F = c->F; d.nb = c->n_blocks;
   d.S = S; d.M = c->B * S;
   d.dtype = c->dtype == SR_BF16 ? sr::kBF16 : sr::kF32;
-  d.kind = c->kind;
+  d.kind = block_kind(c);
+  d.save8 = (c->kind & SR_BLOCK_SAVE8) != 0;
   d.eps = c->ln_eps;
   d.elt = elt_of(c->dtype);
   return d;
@@ -123,7 +127,7 @@ sr_status check_params(const sr_config* c, const sr_block_params* p, const void*
       SR_CHECK(aligned16(q), SR_EALIGN, "block %d: a weight or bias pointer is not 16-byte aligned", i);
     }
     // the row kernels read gamma / beta and the modulation weights with 8- and 16-byte loads
-    if (c->kind == SR_BLOCK_PRELN) {
+    if (block_kind(c) == SR_BLOCK_PRELN) {
       const void* ln[] = {w.ln1_w, w.ln1_b, w.ln2_w, w.ln2_b};
       for (const void* q : ln) {
         SR_CHECK(q != nullptr, SR_EINVAL, "block %d: a LayerNorm parameter is NULL", i);
@@ -135,7 +139,7 @@ sr_status check_params(const sr_config* c, const sr_block_params* p, const void*
                "block %d: w_ada or b_ada is not 16-byte aligned", i);
     }
   }
-  if (c->kind == SR_BLOCK_ADALN) SR_PTR(cond, "cond");
+  if (block_kind(c) == SR_BLOCK_ADALN) SR_PTR(cond, "cond");
   return SR_OK;
 }
 
@@ -299,7 +303,7 @@ sr_status sr_sparse_blocks_bwd(const sr_config* cfg, int32_t S, const sr_block_p
   if ((s = check_ws(cfg, S, saved, saved_bytes, scratch, scratch_bytes, true)) != SR_OK) return s;
   sr::Dims d = dims_of(cfg, S);
   return hip_status(sr::stack_bwd(d, params, cond, (const char*)saved, dh_out, dh_in, grads,
-                                  cfg->kind == SR_BLOCK_ADALN ? dcond : nullptr, (char*)scratch, scratch_bytes,
+                                  block_kind(cfg) == SR_BLOCK_ADALN ? dcond : nullptr, (char*)scratch, scratch_bytes,
                                   (hipStream_t)stream),
                     "blocks_bwd");
 }
@@ -341,7 +345,7 @@ sr_status sr_routed_blocks_bwd(const sr_config* cfg, int32_t K, const int32_t* i
   sr::Route rt;
   rt.idx = idx; rt.x = g; rt.shared = cfg->idx_shared;
   return hip_status(sr::stack_bwd(d, params, cond, (const char*)saved, nullptr, nullptr, grads,
-                                  cfg->kind == SR_BLOCK_ADALN ? dcond : nullptr, (char*)scratch, scratch_bytes,
+                                  block_kind(cfg) == SR_BLOCK_ADALN ? dcond : nullptr, (char*)scratch, scratch_bytes,
                                   (hipStream_t)stream, &rt),
                     "routed_blocks_bwd");
 }
@@ -370,6 +374,8 @@ sr_status sr_attention_colsums(const sr_config* cfg, int32_t S, const void* save
   sr_status s = check_cfg(cfg, false, S);
   if (s != SR_OK) return s;
   SR_CHECK(S >= 1 && S <= cfg->L, SR_ESHAPE, "S=%d outside [1, L=%d]", S, cfg->L);
+  SR_CHECK(!(cfg->kind & SR_BLOCK_SAVE8), SR_EUNSUPPORTED,
+           "column sums need the forward's q and k, which SR_BLOCK_SAVE8 does not keep");
   SR_CHECK(block >= 0 && block < cfg->n_blocks, SR_EINVAL, "block %d outside [0, n_blocks=%d)", block,
            cfg->n_blocks);
   if ((s = check_ws(cfg, S, saved, saved_bytes, nullptr, 0, false)) != SR_OK) return s;

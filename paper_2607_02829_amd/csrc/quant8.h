@@ -26,6 +26,17 @@ hipError_t launch_quantize8(int kind, int dtype, int M, int N, const void* x, in
 hipError_t launch_dequantize8(int kind, int dtype, int M, int N, const int8_t* q, const void* scale, void* x,
                               hipStream_t st);
 
+// SR_Q8_BLOCK of up to kMaxQ8Jobs tensors in one launch, with the values of single calls.
+struct Q8Job {
+  void* x = nullptr;   // n elements of the type, a multiple of 64
+  int dtype = 0;
+  size_t n = 0;
+  int8_t* q = nullptr;
+  uint8_t* e = nullptr;
+};
+constexpr int kMaxQ8Jobs = 6;
+hipError_t launch_q8_jobs(const Q8Job* jobs, int njobs, bool quantize, hipStream_t st);
+
 // y = act(xs_m ws_n sum_k xq_mk wq_nk + bias_n)
 struct Linear8 {
   int M = 0, N = 0, K = 0;

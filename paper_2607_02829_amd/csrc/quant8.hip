@@ -195,10 +195,7 @@ __global__ __launch_bounds__(256) void dequant_rows_kernel(const int8_t* __restr
 
 // Eight elements per lane, four lanes per block of 32 channels.
 template <typename T>
-__global__ __launch_bounds__(256) void quant_blocks_kernel(const T* __restrict__ x, size_t n8, int8_t* __restrict__ q,
-                                                           uint8_t* __restrict__ e) {
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= n8) return;   // n8 is a multiple of 8: the four lanes of a block leave together
+SR_DEV void quant_block8(const T* __restrict__ x, size_t i, int8_t* __restrict__ q, uint8_t* __restrict__ e) {
   float v[8];
   load8(x + i * 8, v);
   uint32_t m = 0;
@@ -219,16 +216,43 @@ __global__ __launch_bounds__(256) void quant_blocks_kernel(const T* __restrict__
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void dequant_blocks_kernel(const int8_t* __restrict__ q, const uint8_t* __restrict__ e,
-                                                             size_t n8, T* __restrict__ x) {
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= n8) return;
+SR_DEV void dequant_block8(const int8_t* __restrict__ q, const uint8_t* __restrict__ e, size_t i, T* __restrict__ x) {
   const i32x2 w = reinterpret_cast<const i32x2*>(q)[i];
   const float s = block_scale(e[i >> 2]);
   float v[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) v[j] = (float)(int8_t)((uint32_t)w[j >> 2] >> (8 * (j & 3))) * s;
   store8(x + i * 8, v);
+}
+
+template <typename T, bool QUANT>
+__global__ __launch_bounds__(256) void blocks8_kernel(T* __restrict__ x, size_t n8, int8_t* __restrict__ q,
+                                                      uint8_t* __restrict__ e) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n8) return;   // n8 is a multiple of 8: the four lanes of a block leave together
+  if constexpr (QUANT) quant_block8<T>(x, i, q, e);
+  else dequant_block8<T>(q, e, i, x);
+}
+
+// Job j takes the workgroups [first[j], first[j + 1]).
+struct Q8Jobs {
+  Q8Job job[kMaxQ8Jobs];
+  int first[kMaxQ8Jobs + 1];
+};
+template <bool QUANT>
+__global__ __launch_bounds__(256) void q8_jobs_kernel(Q8Jobs js) {
+  int j = 0;
+  while (j + 1 < kMaxQ8Jobs && (int)blockIdx.x >= js.first[j + 1]) ++j;
+  const Q8Job& b = js.job[j];
+  const size_t i = (size_t)((int)blockIdx.x - js.first[j]) * 256 + threadIdx.x;
+  if (i >= b.n / 8) return;
+  if (b.dtype == kBF16) {
+    if constexpr (QUANT) quant_block8<bf16_t>((const bf16_t*)b.x, i, b.q, b.e);
+    else dequant_block8<bf16_t>(b.q, b.e, i, (bf16_t*)b.x);
+  } else {
+    if constexpr (QUANT) quant_block8<float>((const float*)b.x, i, b.q, b.e);
+    else dequant_block8<float>(b.q, b.e, i, (float*)b.x);
+  }
 }
 
 template <typename T>
@@ -248,8 +272,8 @@ hipError_t quant(int kind, int M, int N, const void* x, int8_t* q, void* scale, 
     else rows(IC<256>{}, IC<0>{});
   } else {
     const size_t n8 = (size_t)M * N / 8;
-    SR_LAUNCH(quant_blocks_kernel<T>, dim3((unsigned)((n8 + 255) / 256)), dim3(256), 0, st, (const T*)x, n8, q,
-              (uint8_t*)scale);
+    SR_LAUNCH((blocks8_kernel<T, true>), dim3((unsigned)((n8 + 255) / 256)), dim3(256), 0, st, (T*)const_cast<void*>(x),
+              n8, q, (uint8_t*)scale);
   }
   return hipGetLastError();
 }
@@ -261,11 +285,28 @@ hipError_t dequant(int kind, int M, int N, const int8_t* q, const void* scale, v
   if (kind == SR_Q8_ROW)
     SR_LAUNCH(dequant_rows_kernel<T>, grid, dim3(256), 0, st, q, (const float*)scale, n8, N / 8, (T*)x);
   else
-    SR_LAUNCH(dequant_blocks_kernel<T>, grid, dim3(256), 0, st, q, (const uint8_t*)scale, n8, (T*)x);
+    SR_LAUNCH((blocks8_kernel<T, false>), grid, dim3(256), 0, st, (T*)x, n8, const_cast<int8_t*>(q),
+              (uint8_t*)const_cast<void*>(scale));
   return hipGetLastError();
 }
 
 }  // namespace
+
+hipError_t launch_q8_jobs(const Q8Job* jobs, int njobs, bool quantize, hipStream_t st) {
+  if (njobs > kMaxQ8Jobs) return hipErrorInvalidValue;
+  Q8Jobs js{};
+  int blocks = 0;
+  for (int j = 0; j < njobs; ++j) {
+    js.job[j] = jobs[j];
+    js.first[j] = blocks;
+    blocks += (int)((jobs[j].n / 8 + 255) / 256);
+  }
+  if (blocks == 0) return hipSuccess;
+  for (int j = njobs; j <= kMaxQ8Jobs; ++j) js.first[j] = blocks;
+  if (quantize) SR_LAUNCH(q8_jobs_kernel<true>, dim3((unsigned)blocks), dim3(256), 0, st, js);
+  else SR_LAUNCH(q8_jobs_kernel<false>, dim3((unsigned)blocks), dim3(256), 0, st, js);
+  return hipGetLastError();
+}
 
 hipError_t launch_quantize8(int kind, int dtype, int M, int N, const void* x, int8_t* q, void* scale, hipStream_t st) {
   return dtype == kBF16 ? quant<bf16_t>(kind, M, N, x, q, scale, st) : quant<float>(kind, M, N, x, q, scale, st);

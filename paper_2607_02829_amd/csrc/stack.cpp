@@ -26,6 +26,7 @@
 
 #include "common.h"
 #include "profile.h"
+#include "quant8.h"
 
 namespace sr {
 
@@ -76,6 +77,55 @@ GemmDesc desc(const Dims& d, const void* A, bool ak, long long lda, size_t abyte
 size_t layout_saved(const Dims& d, char* base, BlockSaved* out) {
   Carver c(base);
   const size_t M = d.M, D = d.D, F = d.F, e = d.elt;
+  if (d.save8) {
+    // the activations in 8 bits per block (10.3 of 24.6 KB per token at D = 1024), then one block's worth of them in
+    // their own types, which the forward writes and the backward restores
+    auto keep = [&](size_t n) {
+      Kept8 k;
+      k.q = c.take<int8_t>(n);
+      k.e = c.take<uint8_t>(n / kQBlock);
+      return k;
+    };
+    const bool ada = d.kind == SR_BLOCK_ADALN;
+    std::vector<BlockSaved> all((size_t)d.nb);
+    for (BlockSaved& s : all) {
+      s.k_hin = keep(M * D);
+      s.k_qkv = keep(M * 3 * D);
+      s.k_O = keep(M * D);
+      s.k_h1 = keep(M * D);
+      s.k_z = keep(M * F);
+      if (ada) {
+        s.k_a = keep(M * D);
+        s.k_m = keep(M * D);
+        s.mod = c.take<float>((size_t)d.B * 6 * D * 4);
+      }
+      s.mean1 = c.take<float>(M * 4);
+      s.rstd1 = c.take<float>(M * 4);
+      s.lse = c.take<float>((size_t)d.B * d.H * d.S * 4);
+      s.mean2 = c.take<float>(M * 4);
+      s.rstd2 = c.take<float>(M * 4);
+    }
+    BlockSaved w{};
+    w.hin = c.take<float>(M * D * 4);
+    w.qkv = c.take<void>(M * 3 * D * e);
+    w.O = c.take<void>(M * D * e);
+    w.h1 = c.take<float>(M * D * 4);
+    w.z = c.take<void>(M * F * e);
+    if (ada) {
+      w.a_out = c.take<void>(M * D * e);
+      w.m_out = c.take<void>(M * D * e);
+    }
+    w.u1 = w.u2 = c.take<void>(M * D * e);
+    w.gz = c.take<void>(M * F * e);
+    if (out)
+      for (int i = 0; i < d.nb; ++i) {
+        BlockSaved& s = all[(size_t)i];
+        s.hin = w.hin; s.qkv = w.qkv; s.O = w.O; s.h1 = w.h1; s.z = w.z;
+        s.a_out = w.a_out; s.m_out = w.m_out; s.u1 = w.u1; s.u2 = w.u2; s.gz = w.gz;
+        out[i] = s;
+      }
+    return c.off;
+  }
   for (int i = 0; i < d.nb; ++i) {
     BlockSaved s{};
     s.hin = c.take<float>(M * D * 4);
@@ -140,6 +190,7 @@ size_t layout_scratch(const Dims& d, char* base, Scratch* out, bool planes) {
   // recomputed operands of the weight-gradient GEMMs (written and read on the second stream)
   s.u_rc = c.take<void>(M * D * e);
   s.gz_rc = c.take<void>(M * F * e);
+  s.w8part = d.save8 ? c.take<float>(wgrad8_scratch(d.dtype, d.M, d.D, d.D)) : nullptr;
   s.attn_splits = planes ? attn_splits(d.dtype, d.B, d.S, d.H, d.D / d.H, kMaxSplit) : 1;
   if (s.attn_splits > 1)
     for (int k = 0; k < s.attn_splits; ++k) s.attn.p[k] = c.take<float>(M * 3 * D * 4);
@@ -167,6 +218,12 @@ size_t scratch_bytes(const Dims& d) {
 
 // Planes of a split attention forward, in buffers of the block that are written only after it: h1, z
 // and GELU(z), the maxima and denominators over u1 (read only before).  Returns the number of runs.
+static Q8Job q8_job(const void* x, int dtype, size_t n, const Kept8& k) {
+  Q8Job j;
+  j.x = const_cast<void*>(x); j.dtype = dtype; j.n = n; j.q = k.q; j.e = k.e;
+  return j;
+}
+
 static int fwd_attn_part(const Dims& d, const BlockSaved& s, AttnPart* part) {
   const size_t plane = (size_t)d.M * d.D, act = (size_t)d.M * d.F * d.elt / 4 / plane * plane;
   int n = 0;
@@ -241,6 +298,14 @@ hipError_t stack_fwd(const Dims& d, const sr_block_params* p, const void* cond, 
         ProfScope ps("gemm_fc1", gemm_flops(M, F, D), gemm_bytes(d, M, F, D, 2 * (int)e), st);
         SR_TRY(launch_gemm(g, EPI_GELU, ep, st));
       }
+      if (d.save8) {   // what the backward reads of this block, before FC2 puts the next one's input over its own
+        const size_t MD = (size_t)M * D;
+        const Q8Job jobs[] = {q8_job(s.hin, kF32, MD, s.k_hin), q8_job(s.qkv, d.dtype, 3 * MD, s.k_qkv),
+                              q8_job(s.O, d.dtype, MD, s.k_O),  q8_job(s.h1, kF32, MD, s.k_h1),
+                              q8_job(s.z, d.dtype, (size_t)M * F, s.k_z), q8_job(s.a_out, d.dtype, MD, s.k_a)};
+        ProfScope ps("quantize8", 0, (double)MD * (8 + 4 * e + 6) + (double)M * F * (e + 1), st);
+        SR_TRY(launch_q8_jobs(jobs, ada ? 6 : 5, true, st));
+      }
       {
         GemmDesc g = desc(d, s.gz, true, F, (size_t)M * F * e, w.w_fc2, true, F, (size_t)D * F * e, M, D, F);
         EpiArgs ep; ep.bias = w.b_fc2; ep.resid = s.h1; ep.ldo = D; ep.S = S;
@@ -254,6 +319,11 @@ hipError_t stack_fwd(const Dims& d, const sr_block_params* p, const void* cond, 
         if (ada) { ep.gate = s.mod + 5 * D; ep.gate_stride = 6 * D; ep.a_save = s.m_out; }
         ProfScope ps("gemm_fc2", gemm_flops(M, D, F), gemm_bytes(d, M, D, F, 8), st);
         SR_TRY(launch_gemm(g, EPI_RESID, ep, st));
+      }
+      if (d.save8 && ada) {
+        const Q8Job job = q8_job(s.m_out, d.dtype, (size_t)M * D, s.k_m);
+        ProfScope ps("quantize8", 0, (double)M * D * (e + 1), st);
+        SR_TRY(launch_q8_jobs(&job, 1, true, st));
       }
     }
     return hipSuccess;
@@ -420,7 +490,14 @@ hipError_t stack_bwd(const Dims& d, const sr_block_params* p, const void* cond, 
   // slots: g_act[0] (FC2 stage) and g_act[1] (output-projection stage) are read by dW_fc2 and
   // dW_o; dz[i % 2] by dW_fc1 and dqkv[i % 2] by dW_qkv of block i
   enum { kFc2 = 0, kO = 1, kFc1 = 2, kQkv = 4 };
-
+  // save8: an activation from its 8 bits back into the one buffer of its kind, before its first reader of the block
+  // and after the side-stream work of the block before it (slot) that read the same buffer
+  auto restore = [&](void* x, int dtype, size_t n, const Kept8& k) -> hipError_t {
+    if (!d.save8) return hipSuccess;
+    const Q8Job job = q8_job(x, dtype, n, k);
+    ProfScope ps("dequantize8", 0, (double)n * ((dtype == kF32 ? 4 : e) + 1), st);
+    return launch_q8_jobs(&job, 1, false, st);
+  };
 
   // pre-LN: the LayerNorm parameter gradients (column sums of the ln_bwd partials) are outputs
   // only, so their reductions join the block's weight-gradient reductions in the one launch on
@@ -458,7 +535,10 @@ hipError_t stack_bwd(const Dims& d, const sr_block_params* p, const void* cond, 
       void* const dz = sc.dz[par];
       void* const dqkv = sc.dqkv[par];
       ReduceJob jobs[6];   // this block's reductions (weights, LN2, the previous LN1), after dW_qkv
+      if (d.save8) SR_TRY(join(kFc2));   // the previous block's GELU(z)
+      SR_TRY(restore(s.z, d.dtype, (size_t)M * F, s.k_z));
       if (ada) {
+        SR_TRY(restore(s.m_out, d.dtype, (size_t)M * D, s.k_m));
         // MLP-branch gradient dm = dh' * gate2 (activation copy) and dgate2 = sum_s dh' * m_out
         SR_TRY(join(kFc2));   // g0 may still be read by the previous block's dW_fc2
         SR_TRY(gate_bwd(d, sc.g_res, s.m_out, s.mod + 5 * D, g0, sc.dmod, 5 * D, sc, st));
@@ -480,6 +560,8 @@ hipError_t stack_bwd(const Dims& d, const sr_block_params* p, const void* cond, 
           return launch_gemm(gd, EPI_DGELU, ep, st);
         }));
       }
+      if (d.save8) SR_TRY(join(kFc1 + 1 - par));   // the previous block's LN2 output
+      SR_TRY(restore(s.h1, kF32, (size_t)M * D, s.k_h1));
       // FC1: dW1, db1; du = dz W1
       SR_TRY(on_side(kFc1 + par, [&](hipStream_t ss) -> hipError_t {
         if (g.w_fc1 || g.b_fc1) {   // u2 = LN2(h1) recomputed from the saved statistics
@@ -508,6 +590,7 @@ hipError_t stack_bwd(const Dims& d, const sr_block_params* p, const void* cond, 
                                   st));
       }
       if (ada) {
+        SR_TRY(restore(s.a_out, d.dtype, (size_t)M * D, s.k_a));
         // attention-branch gradient da = dh1 * gate1 and dgate1 = sum_s dh1 * a_out
         SR_TRY(join(kO));   // g1 may still be read by the previous block's dW_o
         SR_TRY(gate_bwd(d, sc.g_res2, s.a_out, s.mod + 2 * D, g1, sc.dmod, 2 * D, sc, st));
@@ -515,8 +598,19 @@ hipError_t stack_bwd(const Dims& d, const sr_block_params* p, const void* cond, 
       // output projection: dWo, dbo; dO = da Wo (with the attention row statistic
       // delta = rowsum(dO * O) per head in the same epilogue when the head dim is 64)
       SR_TRY(on_side(kO, [&](hipStream_t ss) -> hipError_t {
+        if (d.save8) {   // from the kept codes themselves
+          if (!g.w_o && !g.b_o) return hipSuccess;
+          Wgrad8 a;
+          a.M = M; a.N = D; a.K = D;
+          a.dy = g1; a.xq = s.k_O.q; a.xe = s.k_O.e;
+          a.dw = g.w_o ? g.w_o : sc.wpart[kWgO]; a.db = g.b_o; a.scratch = sc.w8part;
+          ProfScope ps("gemm_dw_o", gemm_flops(D, D, M), gemm_bytes(d, D, D, M, 4), ss);
+          return launch_wgrad8(d.dtype, a, ss);
+        }
         return weight_grad("gemm_dw_o", d, g1, D, s.O, D, g.w_o, g.b_o, sc, kWgO, &jobs[kWgO], ss);
       }));
+      SR_TRY(restore(s.O, d.dtype, (size_t)M * D, s.k_O));
+      SR_TRY(restore(s.qkv, d.dtype, (size_t)M * 3 * D, s.k_qkv));
       const bool fuse_delta = d.dtype == kBF16 && D / d.H == 64;
       {
         GemmDesc gd = desc(d, g1, true, D, (size_t)M * D * e, w.w_o, false, D, (size_t)D * D * e, M, D, D);
@@ -534,6 +628,8 @@ hipError_t stack_bwd(const Dims& d, const sr_block_params* p, const void* cond, 
       SR_TRY(fork_point([&]() -> hipError_t {
         return launch_attn_bwd(d.dtype, s.qkv, sc.dO, s.lse, sc.delta, dqkv, d.B, S, d.H, D, st, sc.attn_splits, sc.attn);
       }));
+      if (d.save8) SR_TRY(join(kQkv + 1 - par));   // the previous block's LN1 output
+      SR_TRY(restore(s.hin, kF32, (size_t)M * D, s.k_hin));
       if (!ada) {   // LN2 of this block and LN1 of the block before it join the reduction launch
         if (g.ln2_w || g.ln2_b) jobs[4] = ln_job(sc.lnpart[0][par], g.ln2_w, g.ln2_b);
         if (ln1_pending && (ln1_pending->ln1_w || ln1_pending->ln1_b))

@@ -13,11 +13,19 @@ struct Dims {
   int dtype, kind;
   float eps;
   size_t elt;   // bytes per storage / activation element
+  bool save8 = false;   // SR_BLOCK_SAVE8
+};
+
+// An activation kept in 8 bits (SR_Q8_BLOCK).
+struct Kept8 {
+  int8_t* q = nullptr;
+  uint8_t* e = nullptr;
 };
 
 struct BlockSaved {
   float *hin, *mean1, *rstd1, *lse, *h1, *mean2, *rstd2, *mod;
   void *u1, *qkv, *O, *u2, *z, *gz, *a_out, *m_out;
+  Kept8 k_hin, k_qkv, k_O, k_h1, k_z, k_a, k_m;   // save8: what is kept; the buffers above are then one block's
 };
 
 struct Scratch {
@@ -29,6 +37,7 @@ struct Scratch {
   AttnPart attn;   // planes of a split attention backward
   int attn_splits;
   void *g_act[2], *dz[2], *dO, *dqkv[2], *u_rc, *gz_rc;
+  float* w8part;   // save8: partial planes of the output projection's weight gradient
 };
 
 // Routing fused into the stack's boundaries: the input rows are gathered from x by idx

@@ -24,6 +24,10 @@ forward from that stage's input (x0, the gathered tokens h0, the scattered x1, a
 right before the stage's backward.  The kernels are deterministic, so the recomputed
 activations, and with them every gradient, are bit for bit those of the run without
 checkpointing; the price is one more forward of every block.
+
+Saved activations in 8 bits (optional): the stages keep what their backward reads as 8-bit codes
+with a power of two per 32 channels, less than half the bytes per block, and run no second forward;
+outputs are those without it, gradients those of the kept values.
 """
 from __future__ import annotations
 
@@ -51,11 +55,12 @@ class Trunk:
     stage's input."""
 
     def __init__(self, w, split, params_storage, K: int | None = None, seed: int = 42, select: str = "random",
-                 checkpoint: bool = False):
+                 checkpoint: bool = False, save8: bool = False):
         """``select``: "random" (the method's selector) or "attn" (top-K by the attention each
         token receives in the last dense-early block, summed over heads: the paper's
         attention-score ablation).  ``checkpoint``: keep one stage's saved activations at a
-        time and recompute them in the backward."""
+        time and recompute them in the backward.  ``save8``: keep the saved activations in 8 bits
+        (SR_BLOCK_SAVE8); not with the "attn" selector, which reads the early stage's q and k."""
         import torch
         n1, n2, n3 = split
         if min(n1, n2, n3) < 1:
@@ -68,12 +73,19 @@ class Trunk:
             raise ValueError(f"unknown selector {select!r}")
         if not isinstance(checkpoint, bool):
             raise ValueError(f"checkpoint must be True or False, not {checkpoint!r}")
+        if not isinstance(save8, bool):
+            raise ValueError(f"save8 must be True or False, not {save8!r}")
+        if save8 and select == "attn":
+            raise ValueError("save8 keeps no q and k for the attention-score selector")
         self.w, self.split, self.seed, self.select = w, tuple(split), seed, select
         self.checkpoint = checkpoint
         self.K = w.K if K is None else K
         if not 1 <= self.K <= w.L:
             raise ValueError(f"K={self.K} outside [1, L={w.L}]")
         self.cfg = [device.config_for(w, n_blocks=n) for n in split]
+        if save8:
+            for c in self.cfg:
+                c.kind |= abi.SR_BLOCK_SAVE8
         bounds = (0, n1, n1 + n2, n1 + n2 + n3)
         self.params = [device.DeviceParams(params_storage[bounds[i]:bounds[i + 1]], w.kind) for i in range(3)]
         self.grads = [device.DeviceGrads(w, n, skip_unused=True) for n in split]

@@ -61,3 +61,25 @@ def test_weight_gradient_equals_differences():
     num = (loss(W + h * V, b + h * u) - loss(W - h * V, b - h * u)) / (2 * h)
     ana = float((dw * V).sum() + (db * u).sum())
     assert abs(num - ana) <= 1e-7 * max(1.0, abs(ana))
+
+
+@pytest.mark.parametrize("kind", ["preln", "adaln"])
+def test_kept_backward_without_rounding_is_the_backward(kind, monkeypatch):
+    # with a format that rounds nothing the kept backward is the block's own
+    from oracle import block as oblk
+    rng = np.random.default_rng(9)
+    B, S, D, H, F = 2, 5, 64, 2, 128
+    shapes = {"ln1_w": (D,), "ln1_b": (D,), "w_qkv": (3 * D, D), "b_qkv": (3 * D,), "w_o": (D, D), "b_o": (D,),
+              "ln2_w": (D,), "ln2_b": (D,), "w_fc1": (F, D), "b_fc1": (F,), "w_fc2": (D, F), "b_fc2": (D,),
+              "w_ada": (6 * D, D), "b_ada": (6 * D,)}
+    p = {k: 0.2 * rng.standard_normal(s) + (1.0 if k in ("ln1_w", "ln2_w") else 0.0) for k, s in shapes.items()}
+    cond = rng.standard_normal((B, D)) if kind == "adaln" else None
+    h, dh = rng.standard_normal((B, S, D)), rng.standard_normal((B, S, D))
+    _, cache = oblk.block_fwd(h, p, H, 1e-6, kind, cond)
+    monkeypatch.setattr(oq, "kept", lambda t: t)
+    got, want = oq.block_bwd_kept(dh, p, cache), oblk.block_bwd(dh, p, cache)
+    np.testing.assert_allclose(got[0], want[0], rtol=1e-9, atol=1e-11)
+    for k in p:
+        np.testing.assert_allclose(got[1][k], want[1][k], rtol=1e-9, atol=1e-10)
+    if kind == "adaln":
+        np.testing.assert_allclose(got[2], want[2], rtol=1e-9, atol=1e-11)

@@ -130,3 +130,53 @@ _Zstore:
 .Lfunc_end2:
 """
     assert kernel_hazards(asm) == {"_Zkept": 0, "_Zearly": 1, "_Zstore": 1}
+
+
+def _cfg(**kw):
+    base = dict(B=2, L=400, D=1024, H=16, F=4096, n_blocks=8, dtype=BF, kind=abi.SR_BLOCK_PRELN, ln_eps=1e-6, idx_shared=0)
+    base.update(kw)
+    return abi.SrConfig(**base)
+
+
+def test_save8_sizes():
+    _lib()
+    for kind in (abi.SR_BLOCK_PRELN, abi.SR_BLOCK_ADALN):
+        plain, save = _cfg(kind=kind), _cfg(kind=kind | abi.SR_BLOCK_SAVE8)
+        a, b = abi.sr_workspace_bytes(plain, 400)[0], abi.sr_workspace_bytes(save, 400)[0]
+        a1, b1 = (abi.sr_workspace_bytes(_cfg(kind=c.kind, n_blocks=9), 400)[0] for c in (plain, save))
+        # per token and block: 10 D channels of a byte and a 32nd (12 with adaLN), and statistics, against 24 D bytes
+        # and more in bf16
+        assert b < a and (b1 - b) < 0.46 * (a1 - a)
+        last = (0, 0)
+        for S in range(1, 400):
+            n = abi.sr_workspace_bytes(save, S)
+            assert n[0] >= last[0] and n[1] >= last[1]
+            last = n
+
+
+def test_save8_refusals():
+    L = _lib()
+    for kind in (abi.SR_BLOCK_SAVE8 | 2, 32, abi.SR_BLOCK_SAVE8 | 32, -1):
+        assert L.sr_workspace_bytes(ctypes.byref(_cfg(kind=kind)), 10, None, None) == abi.SR_EINVAL
+    c = _cfg(kind=abi.SR_BLOCK_SAVE8)
+    assert L.sr_attention_colsums(ctypes.byref(c), 25, FAKE, 1 << 40, 0, FAKE, None) == abi.SR_EUNSUPPORTED
+    ada = _cfg(kind=abi.SR_BLOCK_ADALN | abi.SR_BLOCK_SAVE8)
+    params = (abi.SrBlockParams * 8)()
+    for i in range(8):
+        for n in abi.PARAM_FIELDS:
+            setattr(params[i], n, FAKE)
+    assert L.sr_sparse_blocks_fwd(ctypes.byref(ada), 25, params, None, FAKE, FAKE + 4096, FAKE, 1 << 40, None, 0,
+                                  None) == abi.SR_EINVAL   # adaLN without cond
+    need = abi.sr_workspace_bytes(c, 25)[0]
+    assert L.sr_sparse_blocks_fwd(ctypes.byref(c), 25, params, None, FAKE, FAKE + 4096, FAKE, need - 1, None, 0,
+                                  None) == abi.SR_EWORKSPACE
+
+
+def test_trunk_save8_arguments():
+    from paper_2607_02829_amd import inputs
+    from paper_2607_02829_amd.trunk import Trunk
+    w = inputs.small("trunk_s")
+    params = inputs.params_to_storage(inputs.block_params(w, 3), w.dtype)
+    for kw in (dict(save8="yes"), dict(save8=True, select="attn")):
+        with pytest.raises(ValueError):
+            Trunk(w, (1, 1, 1), params, **kw)
