@@ -412,6 +412,27 @@ SR_API sr_status sr_weight_grad8(int32_t dtype, int32_t M, int32_t N, int32_t K,
                           const uint8_t* xe, float* dw, float* db, void* scratch, size_t scratch_bytes,
                           void* stream);
 
+/* The blocks' forward with weights and tokens in 8 bits, for forecasts (nothing is kept for a backward): the
+ * block of sr_config.kind with its four linear layers as sr_linear8 on SR_Q8_ROW tokens (the LayerNorm outputs, the
+ * attention output and GELU's output, each quantised per token) and SR_Q8_ROW weights.  LayerNorm, attention,
+ * modulation and the fp32 residual stream are those of sr_sparse_blocks_fwd.
+ * Parameters of one block: int8 weights [out,in] with fp32 scales [out], as sr_quantize8 (SR_Q8_ROW) gives them
+ * for the rows of nn.Linear weights; the others in storage dtype (ln* for SR_BLOCK_PRELN, w_ada / b_ada for
+ * SR_BLOCK_ADALN, the rest may be NULL). */
+typedef struct {
+  const void *ln1_w, *ln1_b, *b_qkv, *b_o, *ln2_w, *ln2_b, *b_fc1, *b_fc2, *w_ada, *b_ada;
+  const int8_t *w_qkv, *w_o, *w_fc1, *w_fc2;
+  const float *s_qkv, *s_o, *s_fc1, *s_fc2;
+} sr_block_params8;
+
+/* Bytes of scratch for S tokens per sample (never less for more of S or B). */
+SR_API sr_status sr_blocks8_scratch_bytes(const sr_config* cfg, int32_t S, size_t* scratch_bytes);
+
+/* h_in [B,S,D] -> h_out [B,S,D] (storage dtype; may alias h_in): n_blocks blocks; params: host array of n_blocks;
+ * cond: [B,D] (ADALN) or NULL.  S is not bounded by cfg->L. */
+SR_API sr_status sr_blocks8_fwd(const sr_config* cfg, int32_t S, const sr_block_params8* params, const void* cond,
+                         const void* h_in, void* h_out, void* scratch, size_t scratch_bytes, void* stream);
+
 /* Launch timing for measurement (not needed by the method).  After
  * sr_profile_start, every library launch group whose name contains `name_filter`
  * ("" or NULL = all) is timed with HIP events bound to its first and last kernel at launch
@@ -427,7 +448,8 @@ SR_API sr_status sr_weight_grad8(int32_t dtype, int32_t M, int32_t N, int32_t K,
  * scatter_delta, gather_f32, scatter_f32, ln_fwd, ln_bwd,
  * gemm_<op> (qkv, o, fc1, fc2, dx_fc2, dx_fc1, dx_o, dx_qkv, dw_<op>), attn_fwd,
  * attn_bwd_dkv, attn_bwd_dq, attn_bwd_f32 (both passes of fp32 storage), attn_bwd_delta, reduce,
- * colsum, convert, mod, quantize8, dequantize8, linear8, weight_grad8.  Where few workgroups make dK/dV and dQ one launch (bf16, head dim 64),
+ * colsum, convert, mod, quantize8, dequantize8, linear8, weight_grad8,
+ * ln_quant.  Where few workgroups make dK/dV and dQ one launch (bf16, head dim 64),
  * attn_bwd_dkv holds both passes. */
 SR_API sr_status sr_profile_start(const char* name_filter);
 SR_API sr_status sr_profile_stop(char* out, size_t out_bytes, size_t* needed);

@@ -142,3 +142,28 @@ def stack_bwd_kept(dh, params64, caches):
         dh, grads[i], dc = block_bwd_kept(dh, params64[i], caches[i])
         dcond = dc if dcond is None or dc is None else dcond + dc
     return dh, grads, dcond
+
+
+def _linear8(x, w, b):
+    """Rows of x (B, S, K) and of w quantised, their product, bias."""
+    xq, xs = quant_rows(x.reshape(-1, x.shape[-1]))
+    wq, ws = quant_rows(w)
+    return linear(xq, xs, wq, ws, b).reshape(*x.shape[:-1], w.shape[0])
+
+
+def block_fwd8(h, p, H, eps, kind="preln", cond=None):
+    """oracle.block.block_fwd with its four linear layers on 8-bit rows."""
+    D = h.shape[-1]
+    ada = kind == "adaln"
+    if ada:
+        sh1, sc1, g1, sh2, sc2, g2 = blk._mod_chunks(p, cond)[0]
+        u = blk.ln_fwd(h, None, None, eps)[0] * (1.0 + sc1) + sh1
+    else:
+        u = blk.ln_fwd(h, p["ln1_w"], p["ln1_b"], eps)[0]
+    qkv = _linear8(u, p["w_qkv"], p["b_qkv"])
+    O = blk.merge_heads(blk.attention_fwd(*(blk.split_heads(qkv[..., i * D:(i + 1) * D], H) for i in range(3))))
+    a = _linear8(O, p["w_o"], p["b_o"])
+    h1 = h + (g1 * a if ada else a)
+    n2 = blk.ln_fwd(h1, None, None, eps)[0] * (1.0 + sc2) + sh2 if ada else blk.ln_fwd(h1, p["ln2_w"], p["ln2_b"], eps)[0]
+    m = _linear8(blk.gelu(_linear8(n2, p["w_fc1"], p["b_fc1"])), p["w_fc2"], p["b_fc2"])
+    return h1 + (g2 * m if ada else m)

@@ -31,6 +31,7 @@ EXPORTS = ("sr_last_error", "sr_version", "sr_workspace_bytes", "sr_select_scrat
            "sr_cross_attention_fwd", "sr_cross_attention_bwd",
            "sr_edm_workspace_bytes", "sr_edm_blocks_fwd", "sr_edm_blocks_bwd",
            "sr_quantize8", "sr_dequantize8", "sr_linear8", "sr_weight_grad8", "sr_weight_grad8_scratch_bytes",
+           "sr_blocks8_scratch_bytes", "sr_blocks8_fwd",
            "sr_profile_start", "sr_profile_stop", "sr_probe_mfma_rate")
 
 
@@ -70,6 +71,14 @@ class SrEdmBlockParams(ctypes.Structure):
 
 class SrEdmBlockGrads(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in EDM_PARAM_FIELDS]
+
+
+PARAM8_FIELDS = ("ln1_w", "ln1_b", "b_qkv", "b_o", "ln2_w", "ln2_b", "b_fc1", "b_fc2", "w_ada", "b_ada",
+                 "w_qkv", "w_o", "w_fc1", "w_fc2", "s_qkv", "s_o", "s_fc1", "s_fc2")
+
+
+class SrBlockParams8(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in PARAM8_FIELDS]
 
 
 _lib = None
@@ -113,6 +122,8 @@ def lib(path: str = LIB_PATH):
         "sr_linear8": ([I32, I32, I32, I32, I32, P, P, P, P, P, P, P], I32),
         "sr_weight_grad8_scratch_bytes": ([I32, I32, I32, I32, ctypes.POINTER(SZ)], I32),
         "sr_weight_grad8": ([I32, I32, I32, I32, P, P, P, P, P, P, SZ, P], I32),
+        "sr_blocks8_scratch_bytes": ([CP, I32, ctypes.POINTER(SZ)], I32),
+        "sr_blocks8_fwd": ([CP, I32, P, P, P, P, P, SZ, P], I32),
         "sr_profile_start": ([ctypes.c_char_p], I32),
         "sr_profile_stop": ([ctypes.c_char_p, SZ, ctypes.POINTER(SZ)], I32),
         "sr_probe_mfma_rate": ([P, ctypes.POINTER(ctypes.c_double), P], I32),
@@ -292,6 +303,17 @@ def sr_weight_grad8_scratch_bytes(dtype: int, M: int, N: int, K: int) -> int:
 def sr_weight_grad8(dtype, M, N, K, dy, xq, xe, dw, db, scratch, stream=None):
     _check(lib().sr_weight_grad8(dtype, M, N, K, _p(dy), _p(xq), _p(xe), _p(dw), _p(db), _p(scratch),
                                  _nbytes(scratch), _stream(stream)))
+
+
+def sr_blocks8_scratch_bytes(cfg: SrConfig, S: int) -> int:
+    a = ctypes.c_size_t()
+    _check(lib().sr_blocks8_scratch_bytes(ctypes.byref(cfg), S, ctypes.byref(a)))
+    return a.value
+
+
+def sr_blocks8_fwd(cfg, S, params, cond, h_in, h_out, scratch, stream=None):
+    _check(lib().sr_blocks8_fwd(ctypes.byref(cfg), S, params, _p(cond), _p(h_in), _p(h_out), _p(scratch),
+                                _nbytes(scratch), _stream(stream)))
 
 
 def sr_profile_start(name_filter: str = "") -> None:

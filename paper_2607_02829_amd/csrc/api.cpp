@@ -648,6 +648,54 @@ sr_status sr_linear8(int32_t dtype, int32_t act, int32_t M, int32_t N, int32_t K
   return hip_status(sr::launch_linear8(dtype == SR_BF16 ? sr::kBF16 : sr::kF32, a, st), "linear8");
 }
 
+namespace {
+sr_status check_blocks8(const sr_config* cfg, int32_t S) {
+  SR_CHECK(cfg != nullptr, SR_EINVAL, "cfg is NULL");
+  SR_CHECK(S >= 1, SR_EINVAL, "S=%d must be >= 1", S);
+  sr_config c = *cfg;   // the block calls' checks on S rows per sample; L is not read
+  c.L = S;
+  sr_status s = check_cfg(&c, false, S);
+  if (s != SR_OK) return s;
+  SR_CHECK(cfg->n_blocks >= 1, SR_EINVAL, "n_blocks must be >= 1");
+  SR_CHECK(cfg->F <= 65536, SR_EUNSUPPORTED, "F=%d > 65536", cfg->F);
+  return SR_OK;
+}
+}  // namespace
+
+sr_status sr_blocks8_scratch_bytes(const sr_config* cfg, int32_t S, size_t* scratch_bytes) {
+  sr_status s = check_blocks8(cfg, S);
+  if (s != SR_OK) return s;
+  SR_CHECK(scratch_bytes != nullptr, SR_EINVAL, "scratch_bytes is NULL");
+  *scratch_bytes = sr::layout_blocks8(dims_of(cfg, S), nullptr, nullptr, nullptr, nullptr);
+  return SR_OK;
+}
+
+sr_status sr_blocks8_fwd(const sr_config* cfg, int32_t S, const sr_block_params8* params, const void* cond,
+                         const void* h_in, void* h_out, void* scratch, size_t scratch_bytes, void* stream) {
+  sr_status s = check_blocks8(cfg, S);
+  if (s != SR_OK) return s;
+  SR_CHECK(params != nullptr, SR_EINVAL, "params is NULL");
+  const bool ada = block_kind(cfg) == SR_BLOCK_ADALN;
+  for (int i = 0; i < cfg->n_blocks; ++i) {
+    const sr_block_params8& w = params[i];
+    const void* all[] = {w.w_qkv, w.w_o, w.w_fc1, w.w_fc2, w.s_qkv, w.s_o, w.s_fc1, w.s_fc2, w.b_qkv, w.b_o,
+                         w.b_fc1, w.b_fc2, ada ? w.w_ada : w.ln1_w, ada ? w.b_ada : w.ln1_b,
+                         ada ? w.w_ada : w.ln2_w, ada ? w.b_ada : w.ln2_b};
+    for (const void* q : all) {
+      SR_CHECK(q != nullptr, SR_EINVAL, "block %d: a parameter pointer is NULL", i);
+      SR_CHECK(aligned16(q), SR_EALIGN, "block %d: a parameter pointer is not 16-byte aligned", i);
+    }
+  }
+  if (ada) SR_PTR(cond, "cond");
+  SR_PTR(h_in, "h_in");
+  SR_PTR(h_out, "h_out");
+  const sr::Dims d = dims_of(cfg, S);
+  const size_t need = sr::layout_blocks8(d, nullptr, nullptr, nullptr, nullptr);
+  SR_PTR(scratch, "scratch");
+  SR_CHECK(scratch_bytes >= need, SR_EWORKSPACE, "scratch buffer has %zu bytes, needs %zu", scratch_bytes, need);
+  return hip_status(sr::blocks8_fwd(d, params, cond, h_in, h_out, (char*)scratch, (hipStream_t)stream), "blocks8_fwd");
+}
+
 sr_status sr_weight_grad8_scratch_bytes(int32_t dtype, int32_t M, int32_t N, int32_t K, size_t* scratch_bytes) {
   sr_status s = check_wgrad8(dtype, M, N, K);
   if (s != SR_OK) return s;

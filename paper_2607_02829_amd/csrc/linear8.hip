@@ -48,6 +48,21 @@ SR_DEV Cols load_cols(const Linear8& a, int n) {
   c.bias = a.bias ? load4<T>(a.bias, n) : f32x4{0.f, 0.f, 0.f, 0.f};
   return c;
 }
+// Type of what a tile stages, and the store of columns n .. n + 3 of row m.
+template <int ACT, typename T>
+struct OutOf { typedef T type; };
+template <typename T>
+struct OutOf<kActResid, T> { typedef float type; };
+template <int ACT, typename T>
+SR_DEV void put4(const Linear8& a, int m, int n, f32x4 v) {
+  const size_t o = (size_t)m * a.N + n;
+  if constexpr (ACT == kActResid) {
+    if (a.gate) v *= *reinterpret_cast<const f32x4*>(a.gate + (size_t)(m / a.S) * a.gate_stride + n);
+    *reinterpret_cast<f32x4*>(a.out + o) = *reinterpret_cast<const f32x4*>(a.resid + o) + v;
+  } else {
+    store4<T>(a.y, o, v);
+  }
+}
 template <int ACT, typename T>
 SR_DEV f32x4 finish4(float xs, const Cols& c, i32x4 acc) {
   f32x4 v;
@@ -232,7 +247,8 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear8_tile_kernel(Li
     // register quad (register r: channel 8 (r/4) + 4 h + r%4, token lane % 32) and finishes them where they are.  The
     // results go through LDS, IPP blocks of every wave row at a time, so that memory sees whole rows of the tile
     // (16200 x 4096 x 1024: 105 us in 32-byte pieces from the registers, 95 in rows).
-    constexpr int E = sizeof(T), LDB = BN * E + 16, PR = 32 * WM;
+    typedef typename OutOf<ACT, T>::type O;
+    constexpr int E = sizeof(O), LDB = BN * E + 16, PR = 32 * WM;
     constexpr int FIT = NST * SB / (PR * LDB), IPP = FIT >= MI ? MI : FIT >= 2 && MI % 2 == 0 ? 2 : 1;
     static_assert(IPP * PR * LDB <= NST * SB && MI % IPP == 0, "staging fits the stages");
     constexpr int CPR = BN * E / 16, NB = IPP * PR * CPR / NT;
@@ -255,7 +271,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear8_tile_kernel(Li
                             *reinterpret_cast<const f32x4*>(sc + BN + nb + 8 * q + 4 * h)};
             v[q] = finish4<ACT, T>(xs, c, i32x4{acc[p + i][j][4 * q], acc[p + i][j][4 * q + 1], acc[p + i][j][4 * q + 2],
                                                 acc[p + i][j][4 * q + 3]});
-            store4<T>(row, nb + 8 * q + 4 * h, v[q]);
+            store4<O>(row, nb + 8 * q + 4 * h, v[q]);
           }
         }
       }
@@ -264,8 +280,11 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear8_tile_kernel(Li
       for (int b = 0; b < NB; ++b) {
         const int c = threadIdx.x + NT * b, lr = c / CPR, col = c % CPR * (16 / E), blk = lr >> 5;
         const int m = m0 + blk % WM * (BM / WM) + 32 * (p + blk / WM) + (lr & 31), n = n0 + col;
-        if (m < a.M && n < a.N)
-          *reinterpret_cast<i32x4*>((T*)a.y + (size_t)m * a.N + n) = *reinterpret_cast<const i32x4*>(smem + lr * LDB + col * E);
+        if (m < a.M && n < a.N) {
+          const i32x4 w = *reinterpret_cast<const i32x4*>(smem + lr * LDB + col * E);
+          if constexpr (ACT == kActResid) put4<ACT, T>(a, m, n, __builtin_bit_cast(f32x4, w));
+          else *reinterpret_cast<i32x4*>((T*)a.y + (size_t)m * a.N + n) = w;
+        }
       }
     }
   } else {
@@ -309,7 +328,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear8_tile_kernel(Li
           i32x4 v = *reinterpret_cast<const i32x4*>(stg + lr * LD + c4);
 #pragma unroll
           for (int g = 1; g < KG; ++g) v += *reinterpret_cast<const i32x4*>(stg + (g * PR + lr) * LD + c4);
-          store4<T>(a.y, (size_t)m * a.N + n, finish4<ACT, T>(xs[p][q], cols, v));
+          put4<ACT, T>(a, m, n, finish4<ACT, T>(xs[p][q], cols, v));
         }
       }
     }
@@ -354,7 +373,7 @@ __global__ __launch_bounds__(64 * W) void linear8_few_kernel(Linear8 a) {
       i32x4 v = *reinterpret_cast<const i32x4*>(&stg[0][lr][c4]);
 #pragma unroll
       for (int g = 1; g < W; ++g) v += *reinterpret_cast<const i32x4*>(&stg[g][lr][c4]);
-      store4<T>(a.y, (size_t)m * a.N + n, finish4<ACT, T>(a.xs[m], load_cols<T>(a, n), v));
+      put4<ACT, T>(a, m, n, finish4<ACT, T>(a.xs[m], load_cols<T>(a, n), v));
     }
   }
 }
@@ -421,7 +440,12 @@ int pick_shape(const Linear8& a) {
 
 template <typename T>
 hipError_t run(int shape, const Linear8& a, hipStream_t st) {
-  return a.act == SR_ACT_GELU ? run_shape<SR_ACT_GELU, T>(shape, a, st) : run_shape<SR_ACT_NONE, T>(shape, a, st);
+  switch (a.act) {
+    case SR_ACT_NONE: return run_shape<SR_ACT_NONE, T>(shape, a, st);
+    case SR_ACT_GELU: return run_shape<SR_ACT_GELU, T>(shape, a, st);
+    case kActResid: return run_shape<kActResid, T>(shape, a, st);
+  }
+  return hipErrorInvalidValue;
 }
 
 }  // namespace

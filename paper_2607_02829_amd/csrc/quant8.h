@@ -37,14 +37,24 @@ struct Q8Job {
 constexpr int kMaxQ8Jobs = 6;
 hipError_t launch_q8_jobs(const Q8Job* jobs, int njobs, bool quantize, hipStream_t st);
 
-// y = act(xs_m ws_n sum_k xq_mk wq_nk + bias_n)
+// LayerNorm of the fp32 rows x [M, D] (affine, or modulated by mod as in launch_ln_fwd; D <= 2048) to SR_Q8_ROW
+// codes in one pass.
+hipError_t launch_ln_quant(int dtype, const float* x, const void* gamma, const void* beta, const float* mod, int mod_off,
+                           int M, int S, int D, float eps, int8_t* q, float* scale, hipStream_t st);
+
+// y = act(xs_m ws_n sum_k xq_mk wq_nk + bias_n);  with kActResid out = resid + gate_b (the value before act), fp32
+constexpr int kActResid = 2;
 struct Linear8 {
   int M = 0, N = 0, K = 0;
   const int8_t *xq = nullptr, *wq = nullptr;
   const float *xs = nullptr, *ws = nullptr;
   const void* bias = nullptr;   // storage type, or null
-  void* y = nullptr;            // storage type
+  void* y = nullptr;            // storage type (not with kActResid)
   int act = SR_ACT_NONE;
+  const float* resid = nullptr;   // [M, N]
+  const float* gate = nullptr;    // per sample (S rows each), gate[b * gate_stride + n], or null
+  int gate_stride = 0, S = 1;
+  float* out = nullptr;           // [M, N], may not be resid
 };
 hipError_t launch_linear8(int dtype, const Linear8& a, hipStream_t st);
 

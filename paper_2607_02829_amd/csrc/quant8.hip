@@ -180,6 +180,77 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const T* __restrict__ x
   }
 }
 
+// LayerNorm and the codes of its rows: one wave per row, C chunks of eight channels per lane; mean, variance and
+// maximum from registers, in fp32.
+template <typename T, int C>
+__global__ __launch_bounds__(256) void ln_quant_kernel(const float* __restrict__ x, const T* __restrict__ gamma,
+                                                       const T* __restrict__ beta, const float* __restrict__ mod,
+                                                       int mod_off, int M, int S, int D, float eps,
+                                                       int8_t* __restrict__ q, float* __restrict__ scale) {
+  const int row = blockIdx.x * 4 + wave_index(), lane = threadIdx.x & 63;
+  if (row >= M) return;
+  const float* shift = mod ? mod + (size_t)(row / S) * 6 * D + mod_off : nullptr;
+  float v[C][8], sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < C; ++i) {
+    const int c = (lane + i * 64) * 8;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+    if (c < D) load8(x + (size_t)row * D + c, v[i]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum += v[i][j];
+  }
+  const float mean = wave_sum(sum) / (float)D;
+  float sq = 0.f;
+#pragma unroll
+  for (int i = 0; i < C; ++i)
+    if ((lane + i * 64) * 8 < D) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        v[i][j] -= mean;
+        sq = fmaf(v[i][j], v[i][j], sq);
+      }
+    }
+  const float rstd = rsqrtf(wave_sum(sq) / (float)D + eps);
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < C; ++i) {
+    const int c = (lane + i * 64) * 8;
+    if (c < D) {
+      float w[8], b[8];
+      if (mod) {
+        load8(shift + D + c, w);
+        load8(shift + c, b);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] += 1.0f;
+      } else {
+        load8(gamma + c, w);
+        load8(beta + c, b);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        v[i][j] = fmaf(v[i][j] * rstd, w[j], b[j]);
+        m = max(m, abs_bits(v[i][j]));
+      }
+    }
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+  const bool ok = m < kInfBits;
+  const float amax = __uint_as_float(m);
+  if (lane == 0) scale[row] = ok ? __fdiv_rn(amax, 127.0f) : __uint_as_float(0x7FC00000u);
+  const RowCode<float> rc(ok && m ? amax : 1.0f);
+#pragma unroll
+  for (int i = 0; i < C; ++i) {
+    const int c = (lane + i * 64) * 8;
+    rc.codes(v[i]);
+    i32x2 b;
+    b[0] = ok ? (int)low_bytes(v[i][0], v[i][1], v[i][2], v[i][3]) : 0;
+    b[1] = ok ? (int)low_bytes(v[i][4], v[i][5], v[i][6], v[i][7]) : 0;
+    if (c < D) *reinterpret_cast<i32x2*>(q + (size_t)row * D + c) = b;
+  }
+}
+
 template <typename T>
 __global__ __launch_bounds__(256) void dequant_rows_kernel(const int8_t* __restrict__ q, const float* __restrict__ scale,
                                                            size_t n8, int N8, T* __restrict__ x) {
@@ -306,6 +377,25 @@ hipError_t launch_q8_jobs(const Q8Job* jobs, int njobs, bool quantize, hipStream
   if (quantize) SR_LAUNCH(q8_jobs_kernel<true>, dim3((unsigned)blocks), dim3(256), 0, st, js);
   else SR_LAUNCH(q8_jobs_kernel<false>, dim3((unsigned)blocks), dim3(256), 0, st, js);
   return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t ln_quant(const float* x, const void* gamma, const void* beta, const float* mod, int mod_off, int M, int S,
+                           int D, float eps, int8_t* q, float* scale, hipStream_t st) {
+  auto rows = [&](auto c) {
+    SR_LAUNCH((ln_quant_kernel<T, decltype(c)::value>), dim3((unsigned)((M + 3) / 4)), dim3(256), 0, st, x,
+              (const T*)gamma, (const T*)beta, mod, mod_off, M, S, D, eps, q, scale);
+  };
+  if (D <= 512) rows(IC<1>{});
+  else if (D <= 1024) rows(IC<2>{});
+  else if (D <= 2048) rows(IC<4>{});
+  else return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+hipError_t launch_ln_quant(int dtype, const float* x, const void* gamma, const void* beta, const float* mod, int mod_off,
+                           int M, int S, int D, float eps, int8_t* q, float* scale, hipStream_t st) {
+  return dtype == kBF16 ? ln_quant<bf16_t>(x, gamma, beta, mod, mod_off, M, S, D, eps, q, scale, st)
+                        : ln_quant<float>(x, gamma, beta, mod, mod_off, M, S, D, eps, q, scale, st);
 }
 
 hipError_t launch_quantize8(int kind, int dtype, int M, int N, const void* x, int8_t* q, void* scale, hipStream_t st) {

@@ -231,7 +231,7 @@ static int fwd_attn_part(const Dims& d, const BlockSaved& s, AttnPart* part) {
     for (size_t o = 0; o + plane <= floats && n < kMaxSplit; o += plane) part->p[n++] = (float*)base + o;
   };
   add(s.h1, plane);
-  add(s.z, act);
+  if (s.z) add(s.z, act);
   add(s.gz, act);
   part->ml = (float*)s.u1;   // 8 bytes per run, head and row in a row of 2 hd bytes per head
   return attn_splits(d.dtype, d.B, d.S, d.H, d.D / d.H, n);
@@ -331,6 +331,97 @@ hipError_t stack_fwd(const Dims& d, const sr_block_params* p, const void* cond, 
   err = run();
   delete[] sv;
   return err;
+}
+
+// ============================================================================ forward in 8 bits
+
+// One block's buffers: the residual stream (hin, h1), q, k, v, attention output and GELU output; q, qs: the codes and
+// scales of the product's tokens, of which the codes also serve as the attention planes' row statistics (8 bytes per
+// run, head and row in a row of hd >= 32 bytes per head).
+size_t layout_blocks8(const Dims& d, char* base, BlockSaved* out, int8_t** q, float** qs) {
+  Carver c(base);
+  const size_t M = d.M, D = d.D, F = d.F, e = d.elt;
+  BlockSaved s{};
+  s.hin = c.take<float>(M * D * 4);
+  s.h1 = c.take<float>(M * D * 4);
+  s.qkv = c.take<void>(M * 3 * D * e);
+  s.O = c.take<void>(M * D * e);
+  s.lse = c.take<float>((size_t)d.B * d.H * d.S * 4);
+  s.gz = c.take<void>(M * F * e);
+  if (d.kind == SR_BLOCK_ADALN) s.mod = c.take<float>((size_t)d.B * 6 * D * 4);
+  int8_t* codes = c.take<int8_t>(M * std::max(D, F));
+  float* scales = c.take<float>(M * 4);
+  s.u1 = codes;
+  if (out) {
+    *out = s;
+    *q = codes;
+    *qs = scales;
+  }
+  return c.off;
+}
+
+hipError_t blocks8_fwd(const Dims& d, const sr_block_params8* p, const void* cond, const void* h_in, void* h_out,
+                       char* scratch, hipStream_t st) {
+  BlockSaved s;
+  int8_t* q = nullptr;
+  float* qs = nullptr;
+  layout_blocks8(d, scratch, &s, &q, &qs);
+  const int M = d.M, D = d.D, F = d.F, S = d.S;
+  const size_t e = d.elt;
+  const bool ada = d.kind == SR_BLOCK_ADALN;
+  Linear8 a;   // the product that the codes in q are the tokens of
+  auto product = [&](int N, int K, const int8_t* w, const float* ws, const void* bias, int out_elt) {
+    ProfScope ps("linear8", gemm_flops(M, N, K), (double)M * K + (double)N * K + (double)M * N * out_elt, st);
+    a.M = M; a.N = N; a.K = K; a.xq = q; a.xs = qs; a.wq = w; a.ws = ws; a.bias = bias; a.S = S;
+    return launch_linear8(d.dtype, a, st);
+  };
+  auto rows = [&](const void* x, int N) {
+    ProfScope ps("quantize8", 0, (double)M * N * (e + 1), st);
+    return launch_quantize8(SR_Q8_ROW, d.dtype, M, N, x, q, qs, st);
+  };
+  auto norm = [&](const float* x, const void* g, const void* b, int mod_off) {
+    ProfScope ps("ln_quant", 0, (double)M * D * 5, st);
+    return launch_ln_quant(d.dtype, x, g, b, ada ? s.mod : nullptr, mod_off, M, S, D, d.eps, q, qs, st);
+  };
+  auto branch = [&](const float* resid, float* out, int gate_off) {   // out = resid + gate (the product)
+    a.act = kActResid; a.resid = resid; a.out = out;
+    a.gate = ada ? s.mod + gate_off : nullptr; a.gate_stride = 6 * D;
+  };
+  {
+    ProfScope ps("convert", 0, (double)M * D * (e + 4), st);
+    SR_TRY(launch_convert(d.dtype, h_in, kF32, s.hin, (size_t)M * D, nullptr, st));
+  }
+  for (int i = 0; i < d.nb; ++i) {
+    const sr_block_params8& w = p[i];
+    if (ada) {
+      ProfScope ps("mod", gemm_flops(d.B, 6 * D, D), gemm_bytes(d, d.B, 6 * D, D, 4), st);
+      SR_TRY(launch_gemv_rows(d.dtype, cond, D, w.w_ada, w.b_ada, d.B, 6 * D, D, s.mod, 6 * D, st));
+    }
+    SR_TRY(norm(s.hin, w.ln1_w, w.ln1_b, 0));
+    a = Linear8{};
+    a.y = s.qkv;
+    SR_TRY(product(3 * D, D, w.w_qkv, w.s_qkv, w.b_qkv, (int)e));
+    {
+      ProfScope ps("attn_fwd", 4.0 * d.B * (double)S * S * D, (double)M * D * e * 4, st);
+      AttnPart part;
+      const int runs = fwd_attn_part(d, s, &part);
+      SR_TRY(launch_attn_fwd(d.dtype, s.qkv, s.O, s.lse, d.B, S, d.H, D, st, runs, part));
+    }
+    SR_TRY(rows(s.O, D));
+    a = Linear8{};
+    branch(s.hin, s.h1, 2 * D);
+    SR_TRY(product(D, D, w.w_o, w.s_o, w.b_o, 8));
+    SR_TRY(norm(s.h1, w.ln2_w, w.ln2_b, 3 * D));
+    a = Linear8{};
+    a.act = SR_ACT_GELU; a.y = s.gz;
+    SR_TRY(product(F, D, w.w_fc1, w.s_fc1, w.b_fc1, (int)e));
+    SR_TRY(rows(s.gz, F));
+    a = Linear8{};
+    branch(s.h1, s.hin, 5 * D);
+    SR_TRY(product(D, F, w.w_fc2, w.s_fc2, w.b_fc2, 8));
+  }
+  ProfScope ps("convert", 0, (double)M * D * (e + 4), st);
+  return launch_convert(kF32, s.hin, d.dtype, h_out, (size_t)M * D, nullptr, st);
 }
 
 // ============================================================================ backward

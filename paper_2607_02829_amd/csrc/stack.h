@@ -58,6 +58,10 @@ size_t scratch_bytes(const Dims& d);
 // With `rt`, h_in / h_out (forward) and dh_out / dh_in (backward) are unused.
 hipError_t stack_fwd(const Dims& d, const sr_block_params* p, const void* cond, const void* h_in, void* h_out,
                      char* saved, hipStream_t st, const Route* rt = nullptr);
+// Forward of the blocks with weights and tokens in 8 bits (sr_blocks8_fwd); nothing is kept.
+size_t layout_blocks8(const Dims& d, char* base, BlockSaved* out, int8_t** q, float** qs);
+hipError_t blocks8_fwd(const Dims& d, const sr_block_params8* p, const void* cond, const void* h_in, void* h_out,
+                       char* scratch, hipStream_t st);
 hipError_t stack_bwd(const Dims& d, const sr_block_params* p, const void* cond, const char* saved,
                      const void* dh_out, void* dh_in, const sr_block_grads* g, float* dcond, char* scratch, size_t scratch_size,
                      hipStream_t st, const Route* rt = nullptr);

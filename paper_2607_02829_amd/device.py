@@ -54,6 +54,32 @@ class DeviceParams:
                 setattr(self.array[i], name, p[name].data_ptr() if use else None)
 
 
+class DeviceParams8:
+    """Block parameters with the linear weights in 8 bits (sr_quantize8 by output channel, on the
+    current stream) plus the host array of sr_block_params8.  ``src``: the DeviceParams to take them
+    from; its biases, LayerNorm and modulation parameters are shared, not copied."""
+
+    LINEAR = ("w_qkv", "w_o", "w_fc1", "w_fc2")
+
+    def __init__(self, src: DeviceParams):
+        import torch
+        self.src = src
+        self.tensors = []
+        self.array = (abi.SrBlockParams8 * len(src.tensors))()
+        for i, p in enumerate(src.tensors):
+            t = {}
+            for name in self.LINEAR:
+                w = p[name]
+                q = torch.empty(w.shape, dtype=torch.int8, device=w.device)
+                s = torch.empty(w.shape[0], dtype=torch.float32, device=w.device)
+                abi.sr_quantize8(abi.SR_Q8_ROW, abi.SR_BF16 if w.dtype == torch.bfloat16 else abi.SR_F32,
+                                 w.shape[0], w.shape[1], w, q, s)
+                t[name], t["s" + name[1:]] = q, s
+            self.tensors.append(t)
+            for name in abi.PARAM8_FIELDS:
+                setattr(self.array[i], name, t[name].data_ptr() if name in t else getattr(src.array[i], name))
+
+
 class DeviceGrads:
     """fp32 gradient buffers for n blocks plus the host array of sr_block_grads."""
 

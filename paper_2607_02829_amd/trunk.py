@@ -86,6 +86,7 @@ class Trunk:
         if save8:
             for c in self.cfg:
                 c.kind |= abi.SR_BLOCK_SAVE8
+        self.params8 = None
         bounds = (0, n1, n1 + n2, n1 + n2 + n3)
         self.params = [device.DeviceParams(params_storage[bounds[i]:bounds[i + 1]], w.kind) for i in range(3)]
         self.grads = [device.DeviceGrads(w, n, skip_unused=True) for n in split]
@@ -150,6 +151,31 @@ class Trunk:
             a.sr_dense_blocks_fwd(ce, pe.array, None, self.x0, self.g0, self.saved[0], self.scratch)
         a.sr_dense_blocks_bwd(ce, pe.array, None, self.saved[0], self.g2, self.g0, ge, None, self.scratch)
         return self.g0
+
+    def quantize(self):
+        """Take the linear weights into 8 bits for ``forecast`` (again after they change)."""
+        import torch
+        if self.select == "attn":
+            raise ValueError("the attention-score selector needs the early stage's saved activations")
+        self.params8 = [device.DeviceParams8(p) for p in self.params]
+        n = max(abi.sr_blocks8_scratch_bytes(c, s) for c, s in zip(self.cfg, (self.w.L, self.K, self.w.L)))
+        self.scratch8 = torch.empty(n, dtype=torch.uint8, device="cuda")
+
+    def forecast(self, x0, step: int):
+        """The forward with weights and tokens in 8 bits (``quantize`` first), keeping nothing for a
+        backward: x0 (B, L, D) storage tensor, not modified.  Returns the trunk output x3; an earlier
+        ``forward``'s buffers (x1, x3, idx, h0, h) are overwritten."""
+        if self.params8 is None:
+            raise RuntimeError("forecast needs quantize() first")
+        a, (ce, cm, cl), (pe, pm, pl) = abi, self.cfg, self.params8
+        K, L = self.K, self.w.L
+        a.sr_blocks8_fwd(ce, L, pe.array, None, x0, self.x1, self.scratch8)
+        a.sr_select_indices(cm, K, a.SR_SEL_RANDOM, self.seed, step, None, None, self.idx)
+        a.sr_gather(cm, K, self.x1, self.idx, self.h0)
+        a.sr_blocks8_fwd(cm, K, pm.array, None, self.h0, self.h, self.scratch8)
+        a.sr_scatter_delta(cm, K, self.x1, self.h, self.h0, self.idx)
+        a.sr_blocks8_fwd(cl, L, pl.array, None, self.x1, self.x3, self.scratch8)
+        return self.x3
 
     def block_grads(self):
         """The fp32 gradient tensors of all n1 + n2 + n3 blocks, in trunk order."""

@@ -1,0 +1,104 @@
+"""The blocks' forward with weights and tokens in 8 bits (sr_blocks8_fwd) against the oracle's block on 8-bit
+rows, and the trunk's forecast built from it."""
+import numpy as np
+import pytest
+
+import gpu_helpers as gh
+from oracle import quant8 as oq
+from oracle import stack as ostack
+from oracle.numerics import storage_to_f64
+from paper_2607_02829_amd import abi, device, inputs
+from paper_2607_02829_amd.trunk import Trunk
+
+pytestmark = pytest.mark.gpu
+
+CASES = {
+    "preln_bf16": (inputs.small("b8_p", B=2, Hg=9, Wg=15, D=256, H=4, F=1024), 2),
+    "preln_f32": (inputs.small("b8_f", B=1, Hg=7, Wg=11, D=128, H=2, F=512, dtype="f32"), 2),
+    "adaln_bf16": (inputs.small("b8_a", B=3, Hg=9, Wg=15, D=256, H=4, F=1024, kind="adaln"), 2),
+    "adaln_f32": (inputs.small("b8_b", B=2, Hg=5, Wg=7, D=64, H=2, F=256, dtype="f32", kind="adaln"), 2),
+    "one_token": (inputs.small("b8_1", B=1, Hg=1, Wg=1, D=1024, H=16, F=4096), 2),
+    "head_dim_128": (inputs.small("b8_h", B=1, Hg=10, Wg=13, D=1280, H=10, F=2048), 1),
+    "ragged_large": (inputs.small("b8_l", B=1, Hg=25, Wg=41, D=512, H=8, F=2048), 1),
+}
+
+
+def _run(w, S, h, params, cond, stream=None, alias=False):
+    import torch
+    cfg = device.config_for(w, n_blocks=len(params))
+    dp = device.DeviceParams(params, w.kind)
+    p8 = device.DeviceParams8(dp)
+    hd = device.to_device(h)
+    c = device.to_device(cond) if cond is not None else None
+    n = abi.sr_blocks8_scratch_bytes(cfg, S)
+    buf = torch.full((n + 4096,), 0x77, dtype=torch.uint8, device="cuda")
+    out = hd if alias else torch.empty_like(hd)
+    abi.sr_blocks8_fwd(cfg, S, p8.array, c, hd, out, (buf.data_ptr(), n))
+    torch.cuda.synchronize()
+    assert bool((buf[n:] == 0x77).all())
+    return device.to_host(out)
+
+
+@pytest.mark.parametrize("case", list(CASES))
+def test_blocks8_match_the_oracle(case):
+    w, nb = CASES[case]
+    print(f"[blocks8 {case}] B={w.B} S={w.L} D={w.D} {w.dtype} {w.kind}", flush=True)
+    h, params, cond, _ = gh.host_inputs(w, nb)
+    got = _run(w, w.L, h, params, cond)
+    p64 = ostack.params_f64(params)
+    c64 = storage_to_f64(cond) if cond is not None else None
+    ref = h64 = storage_to_f64(h)
+    for p in p64:
+        ref = oq.block_fwd8(ref, p, w.H, 1e-6, w.kind, c64)
+    # Both sides round each product's tokens to a step s = a / 127 of the row, and what they round differs by rounding
+    # errors upstream that, of the order of a step, decide codes differently: an element then differs by at most the two
+    # roundings, sqrt(2) s / sqrt(12) = 0.41 s in the mean square.  With a largest value of at most four deviations
+    # (rows of up to 4096) that is 1.3 % per operand; four operands per block (the weights' codes are the same), blocks
+    # and operands adding in squares: 0.013 sqrt(8) = 3.6 % of the blocks' update for two blocks.
+    full, _ = ostack.stack_fwd(h64, p64, w.H, 1e-6, w.kind, c64)
+    assert np.linalg.norm(storage_to_f64(got) - ref) <= 0.04 * np.linalg.norm(full - h64)
+    # and the blocks' own update (h_out - h_in) within 4 % of the one without 8 bits: 0.5 % per rounded operand (a step of
+    # a / 127 for rows whose largest value is three to four deviations), eight operands a block in squares, two blocks
+    assert np.linalg.norm(ref - full) <= 0.04 * np.linalg.norm(full - h64)
+    assert np.array_equal(_run(w, w.L, h, params, cond, alias=True), got)
+
+
+def test_a_non_finite_sample_leaves_the_others_alone():
+    w, nb = CASES["adaln_bf16"]
+    h, params, cond, _ = gh.host_inputs(w, nb)
+    clean = _run(w, w.L, h, params, cond)
+    h2 = h.copy()
+    h2[1, 4, 9] = 0x7F80   # Inf
+    got = _run(w, w.L, h2, params, cond)
+    assert np.array_equal(got[[0, 2]], clean[[0, 2]]) and not np.isfinite(storage_to_f64(got[1])).all()
+
+
+@pytest.mark.parametrize("w,split", [(inputs.small("b8_t", Hg=10, Wg=21), (1, 2, 1)),
+                                     (inputs.WORKLOADS["b5625"].with_(B=2), (1, 2, 1))], ids=["small", "b5625"])
+def test_forecast_follows_the_forward(w, split):
+    import torch
+    params = inputs.params_to_storage(inputs.block_params(w, sum(split), randomise_affine=True), w.dtype)
+    x0 = device.to_device(inputs.to_storage(inputs.token_field(w), w.dtype))
+    tr = Trunk(w, split, params, seed=7)
+    with pytest.raises(RuntimeError):
+        tr.forecast(x0, 3)
+    x3 = tr.forward(x0, 3).clone()
+    idx = tr.idx.clone()
+    tr.quantize()
+    y = tr.forecast(x0, 3).clone()
+    torch.cuda.synchronize()
+    assert torch.equal(tr.idx, idx)
+    d = (x3.double() - x0.double()).norm()
+    assert float((y.double() - x3.double()).norm() / d) <= 0.05
+    # replays of a captured forecast, with eager work between them
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        tr.forecast(x0, 3)
+    for rep in range(3):
+        tr.x3.zero_(); tr.x1.zero_(); tr.scratch8.fill_(0xFF)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(tr.x3.view(torch.int16), y.view(torch.int16)), rep
+        tr.forward(x0, 4)
+        torch.cuda.synchronize()

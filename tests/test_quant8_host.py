@@ -180,3 +180,35 @@ def test_trunk_save8_arguments():
     for kw in (dict(save8="yes"), dict(save8=True, select="attn")):
         with pytest.raises(ValueError):
             Trunk(w, (1, 1, 1), params, **kw)
+
+
+def test_blocks8_refusals():
+    L = _lib()
+    n = ctypes.c_size_t()
+    c = _cfg()
+    assert L.sr_blocks8_scratch_bytes(ctypes.byref(c), 0, ctypes.byref(n)) == abi.SR_EINVAL
+    assert L.sr_blocks8_scratch_bytes(ctypes.byref(c), 10, None) == abi.SR_EINVAL
+    assert L.sr_blocks8_scratch_bytes(None, 10, ctypes.byref(n)) == abi.SR_EINVAL
+    assert L.sr_blocks8_scratch_bytes(ctypes.byref(_cfg(B=1)), 200000, ctypes.byref(n)) == abi.SR_EUNSUPPORTED
+    assert L.sr_blocks8_scratch_bytes(ctypes.byref(_cfg(n_blocks=0)), 10, ctypes.byref(n)) == abi.SR_EINVAL
+    last = 0
+    for S in range(1, 300):
+        v = abi.sr_blocks8_scratch_bytes(c, S)
+        assert v >= last
+        last = v
+    need = abi.sr_blocks8_scratch_bytes(c, 25)
+    ada = {"w_ada", "b_ada"}
+    for kind in (abi.SR_BLOCK_PRELN, abi.SR_BLOCK_ADALN):
+        c = _cfg(kind=kind, n_blocks=2)
+        for name in abi.PARAM8_FIELDS:
+            used = not (name in ada if kind == abi.SR_BLOCK_PRELN else name.startswith("ln"))
+            for bad, status in ((None, abi.SR_EINVAL), (FAKE + 8, abi.SR_EALIGN)):
+                p = (abi.SrBlockParams8 * 2)()
+                for i in range(2):
+                    for f in abi.PARAM8_FIELDS:
+                        setattr(p[i], f, FAKE)
+                setattr(p[1], name, bad)
+                got = L.sr_blocks8_fwd(ctypes.byref(c), 25, p, FAKE, FAKE, FAKE, FAKE, 16, None)
+                assert got == (status if used else abi.SR_EWORKSPACE), (kind, name)
+    assert L.sr_blocks8_fwd(ctypes.byref(c), 25, p, None, FAKE, FAKE, FAKE, need, None) != abi.SR_OK   # adaLN without cond
+    assert L.sr_blocks8_fwd(ctypes.byref(_cfg()), 25, None, None, FAKE, FAKE, FAKE, need, None) == abi.SR_EINVAL
