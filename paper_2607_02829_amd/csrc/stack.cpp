@@ -21,6 +21,7 @@
 #include "stack.h"
 
 #include <cmath>
+#include <initializer_list>
 #include <mutex>
 #include <vector>
 
@@ -581,14 +582,15 @@ hipError_t stack_bwd(const Dims& d, const sr_block_params* p, const void* cond, 
   // slots: g_act[0] (FC2 stage) and g_act[1] (output-projection stage) are read by dW_fc2 and
   // dW_o; dz[i % 2] by dW_fc1 and dqkv[i % 2] by dW_qkv of block i
   enum { kFc2 = 0, kO = 1, kFc1 = 2, kQkv = 4 };
-  // save8: an activation from its 8 bits back into the one buffer of its kind, before its first reader of the block
-  // and after the side-stream work of the block before it (slot) that read the same buffer
-  auto restore = [&](void* x, int dtype, size_t n, const Kept8& k) -> hipError_t {
-    if (!d.save8) return hipSuccess;
-    const Q8Job job = q8_job(x, dtype, n, k);
-    ProfScope ps("dequantize8", 0, (double)n * ((dtype == kF32 ? 4 : e) + 1), st);
-    return launch_q8_jobs(&job, 1, false, st);
+  // save8: activations from their 8 bits back into the one buffer of each kind, before their first readers of the
+  // block and after the side-stream work of the block before it that read the same buffers
+  auto restore = [&](std::initializer_list<Q8Job> jobs) -> hipError_t {
+    double bytes = 0;
+    for (const Q8Job& j : jobs) bytes += (double)j.n * ((j.dtype == kF32 ? 4 : e) + 1);
+    ProfScope ps("dequantize8", 0, bytes, st);
+    return launch_q8_jobs(jobs.begin(), (int)jobs.size(), false, st);
   };
+
 
   // pre-LN: the LayerNorm parameter gradients (column sums of the ln_bwd partials) are outputs
   // only, so their reductions join the block's weight-gradient reductions in the one launch on
@@ -626,10 +628,14 @@ hipError_t stack_bwd(const Dims& d, const sr_block_params* p, const void* cond, 
       void* const dz = sc.dz[par];
       void* const dqkv = sc.dqkv[par];
       ReduceJob jobs[6];   // this block's reductions (weights, LN2, the previous LN1), after dW_qkv
-      if (d.save8) SR_TRY(join(kFc2));   // the previous block's GELU(z)
-      SR_TRY(restore(s.z, d.dtype, (size_t)M * F, s.k_z));
+      const size_t MD = (size_t)M * D;
+      if (d.save8) {   // for the MLP; the previous block's recomputed GELU(z) and LN2 output read the same
+        SR_TRY(join(kFc2));
+        SR_TRY(join(kFc1 + 1 - par));
+        SR_TRY(restore({q8_job(s.z, d.dtype, (size_t)M * F, s.k_z), q8_job(s.h1, kF32, MD, s.k_h1),
+                        q8_job(s.m_out, d.dtype, ada ? MD : 0, s.k_m)}));
+      }
       if (ada) {
-        SR_TRY(restore(s.m_out, d.dtype, (size_t)M * D, s.k_m));
         // MLP-branch gradient dm = dh' * gate2 (activation copy) and dgate2 = sum_s dh' * m_out
         SR_TRY(join(kFc2));   // g0 may still be read by the previous block's dW_fc2
         SR_TRY(gate_bwd(d, sc.g_res, s.m_out, s.mod + 5 * D, g0, sc.dmod, 5 * D, sc, st));
@@ -651,8 +657,6 @@ hipError_t stack_bwd(const Dims& d, const sr_block_params* p, const void* cond, 
           return launch_gemm(gd, EPI_DGELU, ep, st);
         }));
       }
-      if (d.save8) SR_TRY(join(kFc1 + 1 - par));   // the previous block's LN2 output
-      SR_TRY(restore(s.h1, kF32, (size_t)M * D, s.k_h1));
       // FC1: dW1, db1; du = dz W1
       SR_TRY(on_side(kFc1 + par, [&](hipStream_t ss) -> hipError_t {
         if (g.w_fc1 || g.b_fc1) {   // u2 = LN2(h1) recomputed from the saved statistics
@@ -680,8 +684,12 @@ hipError_t stack_bwd(const Dims& d, const sr_block_params* p, const void* cond, 
         SR_TRY(launch_reduce_cols(sc.lnpart[0][0], nln, d.B, 0, 2 * D, D, sc.dmod + 4 * D, sc.dmod + 3 * D, 6 * D,
                                   st));
       }
+      if (d.save8) {   // for the attention; the previous block's recomputed LN1 output reads hin
+        SR_TRY(join(kQkv + 1 - par));
+        SR_TRY(restore({q8_job(s.qkv, d.dtype, 3 * MD, s.k_qkv), q8_job(s.O, d.dtype, MD, s.k_O),
+                        q8_job(s.hin, kF32, MD, s.k_hin), q8_job(s.a_out, d.dtype, ada ? MD : 0, s.k_a)}));
+      }
       if (ada) {
-        SR_TRY(restore(s.a_out, d.dtype, (size_t)M * D, s.k_a));
         // attention-branch gradient da = dh1 * gate1 and dgate1 = sum_s dh1 * a_out
         SR_TRY(join(kO));   // g1 may still be read by the previous block's dW_o
         SR_TRY(gate_bwd(d, sc.g_res2, s.a_out, s.mod + 2 * D, g1, sc.dmod, 2 * D, sc, st));
@@ -700,8 +708,6 @@ hipError_t stack_bwd(const Dims& d, const sr_block_params* p, const void* cond, 
         }
         return weight_grad("gemm_dw_o", d, g1, D, s.O, D, g.w_o, g.b_o, sc, kWgO, &jobs[kWgO], ss);
       }));
-      SR_TRY(restore(s.O, d.dtype, (size_t)M * D, s.k_O));
-      SR_TRY(restore(s.qkv, d.dtype, (size_t)M * 3 * D, s.k_qkv));
       const bool fuse_delta = d.dtype == kBF16 && D / d.H == 64;
       {
         GemmDesc gd = desc(d, g1, true, D, (size_t)M * D * e, w.w_o, false, D, (size_t)D * D * e, M, D, D);
@@ -719,8 +725,6 @@ hipError_t stack_bwd(const Dims& d, const sr_block_params* p, const void* cond, 
       SR_TRY(fork_point([&]() -> hipError_t {
         return launch_attn_bwd(d.dtype, s.qkv, sc.dO, s.lse, sc.delta, dqkv, d.B, S, d.H, D, st, sc.attn_splits, sc.attn);
       }));
-      if (d.save8) SR_TRY(join(kQkv + 1 - par));   // the previous block's LN1 output
-      SR_TRY(restore(s.hin, kF32, (size_t)M * D, s.k_hin));
       if (!ada) {   // LN2 of this block and LN1 of the block before it join the reduction launch
         if (g.ln2_w || g.ln2_b) jobs[4] = ln_job(sc.lnpart[0][par], g.ln2_w, g.ln2_b);
         if (ln1_pending && (ln1_pending->ln1_w || ln1_pending->ln1_b))
