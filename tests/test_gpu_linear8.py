@@ -97,6 +97,21 @@ def test_linear_on_every_tile_shape(M, N, K, dtype, act):
     _check(_run(M, N, K, dtype, data, act, True), M, N, K, dtype, data, act, True)
 
 
+@pytest.mark.parametrize("M,N,K", [(1 << 20, 8, 64), (1, 1 << 18, 64), (3, 1 << 17, 128), (30011, 24, 65536 // 2)])
+def test_linear_at_extreme_shapes(M, N, K):
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(K)
+    xq = torch.randint(-127, 128, (M, K), generator=gen, device="cuda", dtype=torch.int8)
+    wq = torch.randint(-127, 128, (N, K), generator=gen, device="cuda", dtype=torch.int8)
+    xs, ws = torch.rand(M, generator=gen, device="cuda"), torch.rand(N, generator=gen, device="cuda")
+    y = torch.empty((M, N), device="cuda")
+    abi.sr_linear8(abi.SR_F32, 0, M, N, K, xq, xs, wq, ws, None, y)
+    for lo in range(0, M, 1 << 14):   # sums in fp64 by rows: exact
+        acc = xq[lo:lo + (1 << 14)].double() @ wq.double().t().contiguous()
+        want = acc.float() * xs[lo:lo + (1 << 14), None] * ws[None, :]
+        assert torch.equal(y[lo:lo + (1 << 14)], want)
+
+
 @pytest.mark.parametrize("M", [1, 40, 300])
 def test_largest_sums_are_exact(M):
     # codes of 126 and 127 over the longest K: sums near 2^30, beyond what fp32 holds exactly

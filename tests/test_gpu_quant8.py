@@ -122,6 +122,15 @@ def test_row_format_keeps_non_finite_rows_apart(dtype, bad):
     assert np.isnan(back[[0, 8]]).all() and np.isfinite(back[1:8]).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_longer_than_the_registers(dtype):
+    for M, N in ((3, 8256), (2, 20544)):
+        x = _rows(M, N, dtype, 4)
+        q, s, back = _quant(abi.SR_Q8_ROW, x, dtype)
+        wq, ws = oq.quant_rows(storage_to_f64(x))
+        assert np.array_equal(q, wq) and np.array_equal(s, ws)
+
+
 def test_near_ties_of_fp32_rows():
     # quotients one unit in the last place of x on either side of k + 1/2, which a division in fp32 rounds onto it
     rng = np.random.default_rng(8)

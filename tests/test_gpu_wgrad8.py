@@ -67,7 +67,10 @@ def test_weight_grad_matches_oracle(M, N, K, dtype):
                                          ("bf16", 4101, 1032, 832), ("f32", 4101, 1032, 832), ("bf16", 67, 2056, 1088),
                                          ("f32", 67, 2056, 1088), ("bf16", 8201, 1288, 832), ("bf16", 16333, 72, 192),
                                          ("f32", 16333, 72, 192), ("bf16", 8200, 520, 960), ("f32", 9000, 264, 1088),
-                                         ("bf16", 8192, 4104, 2112)])
+                                         ("bf16", 8192, 4104, 2112),
+                                         # few and many of each
+                                         ("bf16", 1 << 20, 8, 64), ("f32", 1 << 19, 8, 64), ("bf16", 1, 1 << 17, 64),
+                                         ("f32", 2, 8, 1 << 16), ("bf16", 300, 8, 1 << 16)])
 def test_weight_grad_over_many_tokens(dtype, M, N, K):
     import torch
     gen = torch.Generator(device="cuda").manual_seed(M)
