@@ -63,13 +63,19 @@ SR_DEV void put4(const Linear8& a, int m, int n, f32x4 v) {
     store4<T>(a.y, o, v);
   }
 }
+// z Phi(z) as max(z, 0) - |z| Phi(-|z|): two operations fewer than z times Phi(z).  The vector units are what the layer
+// with GELU waits for (65 % busy at 16200 x 4096 x 1024, the matrix pipes 29 %).
+template <int DEG>
+SR_DEV float gelu8(float z) {
+  return fmaf(-fabsf(z), half_erfc_of<DEG>(z, z * z), fmaxf(z, 0.f));
+}
 template <int ACT, typename T>
 SR_DEV f32x4 finish4(float xs, const Cols& c, i32x4 acc) {
   f32x4 v;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     v[q] = fmaf((float)acc[q] * xs, c.ws[q], c.bias[q]);
-    if constexpr (ACT == SR_ACT_GELU) v[q] = gelu_f<gelu_deg<T>()>(v[q]);
+    if constexpr (ACT == SR_ACT_GELU) v[q] = gelu8<gelu_deg<T>()>(v[q]);
   }
   return v;
 }
@@ -100,16 +106,20 @@ struct Fill {
 };
 // delta: the tile's byte offset in a row, or 2^31 past the last tile, which keeps the count of fills in flight
 // uniform: those of rows of the operand then lie past its end and read zeros.  (A row past the operand's last
-// one may wrap into the operand; what it holds reaches no output that is stored.)  half: the row ends after
-// 64 bytes of the tile, and what would be its second half reads zeros.
+// one may wrap into the operand; what it holds reaches no output that is stored.)
 template <int BPW>
-SR_DEV void fill_tile(const uint32_t* off, uint32_t upper, __amdgpu_buffer_rsrc_t rs, char* lds, int wid, uint32_t delta,
-                      bool half) {
+SR_DEV void fill_tile(const uint32_t* off, __amdgpu_buffer_rsrc_t rs, char* lds, int wid, uint32_t delta) {
 #pragma unroll
-  for (int i = 0; i < BPW; ++i) {
-    const uint32_t d = half && (upper >> i & 1u) ? 0x80000000u : delta;
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr_t*)(lds + (wid * BPW + i) * 1024), 16, off[i] + d, 0, 0, 0);
-  }
+  for (int i = 0; i < BPW; ++i)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr_t*)(lds + (wid * BPW + i) * 1024), 16, off[i] + delta, 0, 0, 0);
+}
+// A tile of which the row has the first 64 bytes only: what would be the second half reads zeros.
+template <int BPW>
+SR_DEV void fill_half(const uint32_t* off, uint32_t upper, __amdgpu_buffer_rsrc_t rs, char* lds, int wid, uint32_t delta) {
+#pragma unroll
+  for (int i = 0; i < BPW; ++i)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr_t*)(lds + (wid * BPW + i) * 1024), 16,
+                                             off[i] + (upper >> i & 1u ? 0x80000000u : delta), 0, 0, 0);
 }
 
 // BM x BN workgroup tile on WM x WN waves, each MI x NJ tiles of v_mfma_i32_32x32x32_i8; KG such groups of
@@ -163,9 +173,13 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear8_tile_kernel(Li
     char* st = smem + (grp * NST + s) * SB;
     const int k0 = (t0 + t) * KB;
     const uint32_t delta = t < nmine ? (uint32_t)k0 : 0x80000000u;
-    const bool half = KB > 64 && k0 + KB > a.K;
-    fill_tile<APW>(fla.off, fla.upper, ra, st, wid, delta, half);
-    fill_tile<BPW>(flb.off, flb.upper, rb, st + BM * KB, wid, delta, half);
+    if (KB > 64 && t < nmine && k0 + KB > a.K) {
+      fill_half<APW>(fla.off, fla.upper, ra, st, wid, delta);
+      fill_half<BPW>(flb.off, flb.upper, rb, st + BM * KB, wid, delta);
+    } else {
+      fill_tile<APW>(fla.off, ra, st, wid, delta);
+      fill_tile<BPW>(flb.off, rb, st + BM * KB, wid, delta);
+    }
   };
   // fragment of rows r .. r + 31 at k-step ks: lane's row r + lane % 32, chunk 2 ks + lane / 32; rows 16 apart
   // share the swizzle
@@ -380,7 +394,7 @@ __global__ __launch_bounds__(64 * W) void linear8_few_kernel(Linear8 a) {
 
 // ---------------------------------------------------------------- dispatch
 
-enum Shape { kFew16, k32x32g8, k64x64g2, k64x128, k128x128, k128x128x2, k256x256 };
+enum Shape { kFew16, k32x32g8, k64x64g2, k64x128, k128x128, k128x128x2, k256x128x2, k256x256 };
 
 template <int BM, int BN, int KB, int WM, int WN, int KG, int NST, int OCC, int ACT, typename T>
 hipError_t run_tile(const Linear8& a, hipStream_t st) {
@@ -408,6 +422,9 @@ hipError_t run_shape(int shape, const Linear8& a, hipStream_t st) {
     case k64x128: return run_tile<64, 128, 128, 2, 4, 1, 4, 1, ACT, T>(a, st);
     case k128x128: return run_tile<128, 128, 128, 2, 4, 1, 4, 1, ACT, T>(a, st);
     case k128x128x2: return run_tile<128, 128, 128, 2, 4, 1, 2, 2, ACT, T>(a, st);
+    case k256x128x2:
+      if constexpr (ACT == SR_ACT_GELU) return run_tile<256, 128, 64, 2, 2, 1, 3, 2, ACT, T>(a, st);
+      else break;
     case k256x256: return run_tile<256, 256, 128, 2, 4, 1, 2, 1, ACT, T>(a, st);
   }
   return hipErrorInvalidValue;
@@ -425,8 +442,10 @@ hipError_t run_shape(int shape, const Linear8& a, hipStream_t st) {
 //   workgroups are level or ahead: 4050 x 1024 x 1024 10.9 (10.5), 16200 x 256 x 1024 12.3 (14.4)
 //   256 x 256:  16200 x 4096 x 1024 95 (106), 16200 x 1024 x 4096 67 (80), 16200 x 2048 x 512 36 (32);  with half a
 //   round of them 8192 x 1024 x 4096 45 (42);  with GELU, whose vector work wants the second workgroup,
-//   16200 x 2048 x 2048 88 (94), 16200 x 4096 x 1024 123 (122), 8192 x 4096 x 1024 62 (57)
-// Tiles of 256 x 128 and sixteen waves lie within 4 % of these.
+//   16200 x 2048 x 2048 88 (94), 8192 x 4096 x 1024 62 (57)
+//   256 x 128 of 64-byte stages, two workgroups per CU, with GELU from two rounds of them:  16200 x 4096 x 1024 117
+//   (128 x 128 124, 256 x 256 122), 8192 x 4096 x 1024 55.8 (56.3), 4050 x 4096 x 1024 33.6 (32.7)
+// Elsewhere tiles of 256 x 128, and sixteen waves, lie within 4 % of these.
 int pick_shape(const Linear8& a) {
   auto tiles = [&](int bm, int bn) { return (long)((a.M + bm - 1) / bm) * ((a.N + bn - 1) / bn); };
   const long t16 = tiles(16, 16);
@@ -435,7 +454,9 @@ int pick_shape(const Linear8& a) {
   if (tiles(64, 64) <= 256) return k64x64g2;
   if (tiles(64, 128) <= 256) return k64x128;
   if (a.K >= 2048 && tiles(128, 128) <= 256) return k128x128;
-  return a.K >= (a.act == SR_ACT_GELU ? 2048 : 1024) && tiles(256, 256) >= 200 ? k256x256 : k128x128x2;
+  const bool gelu = a.act == SR_ACT_GELU;
+  if (a.K >= (gelu ? 2048 : 1024) && tiles(256, 256) >= 200) return k256x256;
+  return gelu && tiles(256, 128) >= 1024 ? k256x128x2 : k128x128x2;
 }
 
 template <typename T>

@@ -90,7 +90,7 @@ def test_linear_on_many_tokens(M, N, K):
 @pytest.mark.parametrize("M,N,K", [
     # sizes on either side of every border between tile shapes, ragged in rows, columns and the last 64 of k
     (600, 600, 192), (600, 600, 576), (500, 1032, 2112), (1500, 1032, 448), (2050, 1032, 2112), (4050, 1000, 320),
-    (4100, 3336, 1088), (3600, 3600, 2112), (3500, 4104, 64), (2040, 64, 64), (2064, 64, 64), (250, 250 * 8, 1024),
+    (4100, 3336, 1088), (3600, 3600, 2112), (3500, 4104, 64), (8200, 4104, 192), (2040, 64, 64), (2064, 64, 64), (250, 250 * 8, 1024),
 ])
 def test_linear_on_every_tile_shape(M, N, K, dtype, act):
     data = _data(M, N, K, dtype, seed=1)
