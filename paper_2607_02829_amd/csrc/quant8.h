@@ -6,6 +6,7 @@
 
 #include "../../include/sr.h"
 #include "common.h"
+#include "sr_internal.h"
 
 namespace sr {
 
@@ -36,6 +37,9 @@ struct Q8Job {
 };
 constexpr int kMaxQ8Jobs = 6;
 hipError_t launch_q8_jobs(const Q8Job* jobs, int njobs, bool quantize, hipStream_t st);
+
+// gz = GELU(z) of the pre-activation kept in 8 bits, n elements: launch_gelu of the value restored.
+hipError_t launch_gelu_kept(int dtype, const Kept8& z, void* gz, size_t n, hipStream_t st);
 
 // LayerNorm of the fp32 rows x [M, D] (affine, or modulated by mod as in launch_ln_fwd; D <= 2048) to SR_Q8_ROW
 // codes in one pass.

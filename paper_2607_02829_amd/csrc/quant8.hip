@@ -9,6 +9,7 @@
 //
 // Both are bound by memory: 3 bytes per bf16 element (5 per fp32 one) each way.
 #include "common.h"
+#include "epilogue.h"
 #include "quant8.h"
 #include "sr_internal.h"
 
@@ -305,6 +306,19 @@ __global__ __launch_bounds__(256) void blocks8_kernel(T* __restrict__ x, size_t 
   else dequant_block8<T>(q, e, i, x);
 }
 
+template <typename T>
+__global__ __launch_bounds__(256) void gelu_kept_kernel(Kept8 z, size_t n8, T* __restrict__ gz) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n8) return;
+  const i32x2 w = reinterpret_cast<const i32x2*>(z.q)[i];
+  const float s = block_scale(z.e[i >> 2]);
+  float v[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    v[j] = gelu_f<gelu_deg<T>()>((float)(int8_t)((uint32_t)w[j >> 2] >> (8 * (j & 3))) * s);
+  store8(gz + i * 8, v);
+}
+
 // Job j takes the workgroups [first[j], first[j + 1]).
 struct Q8Jobs {
   Q8Job job[kMaxQ8Jobs];
@@ -376,6 +390,14 @@ hipError_t launch_q8_jobs(const Q8Job* jobs, int njobs, bool quantize, hipStream
   for (int j = njobs; j <= kMaxQ8Jobs; ++j) js.first[j] = blocks;
   if (quantize) SR_LAUNCH(q8_jobs_kernel<true>, dim3((unsigned)blocks), dim3(256), 0, st, js);
   else SR_LAUNCH(q8_jobs_kernel<false>, dim3((unsigned)blocks), dim3(256), 0, st, js);
+  return hipGetLastError();
+}
+
+hipError_t launch_gelu_kept(int dtype, const Kept8& z, void* gz, size_t n, hipStream_t st) {
+  const size_t n8 = n / 8;
+  const dim3 grid((unsigned)((n8 + 255) / 256));
+  if (dtype == kBF16) SR_LAUNCH(gelu_kept_kernel<bf16_t>, grid, dim3(256), 0, st, z, n8, (bf16_t*)gz);
+  else SR_LAUNCH(gelu_kept_kernel<float>, grid, dim3(256), 0, st, z, n8, (float*)gz);
   return hipGetLastError();
 }
 

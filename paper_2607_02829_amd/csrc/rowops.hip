@@ -7,6 +7,7 @@
 // variance over D, two-pass mean/variance in fp32 registers, one wave per row.
 // With adaLN the affine step is replaced by y = xhat * (1 + scale_b) + shift_b.
 #include "common.h"
+#include "quant8.h"
 #include "sr_internal.h"
 
 namespace sr {
@@ -63,6 +64,17 @@ template <int V> SR_DEV void stv(bf16_t* p, const float* v) {
   }
 }
 
+// V consecutive values from element o (a multiple of V) of an activation kept in 8 bits.
+template <int V> SR_DEV void ldv(const Kept8& k, size_t o, float* v) {
+  uint32_t w;
+  if constexpr (V == 4) w = *reinterpret_cast<const uint32_t*>(k.q + o);
+  else if constexpr (V == 2) w = *reinterpret_cast<const uint16_t*>(k.q + o);
+  else w = *reinterpret_cast<const uint8_t*>(k.q + o);
+  const float s = block_scale(k.e[o / kQBlock]);
+#pragma unroll
+  for (int j = 0; j < V; ++j) v[j] = (float)(int8_t)(w >> (8 * j)) * s;
+}
+
 // x: fp32 [M, D]; mod (adaLN): fp32 [B, 6D] with shift at mod_off, scale at mod_off + D.
 // One row per wave.  NJC > 0: every lane holds exactly NJC groups of V columns (D = 64 V NJC,
 // all loads unconditional and issued together); NJC = 0: any D <= 64 V kMaxPerLane.
@@ -72,14 +84,15 @@ template <int V> SR_DEV void stv(bf16_t* p, const float* v) {
 // the first LayerNorm in one pass, with the values and arithmetic of the separate steps.
 // APPLY: mean and rstd are read from mean_out / rstd_out (the forward's statistics) instead of
 // computed, and nothing else is written but y: the LayerNorm output recomputed bit for bit.
-template <typename T, typename Ta, int V, int NJC, bool GATHER = false, bool APPLY = false>
+// KEPT: the rows come from kept instead of x.
+template <typename T, typename Ta, int V, int NJC, bool GATHER = false, bool APPLY = false, bool KEPT = false>
 __global__ __launch_bounds__(256) void ln_fwd_kernel(const float* __restrict__ x, const T* __restrict__ gamma,
                                                      const T* __restrict__ beta, const float* __restrict__ mod,
                                                      int mod_off, int M, int S, int D, float eps,
                                                      Ta* __restrict__ y, float* __restrict__ mean_out,
                                                      float* __restrict__ rstd_out, const T* __restrict__ gsrc,
                                                      const int32_t* __restrict__ gidx, int gL,
-                                                     int gshared, float* __restrict__ xcopy) {
+                                                     int gshared, float* __restrict__ xcopy, Kept8 kept) {
   constexpr int NJ = NJC > 0 ? NJC : kMaxPerLane / V;
   const int lane = threadIdx.x & 63;
   const int row = blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -99,6 +112,7 @@ __global__ __launch_bounds__(256) void ln_fwd_kernel(const float* __restrict__ x
     if (j < n) {
       const int c = col_of<V>(lane, j);
       if constexpr (GATHER) ldv<V>(gr + c, v[j]);
+      else if constexpr (KEPT) ldv<V>(kept, (size_t)row * D + c, v[j]);
       else ldv<V>(xr + c, v[j]);
       if (mod) {
         ldv<V>(shift + D + c, w[j]);
@@ -152,15 +166,15 @@ __global__ __launch_bounds__(256) void ln_fwd_kernel(const float* __restrict__ x
 // dx = dres + (dxhat - mean(dxhat) - xhat * mean(dxhat * xhat)) * rstd with
 // dxhat = du * gamma (or du * (1 + scale_b)).  A workgroup takes kLnBwdRows rows of one
 // sample (two per wave, loads issued together) and writes partial column
-// sums of du * xhat and du to part[(b*nchunk + chunk) * 2D].
+// sums of du * xhat and du to part[(b*nchunk + chunk) * 2D].  KEPT: the rows of x come from kept.
 constexpr int kLnBwdRows = 8;
 
-template <typename T, typename Ta, int V, int NJC>
+template <typename T, typename Ta, int V, int NJC, bool KEPT = false>
 __global__ __launch_bounds__(256) void ln_bwd_kernel(const float* __restrict__ du, const float* __restrict__ x,
                                                      const float* __restrict__ mean, const float* __restrict__ rstd,
                                                      const T* __restrict__ gamma, const float* __restrict__ mod,
                                                      int mod_off, const float* dres, int S, int D, float* dx,
-                                                     Ta* __restrict__ dx_act, float* __restrict__ part) {
+                                                     Ta* __restrict__ dx_act, float* __restrict__ part, Kept8 kept) {
   constexpr int NJ = NJC > 0 ? NJC : kMaxPerLane / V;
   constexpr int RG = 2;                        // rows loaded together
   constexpr int NG = kLnBwdRows / (4 * RG);    // row groups per wave
@@ -204,7 +218,8 @@ __global__ __launch_bounds__(256) void ln_bwd_kernel(const float* __restrict__ d
       for (int j = 0; j < NJ; ++j)
         if (j < n && ok[rr]) {
           ldv<V>(du + rows[rr] * D + col_of<V>(lane, j), g[rr][j]);
-          ldv<V>(x + rows[rr] * D + col_of<V>(lane, j), xv[rr][j]);
+          if constexpr (KEPT) ldv<V>(kept, rows[rr] * D + col_of<V>(lane, j), xv[rr][j]);
+          else ldv<V>(x + rows[rr] * D + col_of<V>(lane, j), xv[rr][j]);
           ldv<V>(dres + rows[rr] * D + col_of<V>(lane, j), rv[rr][j]);
         }
     }
@@ -472,7 +487,7 @@ hipError_t launch_ln_fwd(int dtype, const float* x, const void* gamma, const voi
 #define SR_LNF(T)                                                                                    \
   SR_LAUNCH((ln_fwd_kernel<T, T, V, NJC>), grid1d(M, 4), dim3(256), 0, st, x, (const T*)gamma,      \
                      (const T*)beta, mod, mod_off, M, S, D, eps, (T*)y, mean, rstd, (const T*)nullptr, \
-                     (const int32_t*)nullptr, 0, 0, (float*)nullptr)
+                     (const int32_t*)nullptr, 0, 0, (float*)nullptr, Kept8{})
   by_row_length(D, [&](auto v, auto njc) {
     constexpr int V = decltype(v)::value, NJC = decltype(njc)::value;
     if (dtype == kBF16) SR_LNF(bf16_t); else SR_LNF(float);
@@ -487,7 +502,7 @@ hipError_t launch_ln_fwd_gather(int dtype, const void* xsrc, const int32_t* idx,
 #define SR_LNG(T)                                                                                         \
   SR_LAUNCH((ln_fwd_kernel<T, T, V, NJC, true>), grid1d(M, 4), dim3(256), 0, st, (const float*)nullptr, \
                      (const T*)gamma, (const T*)beta, mod, mod_off, M, S, D, eps, (T*)y, mean, rstd,              \
-                     (const T*)xsrc, idx, L, shared, xcopy)
+                     (const T*)xsrc, idx, L, shared, xcopy, Kept8{})
   by_row_length(D, [&](auto v, auto njc) {
     constexpr int V = decltype(v)::value, NJC = decltype(njc)::value;
     if (dtype == kBF16) SR_LNG(bf16_t); else SR_LNG(float);
@@ -498,14 +513,19 @@ hipError_t launch_ln_fwd_gather(int dtype, const void* xsrc, const int32_t* idx,
 
 hipError_t launch_ln_apply(int dtype, const float* x, const void* gamma, const void* beta, const float* mod,
                            int mod_off, int M, int S, int D, const float* mean, const float* rstd, void* y,
-                           hipStream_t st) {
-#define SR_LNA(T)                                                                                       \
-  SR_LAUNCH((ln_fwd_kernel<T, T, V, NJC, false, true>), grid1d(M, 4), dim3(256), 0, st, x,            \
+                           hipStream_t st, const Kept8* kept) {
+#define SR_LNA(T, KEPT)                                                                                 \
+  SR_LAUNCH((ln_fwd_kernel<T, T, V, NJC, false, true, KEPT>), grid1d(M, 4), dim3(256), 0, st, x,      \
                      (const T*)gamma, (const T*)beta, mod, mod_off, M, S, D, 0.0f, (T*)y, const_cast<float*>(mean), \
-                     const_cast<float*>(rstd), (const T*)nullptr, (const int32_t*)nullptr, 0, 0, (float*)nullptr)
+                     const_cast<float*>(rstd), (const T*)nullptr, (const int32_t*)nullptr, 0, 0, (float*)nullptr, \
+                     kept ? *kept : Kept8{})
   by_row_length(D, [&](auto v, auto njc) {
     constexpr int V = decltype(v)::value, NJC = decltype(njc)::value;
-    if (dtype == kBF16) SR_LNA(bf16_t); else SR_LNA(float);
+    if (kept) {
+      if (dtype == kBF16) SR_LNA(bf16_t, true); else SR_LNA(float, true);
+    } else {
+      if (dtype == kBF16) SR_LNA(bf16_t, false); else SR_LNA(float, false);
+    }
   });
 #undef SR_LNA
   return hipGetLastError();
@@ -515,14 +535,18 @@ int ln_bwd_chunks(int S) { return (S + kLnBwdRows - 1) / kLnBwdRows; }
 
 hipError_t launch_ln_bwd(int dtype, const float* du, const float* x, const float* mean, const float* rstd,
                          const void* gamma, const float* mod, int mod_off, const float* dres, int B, int S, int D,
-                         float* dx, void* dx_act, float* part, hipStream_t st) {
+                         float* dx, void* dx_act, float* part, hipStream_t st, const Kept8* kept) {
   dim3 g(ln_bwd_chunks(S), B);
-#define SR_LNB(T)                                                                                  \
-  SR_LAUNCH((ln_bwd_kernel<T, T, V, NJC>), g, dim3(256), 0, st, du, x, mean, rstd, (const T*)gamma, \
-                     mod, mod_off, dres, S, D, dx, (T*)dx_act, part)
+#define SR_LNB(T, KEPT)                                                                            \
+  SR_LAUNCH((ln_bwd_kernel<T, T, V, NJC, KEPT>), g, dim3(256), 0, st, du, x, mean, rstd, (const T*)gamma, \
+                     mod, mod_off, dres, S, D, dx, (T*)dx_act, part, kept ? *kept : Kept8{})
   by_row_length(D, [&](auto v, auto njc) {
     constexpr int V = decltype(v)::value, NJC = decltype(njc)::value;
-    if (dtype == kBF16) SR_LNB(bf16_t); else SR_LNB(float);
+    if (kept) {
+      if (dtype == kBF16) SR_LNB(bf16_t, true); else SR_LNB(float, true);
+    } else {
+      if (dtype == kBF16) SR_LNB(bf16_t, false); else SR_LNB(float, false);
+    }
   });
 #undef SR_LNB
   return hipGetLastError();

@@ -22,6 +22,12 @@ enum {
   EPI_DO = 9,   // dO store plus the attention row statistic delta (head dim 64)
 };
 
+// An activation kept in 8 bits (SR_Q8_BLOCK): codes, and an exponent byte per 32 of them.
+struct Kept8 {
+  int8_t* q = nullptr;
+  uint8_t* e = nullptr;
+};
+
 struct EpiArgs {
   void* out_act = nullptr;     // activation-type output
   void* out_act2 = nullptr;    // second activation output (GELU value)
@@ -112,16 +118,17 @@ hipError_t launch_ln_fwd_gather(int dtype, const void* xsrc, const int32_t* idx,
                                 const void* gamma, const void* beta, const float* mod, int mod_off, int M, int S,
                                 int D, float eps, void* y, float* mean, float* rstd, hipStream_t st);
 // The LayerNorm output from the forward's saved statistics, bit for bit the ln_fwd result.
+// With kept, x is read from its 8 bits (and may be null), here and in launch_ln_bwd.
 hipError_t launch_ln_apply(int dtype, const float* x, const void* gamma, const void* beta, const float* mod,
                            int mod_off, int M, int S, int D, const float* mean, const float* rstd, void* y,
-                           hipStream_t st);
+                           hipStream_t st, const Kept8* kept = nullptr);
 // gz = GELU(z) of the stored FC1 pre-activation (n elements, a multiple of 8), bit for bit the
 // FC1 epilogue's second output.
 hipError_t launch_gelu(int dtype, const void* z, void* gz, size_t n, hipStream_t st);
 int ln_bwd_chunks(int S);
 hipError_t launch_ln_bwd(int dtype, const float* du, const float* x, const float* mean, const float* rstd,
                          const void* gamma, const float* mod, int mod_off, const float* dres, int B, int S, int D,
-                         float* dx, void* dx_act, float* part, hipStream_t st);
+                         float* dx, void* dx_act, float* part, hipStream_t st, const Kept8* kept = nullptr);
 int colsum_chunks(int S);
 // act = T(X * gate_b) and the partial column sums of X * Y (rows of part: colsum_chunks(S) per sample)
 hipError_t launch_gate_bwd(int dtype, const float* X, const void* Y, const float* gate, int gstride, int B, int S,

@@ -582,8 +582,9 @@ hipError_t stack_bwd(const Dims& d, const sr_block_params* p, const void* cond, 
   // slots: g_act[0] (FC2 stage) and g_act[1] (output-projection stage) are read by dW_fc2 and
   // dW_o; dz[i % 2] by dW_fc1 and dqkv[i % 2] by dW_qkv of block i
   enum { kFc2 = 0, kO = 1, kFc1 = 2, kQkv = 4 };
-  // save8: activations from their 8 bits back into the one buffer of each kind, before their first readers of the
-  // block and after the side-stream work of the block before it that read the same buffers
+  // save8: what the dX products, the attention and the gates read goes from its 8 bits back into the one buffer of
+  // each kind; all of them run on the caller's stream.  The side stream's work and the LayerNorms read the 8 bits
+  // themselves.  The restoring launches come after the forks that need not wait for them.
   auto restore = [&](std::initializer_list<Q8Job> jobs) -> hipError_t {
     double bytes = 0;
     for (const Q8Job& j : jobs) bytes += (double)j.n * ((j.dtype == kF32 ? 4 : e) + 1);
@@ -629,13 +630,10 @@ hipError_t stack_bwd(const Dims& d, const sr_block_params* p, const void* cond, 
       void* const dqkv = sc.dqkv[par];
       ReduceJob jobs[6];   // this block's reductions (weights, LN2, the previous LN1), after dW_qkv
       const size_t MD = (size_t)M * D;
-      if (d.save8) {   // for the MLP; the previous block's recomputed GELU(z) and LN2 output read the same
-        SR_TRY(join(kFc2));
-        SR_TRY(join(kFc1 + 1 - par));
-        SR_TRY(restore({q8_job(s.z, d.dtype, (size_t)M * F, s.k_z), q8_job(s.h1, kF32, MD, s.k_h1),
-                        q8_job(s.m_out, d.dtype, ada ? MD : 0, s.k_m)}));
-      }
+      const Kept8* const x1 = d.save8 ? &s.k_hin : nullptr;   // the LayerNorms' inputs, read in 8 bits
+      const Kept8* const x2 = d.save8 ? &s.k_h1 : nullptr;
       if (ada) {
+        if (d.save8) SR_TRY(restore({q8_job(s.m_out, d.dtype, MD, s.k_m)}));
         // MLP-branch gradient dm = dh' * gate2 (activation copy) and dgate2 = sum_s dh' * m_out
         SR_TRY(join(kFc2));   // g0 may still be read by the previous block's dW_fc2
         SR_TRY(gate_bwd(d, sc.g_res, s.m_out, s.mod + 5 * D, g0, sc.dmod, 5 * D, sc, st));
@@ -644,10 +642,12 @@ hipError_t stack_bwd(const Dims& d, const sr_block_params* p, const void* cond, 
       SR_TRY(on_side(kFc2, [&](hipStream_t ss) -> hipError_t {
         if (g.w_fc2 || g.b_fc2) {   // GELU(z) recomputed from the stored pre-activation
           ProfScope ps("recompute", 0, (double)M * F * e * 2, ss);
-          SR_TRY(launch_gelu(d.dtype, s.z, sc.gz_rc, (size_t)M * F, ss));
+          SR_TRY(d.save8 ? launch_gelu_kept(d.dtype, s.k_z, sc.gz_rc, (size_t)M * F, ss)
+                         : launch_gelu(d.dtype, s.z, sc.gz_rc, (size_t)M * F, ss));
         }
         return weight_grad("gemm_dw_fc2", d, g0, D, sc.gz_rc, F, g.w_fc2, g.b_fc2, sc, kWgFc2, &jobs[kWgFc2], ss);
       }));
+      if (d.save8) SR_TRY(restore({q8_job(s.z, d.dtype, (size_t)M * F, s.k_z)}));
       SR_TRY(join(kFc1 + par));   // dz[par] may still be read by dW_fc1 two blocks back
       {
         GemmDesc gd = desc(d, g0, true, D, (size_t)M * D * e, w.w_fc2, false, F, (size_t)D * F * e, M, F, D);
@@ -662,7 +662,7 @@ hipError_t stack_bwd(const Dims& d, const sr_block_params* p, const void* cond, 
         if (g.w_fc1 || g.b_fc1) {   // u2 = LN2(h1) recomputed from the saved statistics
           ProfScope ps("recompute", 0, (double)M * D * (4 + e), ss);
           SR_TRY(launch_ln_apply(d.dtype, s.h1, w.ln2_w, w.ln2_b, ada ? s.mod : nullptr, 3 * D, M, S, D, s.mean2,
-                                 s.rstd2, sc.u_rc, ss));
+                                 s.rstd2, sc.u_rc, ss, x2));
         }
         return weight_grad("gemm_dw_fc1", d, dz, F, sc.u_rc, D, g.w_fc1, g.b_fc1, sc, kWgFc1, &jobs[kWgFc1], ss);
       }));
@@ -677,21 +677,17 @@ hipError_t stack_bwd(const Dims& d, const sr_block_params* p, const void* cond, 
       SR_TRY(fork_point([&]() -> hipError_t {
         ProfScope ps("ln_bwd", 0, (double)M * D * (16 + e), st);
         return launch_ln_bwd(d.dtype, sc.du, s.h1, s.mean2, s.rstd2, w.ln2_w, ada ? s.mod : nullptr, 3 * D, sc.g_res,
-                             d.B, S, D, sc.g_res2, ada ? nullptr : g1, sc.lnpart[0][ada ? 0 : par], st);
+                             d.B, S, D, sc.g_res2, ada ? nullptr : g1, sc.lnpart[0][ada ? 0 : par], st, x2);
       }));
       if (ada) {   // dscale2 -> dmod[4D..5D), dshift2 -> dmod[3D..4D)
         ProfScope ps("reduce", 0, (double)d.B * nln * 2 * D * 4, st);
         SR_TRY(launch_reduce_cols(sc.lnpart[0][0], nln, d.B, 0, 2 * D, D, sc.dmod + 4 * D, sc.dmod + 3 * D, 6 * D,
                                   st));
       }
-      if (d.save8) {   // for the attention; the previous block's recomputed LN1 output reads hin
-        SR_TRY(join(kQkv + 1 - par));
-        SR_TRY(restore({q8_job(s.qkv, d.dtype, 3 * MD, s.k_qkv), q8_job(s.O, d.dtype, MD, s.k_O),
-                        q8_job(s.hin, kF32, MD, s.k_hin), q8_job(s.a_out, d.dtype, ada ? MD : 0, s.k_a)}));
-      }
       if (ada) {
         // attention-branch gradient da = dh1 * gate1 and dgate1 = sum_s dh1 * a_out
         SR_TRY(join(kO));   // g1 may still be read by the previous block's dW_o
+        if (d.save8) SR_TRY(restore({q8_job(s.a_out, d.dtype, MD, s.k_a)}));
         SR_TRY(gate_bwd(d, sc.g_res2, s.a_out, s.mod + 2 * D, g1, sc.dmod, 2 * D, sc, st));
       }
       // output projection: dWo, dbo; dO = da Wo (with the attention row statistic
@@ -708,6 +704,7 @@ hipError_t stack_bwd(const Dims& d, const sr_block_params* p, const void* cond, 
         }
         return weight_grad("gemm_dw_o", d, g1, D, s.O, D, g.w_o, g.b_o, sc, kWgO, &jobs[kWgO], ss);
       }));
+      if (d.save8) SR_TRY(restore({q8_job(s.qkv, d.dtype, 3 * MD, s.k_qkv), q8_job(s.O, d.dtype, MD, s.k_O)}));
       const bool fuse_delta = d.dtype == kBF16 && D / d.H == 64;
       {
         GemmDesc gd = desc(d, g1, true, D, (size_t)M * D * e, w.w_o, false, D, (size_t)D * D * e, M, D, D);
@@ -735,7 +732,7 @@ hipError_t stack_bwd(const Dims& d, const sr_block_params* p, const void* cond, 
         if (g.w_qkv || g.b_qkv) {   // u1 = LN1(h) recomputed from the saved statistics
           ProfScope ps("recompute", 0, (double)M * D * (4 + e), ss);
           SR_TRY(launch_ln_apply(d.dtype, s.hin, w.ln1_w, w.ln1_b, ada ? s.mod : nullptr, 0, M, S, D, s.mean1,
-                                 s.rstd1, sc.u_rc, ss));
+                                 s.rstd1, sc.u_rc, ss, x1));
         }
         SR_TRY(weight_grad("gemm_dw_qkv", d, dqkv, 3 * D, sc.u_rc, D, g.w_qkv, g.b_qkv, sc, kWgQkv, &jobs[kWgQkv],
                            ss));
@@ -756,7 +753,7 @@ hipError_t stack_bwd(const Dims& d, const sr_block_params* p, const void* cond, 
       SR_TRY(fork_point([&]() -> hipError_t {
         ProfScope ps("ln_bwd", 0, (double)M * D * (16 + e), st);
         return launch_ln_bwd(d.dtype, sc.du, s.hin, s.mean1, s.rstd1, w.ln1_w, ada ? s.mod : nullptr, 0, sc.g_res2,
-                             d.B, S, D, sc.g_res, ada ? nullptr : g0, sc.lnpart[ada ? 0 : 1][ada ? 0 : par], st);
+                             d.B, S, D, sc.g_res, ada ? nullptr : g0, sc.lnpart[ada ? 0 : 1][ada ? 0 : par], st, x1);
       }));
       if (ada) {   // dscale1 -> dmod[D..2D), dshift1 -> dmod[0..D)
         ProfScope ps("reduce", 0, (double)d.B * nln * 2 * D * 4, st);

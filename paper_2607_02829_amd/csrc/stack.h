@@ -16,11 +16,6 @@ struct Dims {
   bool save8 = false;   // SR_BLOCK_SAVE8
 };
 
-// An activation kept in 8 bits (SR_Q8_BLOCK).
-struct Kept8 {
-  int8_t* q = nullptr;
-  uint8_t* e = nullptr;
-};
 
 struct BlockSaved {
   float *hin, *mean1, *rstd1, *lse, *h1, *mean2, *rstd2, *mod;
