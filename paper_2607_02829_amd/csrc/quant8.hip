@@ -55,6 +55,26 @@ SR_DEV void store8(float* p, const float v[8]) {
   reinterpret_cast<f32x4*>(p)[1] = b;
 }
 
+// Largest value of each group of LPR (32 or 64) lanes, without LDS round trips (as wave_max).
+template <int CTRL>
+SR_DEV uint32_t dppu(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, false);
+}
+template <int LPR>
+SR_DEV uint32_t lanes_umax(uint32_t v) {
+  v = max(v, dppu<0xB1>(v));
+  v = max(v, dppu<0x4E>(v));
+  v = max(v, dppu<0x141>(v));
+  v = max(v, dppu<0x140>(v));
+  const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max((uint32_t)r[0], (uint32_t)r[1]);
+  if constexpr (LPR == 64) {
+    const auto h = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    v = max((uint32_t)h[0], (uint32_t)h[1]);
+  }
+  return v;
+}
+
 // Adding 1.5 2^23 to |v| < 2^22 rounds v to an integer (halves to even), whose two's complement
 // is then in the low bits of the sum.
 constexpr float kMagic = 12582912.0f;
@@ -150,8 +170,7 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const T* __restrict__ x
       top(v[0]);
     }
   }
-#pragma unroll
-  for (int o = (LPR < 64 ? LPR : 64) / 2; o >= 1; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+  m = lanes_umax<(LPR < 64 ? LPR : 64)>(m);
   if constexpr (LPR > 64) {
     __shared__ uint32_t red[LPR / 64];
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
@@ -235,8 +254,7 @@ __global__ __launch_bounds__(256) void ln_quant_kernel(const float* __restrict__
       }
     }
   }
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+  m = lanes_umax<64>(m);
   const bool ok = m < kInfBits;
   const float amax = __uint_as_float(m);
   if (lane == 0) scale[row] = ok ? __fdiv_rn(amax, 127.0f) : __uint_as_float(0x7FC00000u);
@@ -273,8 +291,8 @@ SR_DEV void quant_block8(const T* __restrict__ x, size_t i, int8_t* __restrict__
   uint32_t m = 0;
 #pragma unroll
   for (int j = 0; j < 8; ++j) m = max(m, abs_bits(v[j]));
-  m = max(m, (uint32_t)__shfl_xor((int)m, 1, 64));
-  m = max(m, (uint32_t)__shfl_xor((int)m, 2, 64));
+  m = max(m, dppu<0xB1>(m));   // the four lanes of a block: pairs, then quads
+  m = max(m, dppu<0x4E>(m));
   const uint32_t E = block_exponent(m);
   const float inv = __uint_as_float((254u - min(E, 253u)) << 23);   // 2^-e
 #pragma unroll
