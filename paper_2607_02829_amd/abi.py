@@ -156,12 +156,20 @@ def _nbytes(t):
     return t.numel() * t.element_size()
 
 
+_raw_stream = None   # address of the current device's current torch stream
+
+
 def _stream(stream):
     if stream is not None:
         return stream if isinstance(stream, int) else stream.cuda_stream
-    import torch
-    # the address alone: building the Stream object of torch.cuda.current_stream() costs 2.6 us
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    global _raw_stream
+    if _raw_stream is None:
+        import torch
+        torch.cuda.current_device()   # initialises the device on first use
+        get_device, get_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+        # the address alone: building the Stream object of torch.cuda.current_stream() costs 2.6 us a call
+        _raw_stream = lambda: get_stream(get_device())  # noqa: E731
+    return _raw_stream()
 
 
 def _check(status: int):
