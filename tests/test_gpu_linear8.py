@@ -164,3 +164,24 @@ def test_a_token_does_not_depend_on_its_batch():
     for lo, n in ((0, 1), (3, 7), (100, 33), (320, 130), (650, 50)):
         part = _run(n, N, K, "f32", (xq[lo:lo + n], xs[lo:lo + n], wq, ws, bias), 1, True)
         assert np.array_equal(part, whole[lo:lo + n]), (lo, n)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,N,K", [(2, 64, 128), (130, 72, 576), (600, 600, 192), (2100, 1032, 192), (4100, 3336, 1088)])
+def test_infinite_pre_activations(M, N, K, dtype):
+    # GELU(+Inf) = +Inf and GELU(-Inf) = 0, from an infinite bias and from scales whose product overflows
+    data = list(_data(M, N, K, dtype))
+    bias = storage_to_f64(data[4]).astype(np.float32)
+    bias[1], bias[N - 2] = np.inf, -np.inf
+    data[4] = inputs.to_storage(bias, dtype)
+    data[1], data[3] = data[1].copy(), data[3].copy()
+    data[1][0], data[3][2] = 1e25, 1e20
+    data[0][0], data[2][2], data[2][N - 3] = 100, 100, -100   # sums of one sign in row 0
+    data[3][N - 3] = 1e20
+    clean = [1, 2, N - 3, N - 2]
+    for act in (0, 1):
+        y = storage_to_f64(_run(M, N, K, dtype, tuple(data), act, True))
+        low = 0.0 if act else -np.inf
+        assert (y[:, 1] == np.inf).all() and (y[:, N - 2] == low).all()
+        assert y[0, 2] == np.inf and y[0, N - 3] == low
+        assert np.isfinite(np.delete(y[1:], clean, axis=1)).all()
