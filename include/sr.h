@@ -385,8 +385,8 @@ typedef enum { SR_ACT_NONE = 0, SR_ACT_GELU = 1 } sr_act;
 SR_API sr_status sr_quantize8(int32_t q8_kind, int32_t dtype, int32_t M, int32_t N, const void* x, int8_t* q,
                        void* scale, void* stream);
 
-/* The values that q and scale stand for -> x [M,N] storage type (SR_Q8_ROW: one rounding to it;
- * SR_Q8_BLOCK: exact).  Sizes as above. */
+/* The values that q and scale stand for -> x [M,N] storage type (SR_Q8_ROW: q * scale in
+ * fp32, then rounded to it; SR_Q8_BLOCK: exact).  Sizes as above. */
 SR_API sr_status sr_dequantize8(int32_t q8_kind, int32_t dtype, int32_t M, int32_t N, const int8_t* q,
                          const void* scale, void* x, void* stream);
 
@@ -394,7 +394,8 @@ SR_API sr_status sr_dequantize8(int32_t q8_kind, int32_t dtype, int32_t M, int32
  *   y[m,n] = act( xs[m] ws[n] sum_k xq[m,k] wq[n,k] + bias[n] )
  * with an exact int32 sum, the rest in fp32 and one rounding to the storage type.
  *   xq [M,K], xs [M]: the tokens;  wq [N,K], ws [N]: the weight;  bias [N] storage type or NULL;
- *   y [M,N] storage type out;  act: sr_act (the exact GELU).
+ *   y [M,N] storage type out;  act: sr_act (the exact GELU; its limits at the
+ * infinities).
  * M >= 1, N % 8 == 0, K % 64 == 0, K <= 65536; M*K, N*K and M*N*elt < 2^31 bytes. */
 SR_API sr_status sr_linear8(int32_t dtype, int32_t act, int32_t M, int32_t N, int32_t K, const int8_t* xq,
                      const float* xs, const int8_t* wq, const float* ws, const void* bias, void* y,
@@ -403,8 +404,8 @@ SR_API sr_status sr_linear8(int32_t dtype, int32_t act, int32_t M, int32_t N, in
 /* Weight and bias gradient of a linear layer from the SR_Q8_BLOCK checkpoint of its input:
  *   dw[n,k] = sum_m dy[m,n] xhat[m,k],   db[n] = sum_m dy[m,n]
  *   dy [M,N] storage type;  xq [M,K], xe [M,K/32]: the checkpoint, read in 8 bits;
- *   dw [N,K] fp32 and db [N] fp32 (or NULL), overwritten.  Every product is exact and sums are fp32,
- *   in a fixed order (deterministic).  scratch: sr_weight_grad8_scratch_bytes bytes (NULL when 0).
+ *   dw [N,K] fp32 and db [N] fp32 (or NULL), overwritten.  Every product is exact (but for the bits
+ *   of an fp32 dy below 2^-133) and sums are fp32, in a fixed order (deterministic).  scratch: sr_weight_grad8_scratch_bytes bytes (NULL when 0).
  * M >= 1, N % 8 == 0, K % 64 == 0, K <= 65536; M*N*elt, M*K and N*K*4 < 2^31 bytes. */
 SR_API sr_status sr_weight_grad8_scratch_bytes(int32_t dtype, int32_t M, int32_t N, int32_t K,
                                         size_t* scratch_bytes);

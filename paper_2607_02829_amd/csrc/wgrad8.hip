@@ -3,8 +3,8 @@
 //
 // xhat is exact in bf16, so bf16 gradients take one product of v_mfma_f32_32x32x16_bf16 per term, exact before
 // the fp32 sum.  fp32 gradients are cut into three bf16 parts of eight significant bits each, dy = hi + mid + lo
-// without a remainder, and take three products per term: a third of the bf16 rate, which is five times
-// that of the fp32 matrix instructions.
+// without a remainder (of values under 2^-117 the bits below 2^-133 are left out), and take three products per term: a
+// third of the bf16 rate, which is five times that of the fp32 matrix instructions.
 //
 // Both operands are token-major and the sum runs over tokens.  A workgroup takes 64 tokens at a time: each
 // thread loads 16-byte pieces of dy and of the codes into registers, two tiles ahead, turns codes (and fp32
@@ -67,12 +67,16 @@ struct Grad8<float> {
     raw[1] = buf_load16(r, off + 16);
   }
   SR_DEV float at(int j) const { return __int_as_float(raw[j >> 2][j & 3]); }
-  // truncation leaves an exact remainder of the bits below: 24 = 8 + 8 + 8
+  // truncation leaves an exact remainder of the bits below, 24 = 8 + 8 + 8; none of an infinity, which would be NaN
+  SR_DEV static float rest(float v) {
+    const float t = truncated(v);
+    return v == t ? 0.f : v - t;
+  }
   SR_DEV void parts(i32x4 p[P]) const {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const float a = at(2 * j), b = at(2 * j + 1);
-      const float ra = a - truncated(a), rb = b - truncated(b);
+      const float ra = rest(a), rb = rest(b);
       p[0][j] = (int)upper2(a, b);
       p[1][j] = (int)upper2(ra, rb);
       p[2][j] = (int)upper2(ra - truncated(ra), rb - truncated(rb));

@@ -193,3 +193,20 @@ def test_the_gradient_of_a_layer_equals_differences():
     got = float((t["dw"].double().cpu().numpy() * V).sum() + (t["db"].double().cpu().numpy() * u).sum())
     scale = float((np.abs(t["dw"].double().cpu().numpy()) * np.abs(V)).sum())
     assert abs(num - got) <= 1e-6 * scale
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_infinite_gradients_keep_their_sign(dtype):
+    M, N, K = 70, 64, 128
+    dy, xq, xe = _data(M, N, K, dtype)
+    f = storage_to_f64(dy).astype(np.float32)
+    f[69, 5], f[7, 9] = np.inf, -np.inf
+    xq = xq.copy()
+    xq[69, ::3] = 0
+    dw, db = _run(M, N, K, dtype, (inputs.to_storage(f, dtype), xq, xe))
+    with np.errstate(invalid="ignore"):
+        for n, m, v in ((5, 69, np.inf), (9, 7, -np.inf)):   # 0 times Inf is NaN
+            assert np.array_equal(dw[n], (v * np.sign(xq[m].astype(np.float64))).astype(np.float32), equal_nan=True)
+            assert db[n] == v
+    keep = np.setdiff1d(np.arange(N), [5, 9])
+    assert np.isfinite(dw[keep]).all() and np.isfinite(db[keep]).all()
