@@ -71,13 +71,20 @@ class DeviceParams8:
             for name in self.LINEAR:
                 w = p[name]
                 q = torch.empty(w.shape, dtype=torch.int8, device=w.device)
-                s = torch.empty(w.shape[0], dtype=torch.float32, device=w.device)
-                abi.sr_quantize8(abi.SR_Q8_ROW, abi.SR_BF16 if w.dtype == torch.bfloat16 else abi.SR_F32,
-                                 w.shape[0], w.shape[1], w, q, s)
-                t[name], t["s" + name[1:]] = q, s
+                t[name], t["s" + name[1:]] = q, torch.empty(w.shape[0], dtype=torch.float32, device=w.device)
             self.tensors.append(t)
             for name in abi.PARAM8_FIELDS:
                 setattr(self.array[i], name, t[name].data_ptr() if name in t else getattr(src.array[i], name))
+        self.quantize()
+
+    def quantize(self):
+        """The codes and scales of the weights' present values, into the same tensors."""
+        import torch
+        for p, t in zip(self.src.tensors, self.tensors):
+            for name in self.LINEAR:
+                w = p[name]
+                abi.sr_quantize8(abi.SR_Q8_ROW, abi.SR_BF16 if w.dtype == torch.bfloat16 else abi.SR_F32,
+                                 w.shape[0], w.shape[1], w, t[name], t["s" + name[1:]])
 
 
 class DeviceGrads:

@@ -87,6 +87,7 @@ class Trunk:
             for c in self.cfg:
                 c.kind |= abi.SR_BLOCK_SAVE8
         self.params8 = None
+        self.overwritten = False   # by a forecast, since the last forward
         bounds = (0, n1, n1 + n2, n1 + n2 + n3)
         self.params = [device.DeviceParams(params_storage[bounds[i]:bounds[i + 1]], w.kind) for i in range(3)]
         self.grads = [device.DeviceGrads(w, n, skip_unused=True) for n in split]
@@ -118,6 +119,7 @@ class Trunk:
         a, (ce, cm, cl), (pe, pm, pl) = abi, self.cfg, self.params
         K = self.K
         self.x0 = x0
+        self.overwritten = False
         a.sr_dense_blocks_fwd(ce, pe.array, None, x0, self.x1, self.saved[0], self.scratch)
         if self.select == "attn":
             a.sr_attention_colsums(ce, self.w.L, self.saved[0], self.split[0] - 1, self.colsum)
@@ -133,6 +135,8 @@ class Trunk:
     def backward(self, g3):
         """g3: (B, L, D) storage gradient of the trunk output (not modified).  Returns the
         input gradient g0; the parameter gradients are in ``self.grads`` (early, middle, late)."""
+        if self.overwritten:
+            raise RuntimeError("a forecast has overwritten the forward's buffers: run forward again")
         a, (ce, cm, cl), (pe, pm, pl) = abi, self.cfg, self.params
         ge, gm, gl = (g.array for g in self.grads)
         K, ck = self.K, self.checkpoint
@@ -153,10 +157,14 @@ class Trunk:
         return self.g0
 
     def quantize(self):
-        """Take the linear weights into 8 bits for ``forecast`` (again after they change)."""
+        """Take the linear weights into 8 bits for ``forecast``; again, into the same tensors, after they change."""
         import torch
         if self.select == "attn":
             raise ValueError("the attention-score selector needs the early stage's saved activations")
+        if self.params8 is not None:
+            for p in self.params8:
+                p.quantize()
+            return
         self.params8 = [device.DeviceParams8(p) for p in self.params]
         n = max(abi.sr_blocks8_scratch_bytes(c, s) for c, s in zip(self.cfg, (self.w.L, self.K, self.w.L)))
         self.scratch8 = torch.empty(n, dtype=torch.uint8, device="cuda")
@@ -164,11 +172,12 @@ class Trunk:
     def forecast(self, x0, step: int):
         """The forward with weights and tokens in 8 bits (``quantize`` first), keeping nothing for a
         backward: x0 (B, L, D) storage tensor, not modified.  Returns the trunk output x3; an earlier
-        ``forward``'s buffers (x1, x3, idx, h0, h) are overwritten."""
+        ``forward``'s buffers (x1, x3, idx, h0, h) are overwritten, and with them its ``backward``."""
         if self.params8 is None:
             raise RuntimeError("forecast needs quantize() first")
         a, (ce, cm, cl), (pe, pm, pl) = abi, self.cfg, self.params8
         K, L = self.K, self.w.L
+        self.overwritten = True
         a.sr_blocks8_fwd(ce, L, pe.array, None, x0, self.x1, self.scratch8)
         a.sr_select_indices(cm, K, a.SR_SEL_RANDOM, self.seed, step, None, None, self.idx)
         a.sr_gather(cm, K, self.x1, self.idx, self.h0)

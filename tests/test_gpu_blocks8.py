@@ -102,3 +102,48 @@ def test_forecast_follows_the_forward(w, split):
         assert torch.equal(tr.x3.view(torch.int16), y.view(torch.int16)), rep
         tr.forward(x0, 4)
         torch.cuda.synchronize()
+
+
+def test_forecast_between_forward_and_backward_is_refused():
+    import torch
+    w, split = inputs.small("b8_s", Hg=10, Wg=21), (1, 1, 1)
+    params = inputs.params_to_storage(inputs.block_params(w, 3, randomise_affine=True), w.dtype)
+    x0, g3 = (device.to_device(inputs.to_storage(f(w), w.dtype)) for f in (inputs.token_field, inputs.upstream_grad))
+    tr = Trunk(w, split, params, seed=7)
+    tr.forward(x0, 3)
+    g0 = tr.backward(g3).clone()
+    tr.quantize()
+    tr.forward(x0, 3)
+    tr.forecast(x0, 4)   # other indices, in the buffers that the backward reads
+    with pytest.raises(RuntimeError):
+        tr.backward(g3)
+    tr.forward(x0, 3)
+    assert torch.equal(tr.backward(g3).view(torch.int16), g0.view(torch.int16))
+
+
+def test_new_weights_reach_a_captured_forecast():
+    import torch
+    w, split = inputs.small("b8_q", Hg=10, Wg=21), (1, 1, 1)
+    params = inputs.params_to_storage(inputs.block_params(w, 3, randomise_affine=True), w.dtype)
+    x0 = device.to_device(inputs.to_storage(inputs.token_field(w), w.dtype))
+    tr = Trunk(w, split, params, seed=7)
+    tr.quantize()
+    tr.forecast(x0, 3)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        tr.forecast(x0, 3)
+    for p in tr.params:
+        for t in p.tensors:
+            t["w_fc2"].mul_(2.0)
+    held = [(t["w_fc2"].data_ptr(), t["s_fc2"].data_ptr()) for p in tr.params8 for t in p.tensors]
+    tr.quantize()   # into the same tensors
+    assert held == [(t["w_fc2"].data_ptr(), t["s_fc2"].data_ptr()) for p in tr.params8 for t in p.tensors]
+    want = tr.forecast(x0, 3).clone()
+    torch.cuda.synchronize()
+    for rep in range(2):
+        tr.x3.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(tr.x3.view(torch.int16), want.view(torch.int16)), rep
