@@ -217,14 +217,14 @@ size_t scratch_bytes(const Dims& d) {
   return most;
 }
 
-// Planes of a split attention forward, in buffers of the block that are written only after it: h1, z
-// and GELU(z), the maxima and denominators over u1 (read only before).  Returns the number of runs.
 static Q8Job q8_job(const void* x, int dtype, size_t n, const Kept8& k) {
   Q8Job j;
   j.x = const_cast<void*>(x); j.dtype = dtype; j.n = n; j.q = k.q; j.e = k.e;
   return j;
 }
 
+// Planes of a split attention forward, in buffers of the block that are written only after it: h1, z
+// and GELU(z), the maxima and denominators over u1 (read only before).  Returns the number of runs.
 static int fwd_attn_part(const Dims& d, const BlockSaved& s, AttnPart* part) {
   const size_t plane = (size_t)d.M * d.D, act = (size_t)d.M * d.F * d.elt / 4 / plane * plane;
   int n = 0;

@@ -16,7 +16,6 @@ struct Dims {
   bool save8 = false;   // SR_BLOCK_SAVE8
 };
 
-
 struct BlockSaved {
   float *hin, *mean1, *rstd1, *lse, *h1, *mean2, *rstd2, *mod;
   void *u1, *qkv, *O, *u2, *z, *gz, *a_out, *m_out;
