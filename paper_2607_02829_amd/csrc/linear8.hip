@@ -415,7 +415,8 @@ hipError_t run_few(const Linear8& a, hipStream_t st) {
 template <int ACT, typename T>
 hipError_t run_shape(int shape, const Linear8& a, hipStream_t st) {
   switch (shape) {
-    case kFew16: return run_few<16, 4, ACT, T>(a, st);
+    case kFew16:   // longer rows on more waves (1 x 1024 x 8192 7.2 -> 6.5 us; x 4096 4.6, 4.4; x 2048 3.4, 3.8)
+      return a.K > 2048 ? run_few<16, 8, ACT, T>(a, st) : run_few<16, 4, ACT, T>(a, st);
     case k32x32g8: return run_tile<32, 32, 64, 1, 1, 8, 4, 1, ACT, T>(a, st);
     case k64x64g2:
       // longer rows in whole lines (512 x 1024 x 4096 12.0 -> 10.8 us; 1024 x 512 x 2048 6.9, 7.7)
@@ -435,10 +436,11 @@ hipError_t run_shape(int shape, const Linear8& a, hipStream_t st) {
 // The smallest tile whose grid is one round of workgroups on the 256 CUs; past one round of 128 x 128 those, two
 // workgroups per CU (one's epilogue under the other's products), or with long rows 256 x 256, once its own grid is most
 // of a round.  us, bf16, M x N x K:
-//   fragments straight from memory, up to one 16 x 16 tile per CU and K <= 1024 (or as much work in more, shorter
-//   tiles):  1 x 4096 x 1024 4.0 (32 x 32 in eight groups 4.9), 64 x 1024 x 1024 4.5 (5.1), 2048 x 64 x 64 3.5
-//   (64 x 64 4.4);  past it 128 x 1024 x 1024 5.5 (5.2), 1 x 1024 x 4096 6.3 (6.1)
-//   32 x 32, eight groups of waves:  128 x 1024 x 4096 6.9 (64 x 64 8.1);  K = 256 4.9 (4.6)
+//   fragments straight from memory, up to one 16 x 16 tile per CU, of long rows with few tokens (or as much work in
+//   more, shorter tiles):  1 x 4096 x 1024 3.3 (32 x 32 in eight groups 4.0), 64 x 1024 x 1024 3.2 (3.8), 1 x 1024 x 4096
+//   4.4 (5.6), 16 x 4096 x 4096 7.2 (8.7), 64 x 1024 x 8192 9.4 (10.2), 128 x 1536 x 64 2.5 (64 x 64 3.3);  past it
+//   100 x 1024 x 1024 4.2 (3.8), 128 x 1024 x 4096 9.2 (6.7), 100 x 512 x 8192 9.2 (8.6)
+//   32 x 32, eight groups of waves:  128 x 1024 x 4096 6.7 (64 x 64 9.1);  x 256 3.6 (3.4)
 //   64 x 64, two groups:  1024 x 1024 x 1024 6.2 (64 x 128 7.3);  64 x 128:  2048 x 1024 x 1024 7.7 (8.7, 128 x 128 9.7)
 //   128 x 128, four stages, one workgroup per CU:  4050 x 1024 x 4096 22.9 (two 26.1);  with shorter rows two
 //   workgroups are level or ahead: 4050 x 1024 x 1024 10.9 (10.5), 16200 x 256 x 1024 12.3 (14.4)
@@ -451,7 +453,7 @@ hipError_t run_shape(int shape, const Linear8& a, hipStream_t st) {
 int pick_shape(const Linear8& a) {
   auto tiles = [&](int bm, int bn) { return (long)((a.M + bm - 1) / bm) * ((a.N + bn - 1) / bn); };
   const long t16 = tiles(16, 16);
-  if (a.K <= 1024 && (t16 <= 256 || t16 * a.K <= 1 << 17)) return kFew16;
+  if ((t16 <= 256 && (a.K <= 4096 || a.M <= 64)) || (a.K <= 1024 && t16 * a.K <= 1 << 17)) return kFew16;
   if (a.K >= 512 && tiles(32, 32) <= 256) return k32x32g8;
   if (tiles(64, 64) <= 256) return k64x64g2;
   if (tiles(64, 128) <= 256) return k64x128;

@@ -185,3 +185,11 @@ def test_infinite_pre_activations(M, N, K, dtype):
         assert (y[:, 1] == np.inf).all() and (y[:, N - 2] == low).all()
         assert y[0, 2] == np.inf and y[0, N - 3] == low
         assert np.isfinite(np.delete(y[1:], clean, axis=1)).all()
+
+
+@pytest.mark.parametrize("dtype,act", [("bf16", 0), ("bf16", 1), ("f32", 1)])
+@pytest.mark.parametrize("M,N,K", [(1, 1024, 4096), (16, 4096, 4096), (17, 2040, 2112), (64, 1024, 8192), (70, 808, 4160),
+                                   (256, 256, 4096), (60, 8, 65536)])
+def test_linear_on_few_tokens_of_long_rows(M, N, K, dtype, act):
+    data = _data(M, N, K, dtype, seed=2)
+    _check(_run(M, N, K, dtype, data, act, True), M, N, K, dtype, data, act, True)
