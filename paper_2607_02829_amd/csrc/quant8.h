@@ -71,7 +71,7 @@ struct Wgrad8 {
   const uint8_t* xe = nullptr;
   float *dw = nullptr, *db = nullptr, *scratch = nullptr;
 };
-size_t wgrad8_scratch(int dtype, int M, int N, int K);   // bytes; not less for more of M
+size_t wgrad8_scratch(int dtype, int M, int N, int K);   // bytes; with N = K not less for more of M
 hipError_t launch_wgrad8(int dtype, const Wgrad8& a, hipStream_t st);
 
 }  // namespace sr

@@ -290,32 +290,60 @@ __global__ __launch_bounds__(64) void wgrad8_sum_kernel(const float* __restrict_
   (w ? reinterpret_cast<f32x4*>(dw)[i] : reinterpret_cast<f32x4*>(db)[i - n4]) = s;
 }
 
-// Tile of dw and runs over tokens.  us on bf16 for M x N x K (tokens, rows and columns of dw), /runs:
-//   64 x 64 on four waves, runs up to a round of workgroups and of at least 256 tokens:  512 x 1024 x 1024 /1 8.5 (128 x
-//     128 10.6, /2 13.9), 2048 x 512 x 2048 /1 19.7 (/2 21.4; 128 x 128 /4 23.9), 1024 x 256 x 256 /4 8.7 (/1 10.9),
-//     16200 x 256 x 256 /16 16.8 (/8 21.3, /32 18.1; 128 x 128 20.2)
-//   128 x 128 on eight waves, where they fill half a round by themselves or many tokens fill it in runs:
-//     1024 x 1024 x 4096 /1 19.3 (64 x 64 26), 4050 x 1024 x 1024 /4 25.3 (64 x 64 /2 27.4), 16200 x 256 x 1024 /16
-//     23.8 (64 x 64 /8 27.2);  four waves of 64 x 64 each are behind: 22.7, 26.7, -
-//   256 x 128, over many tokens:  16200 x 1024 x 4096 /2 157 (128 x 128 /1 182), 16200 x 1024 x 1024 /8 51 (/4 56),
-//     8192 x 1024 x 1024 /8 35 (34);  128 x 256 has twice the codes to decode per thread: 161, 54
-// The scratch for more tokens is never less: every step above raises the planes' number.
+// Tile of dw and runs over tokens, by the size of dw in tiles of 128 x 128 (u) and the tokens.  us on bf16 for M x N x K
+// (tokens, rows and columns of dw), /runs:
+//   64 x 64 on four waves, two workgroups per CU, for a small dw or few tokens:  1024 x 256 x 256 /4 7.5 (/1 9.7,
+//     128 x 128 8.8), 1024 x 2048 x 1024 /1 12.8 (14.5), 4096 x 1024 x 512 /4 18.7 (/2 20.6; 19.9).  Runs fill one round
+//     of workgroups, or two over many tokens.
+//   128 x 128 on eight waves:  4096 x 1024 x 1024 /4 23.5 (64 x 64 /2 25.2), 2048 x 1024 x 4096 /1 26.9 (38; 256 x 128 33),
+//     4096 x 2048 x 1024 /2 32 (36);  four waves of 64 x 64 each are behind.  fp32 gradients, three products a term, reach
+//     it with fewer tokens: 3000 x 1024 x 1024 /4 31 (64 x 64 /1 42).
+//   256 x 128 where it costs less:  16200 x 1024 x 4096 /2 147 (169), 2048 x 4096 x 2048 /1 41 (46), 16200 x 1536 x 1024 /5
+//     65 (77);  128 x 256 has twice the codes to decode per thread
+// Of the larger tiles n runs cost rounds of workgroups x tokens of a run x what a workgroup takes for a token, and, where
+// the sum is cut, a launch and the planes' way through the caches; 2 us more for 256 x 128's first and last tiles.  Over
+// 300 sizes and types what this takes is 0.2 % behind the fastest on average.  Runs are of at least 256 tokens (fp32: 128).
+// More tokens take more runs (their factor falls with n, the rest grows) and larger tiles, so for a square dw the scratch
+// for more tokens is never less.
 enum Shape { k64x64, k128x128, k256x128 };
 struct Plan {
   int shape, splits, per_split, tiles_n, tiles_k;
 };
 Plan plan(int dtype, int M, int N, int K) {
-  auto tiles = [&](int bn, int bk) { return ((N + bn - 1) / bn) * (long)((K + bk - 1) / bk); };
-  const long t128 = tiles(128, 128);
+  const long u = (long)N * K >> 14;
+  const bool bf = dtype == kBF16;
+  const long most = std::min(bf ? (M >= 768 ? M / 256 : 1l) : (M >= 512 ? M / 128 : 1l), 32l);   // runs
+  auto tiled = [&](int shape, int bn, int bk) {
+    Plan p;
+    p.shape = shape;
+    p.tiles_n = (N + bn - 1) / bn;
+    p.tiles_k = (K + bk - 1) / bk;
+    p.splits = 1;
+    return p;
+  };
+  // the runs that cost least, token us per token of a workgroup; returns the cost
+  auto cut = [&](Plan& p, double token) {
+    const long t = (long)p.tiles_n * p.tiles_k;
+    double best = 0;
+    for (long n = 1; n <= most; ++n) {
+      const double us = (double)((t * n + 255) / 256) * M / n * token + (n > 1 ? 4 + 0.8e-6 * n * N * K : 0);
+      if (n == 1 || us < best) best = us, p.splits = (int)n;
+    }
+    return best;
+  };
   Plan p;
-  if (dtype == kBF16 && M >= 8192 && tiles(256, 128) >= 32) p.shape = k256x128;
-  else if (t128 >= 128 || (t128 >= 32 && M >= 4096) || (t128 >= 16 && M >= 8192)) p.shape = k128x128;
-  else p.shape = k64x64;
-  const int bn = p.shape == k64x64 ? 64 : p.shape == k128x128 ? 128 : 256, bk = p.shape == k64x64 ? 64 : 128;
-  p.tiles_n = (N + bn - 1) / bn;
-  p.tiles_k = (K + bk - 1) / bk;
-  const long t = (long)p.tiles_n * p.tiles_k;
-  p.splits = (int)std::max(1l, std::min({256 / t, (long)M / 256, 32l}));
+  if (std::min(N, K) > 64 && (u > 128 || (bf ? M >= 2560 && u * M >= 224 << 10 : M >= 1408 && u * M >= 72 << 10))) {
+    p = tiled(k128x128, 128, 128);
+    const double us = cut(p, bf ? 0.0105 : 0.025);
+    if (bf) {
+      Plan w = tiled(k256x128, 256, 128);
+      if (cut(w, 0.0155) + 2 < us) p = w;
+    }
+  } else {
+    p = tiled(k64x64, 64, 64);
+    const long t = (long)p.tiles_n * p.tiles_k;
+    p.splits = (int)std::max(1l, std::min((M >= 2560 && t * M >= 384 << 10 ? 512 : 256) / t, most));
+  }
   p.per_split = ((M + p.splits - 1) / p.splits + TM - 1) / TM * TM;
   return p;
 }

@@ -210,3 +210,13 @@ def test_infinite_gradients_keep_their_sign(dtype):
             assert db[n] == v
     keep = np.setdiff1d(np.arange(N), [5, 9])
     assert np.isfinite(dw[keep]).all() and np.isfinite(db[keep]).all()
+
+
+@pytest.mark.parametrize("dtype,M,N,K", [
+    # each tile with runs of uneven length, one run, and more than a round of workgroups
+    ("bf16", 700, 264, 448), ("bf16", 2500, 1032, 448), ("bf16", 4500, 1000, 1088), ("bf16", 2003, 1544, 2112),
+    ("bf16", 3001, 4104, 1536), ("bf16", 5101, 1544, 1088), ("bf16", 8195, 776, 2816), ("bf16", 100, 4096, 2048),
+    ("f32", 515, 264, 192), ("f32", 2100, 1000, 832), ("f32", 1501, 776, 2816), ("f32", 8195, 776, 2816),
+    ("f32", 16200, 512, 512)])
+def test_weight_grad_on_every_tile_and_run(dtype, M, N, K):
+    test_weight_grad_over_many_tokens(dtype, M, N, K)

@@ -212,3 +212,12 @@ def test_blocks8_refusals():
                 assert got == (status if used else abi.SR_EWORKSPACE), (kind, name)
     assert L.sr_blocks8_fwd(ctypes.byref(c), 25, p, None, FAKE, FAKE, FAKE, need, None) != abi.SR_OK   # adaLN without cond
     assert L.sr_blocks8_fwd(ctypes.byref(_cfg()), 25, None, None, FAKE, FAKE, FAKE, need, None) == abi.SR_EINVAL
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_weight_grad_scratch_grows_with_the_tokens(dtype):
+    _lib()
+    for D in (64, 192, 320, 512, 768, 1024, 1152, 1536, 2048):
+        sizes = [abi.sr_weight_grad8_scratch_bytes(dtype, M, D, D) for M in range(1, 100000, 97)
+                 if M * D * (4 if dtype == F32 else 2) < 1 << 31]
+        assert sizes == sorted(sizes), D
