@@ -88,29 +88,33 @@ struct Grad8<float> {
   }
 };
 
-// BN x BK tile of dw on WN x WK waves.
-template <typename T, int BN, int BK, int WN, int WK, int OCC>
-__global__ __launch_bounds__(64 * WN * WK, OCC) void wgrad8_kernel(Wgrad8 a, int tiles_n, int tiles_k, int per_split) {
+// BN x BK tile of dw on KG groups of WN x WK waves, each with a part of the run's tokens and LDS stages of its own;
+// the groups' sums meet in LDS.
+template <typename T, int BN, int BK, int WN, int WK, int KG, int OCC>
+__global__ __launch_bounds__(64 * WN * WK * KG, OCC) void wgrad8_kernel(Wgrad8 a, int tiles_n, int tiles_k, int per_split) {
   constexpr int NT = 64 * WN * WK, P = Grad8<T>::P;
   constexpr int NI = BN / (32 * WN), KJ = BK / (32 * WK);
   constexpr int STAGE = TM * (P * BN + BK);                        // bf16 elements: the parts of dy, then xhat
   constexpr int GR = NT / (BN / 8), GL = TM / GR;                  // dy: rows per round of loads, rounds
   constexpr int XR = NT / (BK / 16), XL = TM / XR;                 // codes
   static_assert(GL * GR == TM && XL * XR == TM, "whole rounds of loads");
-  __shared__ __attribute__((aligned(1024))) bf16_t smem[2 * STAGE];
-  const int lane = threadIdx.x & 63, wave = wave_index(), h = lane >> 5;
+  __shared__ __attribute__((aligned(1024))) bf16_t smem[KG * 2 * STAGE];
+  const int grp = KG == 1 ? 0 : wave_index() / (WN * WK), wave = KG == 1 ? wave_index() : wave_index() % (WN * WK);
+  const int tid = KG == 1 ? (int)threadIdx.x : (int)threadIdx.x % NT, lane = threadIdx.x & 63, h = lane >> 5;
   const int wn = wave / WK, wk = wave % WK;
+  bf16_t* const stages = smem + grp * 2 * STAGE;
   int tn, tk, split;
   tile_coords(blockIdx.x, gridDim.x, tiles_n, tiles_k, tn, tk, split);
-  const int n0 = tn * BN, k0 = tk * BK, mbeg = split * per_split, mend = min(a.M, mbeg + per_split);
-  const int ntile = mbeg < mend ? (mend - mbeg + TM - 1) / TM : 0;
+  const int n0 = tn * BN, k0 = tk * BK, mrun = split * per_split, mend = min(a.M, mrun + per_split);
+  const int ntile = mrun < mend ? (mend - mrun + KG * TM - 1) / (KG * TM) : 0;   // per group; past the last token zeros
+  const int mbeg = mrun + grp * ntile * TM;
   const __amdgpu_buffer_rsrc_t ry = make_rsrc(a.dy, (uint32_t)((size_t)a.M * a.N * sizeof(T)));
   const __amdgpu_buffer_rsrc_t rx = make_rsrc(a.xq, (uint32_t)((size_t)a.M * a.K));
   const __amdgpu_buffer_rsrc_t re = make_rsrc(a.xe, (uint32_t)((size_t)a.M * (a.K / kQBlock)));
 
   // this thread's pieces: dy chunk gc of rows gr + i GR, codes 16 xc .. of rows xr + i XR
-  const int gc = threadIdx.x % (BN / 8), gr = threadIdx.x / (BN / 8);
-  const int xc = threadIdx.x % (BK / 16), xr = threadIdx.x / (BK / 16);
+  const int gc = tid % (BN / 8), gr = tid / (BN / 8);
+  const int xc = tid % (BK / 16), xr = tid / (BK / 16);
   const bool gin = n0 + gc * 8 < a.N, xin = k0 + xc * 16 < a.K;
   // pieces of a tile: GL of dy, then XL of codes, which are written in two halves; two tiles of them in flight
   constexpr int NP = GL + XL, NWR = GL + 2 * XL;
@@ -190,15 +194,15 @@ __global__ __launch_bounds__(64 * WN * WK, OCC) void wgrad8_kernel(Wgrad8 a, int
 
   static_for<NP>([&](auto p) { load(IC<0>{}, p); });
   static_for<NP>([&](auto p) { load(IC<1>{}, p); });
-  static_for<NWR>([&](auto w) { write(IC<0>{}, w, smem, true); });
+  static_for<NWR>([&](auto w) { write(IC<0>{}, w, stages, true); });
   static_for<NP>([&](auto p) { load(IC<0>{}, p); });
   // tile t, whose stage has parity S: its products, with the pieces of tile t + 1 written and those of t + 3
   // fetched in between
   constexpr int KS = TM / 16;
   auto body = [&](int t, auto sidx) {
     constexpr int S = decltype(sidx)::value;
-    const bf16_t* st = smem + S * STAGE;
-    bf16_t* next = smem + (1 - S) * STAGE;
+    const bf16_t* st = stages + S * STAGE;
+    bf16_t* next = stages + (1 - S) * STAGE;
     __syncthreads();   // tile t is written, and every wave is done with the other stage
     // fragments of k-step ks: the KJ of xhat, then the NI of each part of dy
     bf16x8 fx[2][KJ], fg[2][P * NI];
@@ -240,6 +244,31 @@ __global__ __launch_bounds__(64 * WN * WK, OCC) void wgrad8_kernel(Wgrad8 a, int
   }
   if (t < ntile) body(t, IC<0>{});
 
+  if constexpr (KG > 1) {   // the groups' sums, in order
+    float* red = reinterpret_cast<float*>(smem);
+    constexpr int TILE = NI * KJ * 16 * NT;
+    static_assert(TILE * 4 * (KG - 1) <= (int)sizeof(smem), "sums fit the stages");
+    __syncthreads();
+    if (grp > 0) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < KJ; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) red[(grp - 1) * TILE + ((i * KJ + j) * 16 + r) * NT + tid] = acc[i][j][r];
+    }
+    __syncthreads();
+    if (grp == 0) {
+#pragma unroll
+      for (int g = 0; g < KG - 1; ++g)
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+          for (int j = 0; j < KJ; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] += red[g * TILE + ((i * KJ + j) * 16 + r) * NT + tid];
+    }
+  }
   const bool cut = per_split < a.M;
   float* dw = cut ? a.scratch + (size_t)split * a.N * a.K : a.dw;
 #pragma unroll
@@ -247,6 +276,7 @@ __global__ __launch_bounds__(64 * WN * WK, OCC) void wgrad8_kernel(Wgrad8 a, int
 #pragma unroll
     for (int j = 0; j < KJ; ++j) {
       const int k = k0 + wk * (BK / WK) + 32 * j + (lane & 31);
+      if (grp > 0) break;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {   // register r: row 8 (r/4) + 4 h + r%4
         const int n = n0 + wn * (BN / WN) + 32 * i + 8 * (r >> 2) + 4 * h + (r & 3);
@@ -255,13 +285,13 @@ __global__ __launch_bounds__(64 * WN * WK, OCC) void wgrad8_kernel(Wgrad8 a, int
     }
   if (want_db) {   // the threads of one chunk, in row order
     __syncthreads();
-    float* red = reinterpret_cast<float*>(smem);   // [GR][BN]
+    float* red = reinterpret_cast<float*>(smem);   // [KG * GR][BN]
 #pragma unroll
-    for (int e = 0; e < 8; ++e) red[gr * BN + gc * 8 + e] = dbv[e];
+    for (int e = 0; e < 8; ++e) red[(grp * GR + gr) * BN + gc * 8 + e] = dbv[e];
     __syncthreads();
-    for (int c = threadIdx.x; c < BN; c += NT) {
+    for (int c = threadIdx.x; c < BN; c += KG * NT) {
       float s = 0.f;
-      for (int r = 0; r < GR; ++r) s += red[r * BN + c];
+      for (int r = 0; r < KG * GR; ++r) s += red[r * BN + c];
       const int n = n0 + c;
       if (n < a.N) (cut ? a.scratch + (size_t)gridDim.x / (tiles_n * tiles_k) * a.N * a.K + (size_t)split * a.N : a.db)[n] = s;
     }
@@ -290,69 +320,74 @@ __global__ __launch_bounds__(64) void wgrad8_sum_kernel(const float* __restrict_
   (w ? reinterpret_cast<f32x4*>(dw)[i] : reinterpret_cast<f32x4*>(db)[i - n4]) = s;
 }
 
-// Tile of dw and runs over tokens, by the size of dw in tiles of 128 x 128 (u) and the tokens.  us on bf16 for M x N x K
-// (tokens, rows and columns of dw), /runs:
-//   64 x 64 on four waves, two workgroups per CU, for a small dw or few tokens:  1024 x 256 x 256 /4 7.5 (/1 9.7,
-//     128 x 128 8.8), 1024 x 2048 x 1024 /1 12.8 (14.5), 4096 x 1024 x 512 /4 18.7 (/2 20.6; 19.9).  Runs fill one round
-//     of workgroups, or two over many tokens.
-//   128 x 128 on eight waves:  4096 x 1024 x 1024 /4 23.5 (64 x 64 /2 25.2), 2048 x 1024 x 4096 /1 26.9 (38; 256 x 128 33),
-//     4096 x 2048 x 1024 /2 32 (36);  four waves of 64 x 64 each are behind.  fp32 gradients, three products a term, reach
-//     it with fewer tokens: 3000 x 1024 x 1024 /4 31 (64 x 64 /1 42).
-//   256 x 128 where it costs less:  16200 x 1024 x 4096 /2 147 (169), 2048 x 4096 x 2048 /1 41 (46), 16200 x 1536 x 1024 /5
-//     65 (77);  128 x 256 has twice the codes to decode per thread
-// Of the larger tiles n runs cost rounds of workgroups x tokens of a run x what a workgroup takes for a token, and, where
-// the sum is cut, a launch and the planes' way through the caches; 2 us more for 256 x 128's first and last tiles.  Over
-// 300 sizes and types what this takes is 0.2 % behind the fastest on average.  Runs are of at least 256 tokens (fp32: 128).
-// More tokens take more runs (their factor falls with n, the rest grows) and larger tiles, so for a square dw the scratch
-// for more tokens is never less.
+// Tile of dw and runs over tokens, by the size of dw in tiles of 128 x 128 (u) and the tokens.  us on bf16 for
+// M x N x K (tokens, rows and columns of dw), /runs:
+//   64 x 64 for a small dw or few tokens, on two groups of four waves up to a tile per CU:  1024 x 1024 x 1024 9.1
+//     (one group 11.0; 128 x 128 14.0), 2048 x 1024 x 1024 13.3 (17.4; /2 18.6), 512 x 512 x 512 6.1 (6.7), and past
+//     it two workgroups per CU:  1024 x 2048 x 1024 12.6 (two groups 14.8).  4096 x 512 x 512 /4 12.5 (/3 13.6), fp32
+//     2048 x 1024 x 512 /2 18 (/1 22).
+//   128 x 128 on eight waves:  8192 x 1024 x 1024 /4 32 (64 x 64 37), 2048 x 1024 x 4096 /1 26.9 (38; 256 x 128 33),
+//     4096 x 2048 x 1024 /2 32 (36);  four waves of 64 x 64 each are behind.  fp32 gradients, three products a term,
+//     reach it with fewer tokens: 4096 x 1024 x 1024 /4 37 (64 x 64 41).
+//   256 x 128 where it costs less:  16200 x 1024 x 4096 /2 147 (169), 2048 x 4096 x 2048 /1 41 (46),
+//     16200 x 1536 x 1024 /5 65 (77);  128 x 256 has twice the codes to decode per thread
+// n runs cost rounds of workgroups x (tokens of a run x what a workgroup takes for a token + 3 us), and, where the sum
+// is cut, a launch and the planes' way through the caches; 2 us more for 256 x 128's first and last tiles.  More
+// tokens take more runs (their factor falls with n, the rest grows) and larger tiles, so for a square dw the scratch
+// for more tokens is never less.  Over 286 sizes and types this is 1 % behind the fastest on average.
 enum Shape { k64x64, k128x128, k256x128 };
+
 struct Plan {
-  int shape, splits, per_split, tiles_n, tiles_k;
+  int shape, splits, per_split, tiles_n, tiles_k, groups;
 };
 Plan plan(int dtype, int M, int N, int K) {
   const long u = (long)N * K >> 14;
   const bool bf = dtype == kBF16;
-  const long most = std::min(bf ? (M >= 768 ? M / 256 : 1l) : (M >= 512 ? M / 128 : 1l), 32l);   // runs
   auto tiled = [&](int shape, int bn, int bk) {
     Plan p;
     p.shape = shape;
     p.tiles_n = (N + bn - 1) / bn;
     p.tiles_k = (K + bk - 1) / bk;
-    p.splits = 1;
+    p.splits = p.groups = 1;
     return p;
   };
-  // the runs that cost least, token us per token of a workgroup; returns the cost
-  auto cut = [&](Plan& p, double token) {
-    const long t = (long)p.tiles_n * p.tiles_k;
+  // the runs of at least `least` tokens that cost least, token us per token of a workgroup; returns the cost
+  auto cut = [&](Plan& p, double token, long least) {
+    const long t = (long)p.tiles_n * p.tiles_k, most = std::clamp(M / least, 1l, 32l);
     double best = 0;
     for (long n = 1; n <= most; ++n) {
-      const double us = (double)((t * n + 255) / 256) * M / n * token + (n > 1 ? 4 + 0.8e-6 * n * N * K : 0);
+      const double rounds = (double)((t * n + 255) / 256);
+      const double us = rounds * (M * token / n + 3) + (n > 1 ? 4 + 1e-6 * n * N * K : 0);
       if (n == 1 || us < best) best = us, p.splits = (int)n;
     }
     return best;
   };
   Plan p;
-  if (std::min(N, K) > 64 && (u > 128 || (bf ? M >= 2560 && u * M >= 224 << 10 : M >= 1408 && u * M >= 72 << 10))) {
+  if (std::min(N, K) > 64 && (u > 128 || (u > 64 ? M >= (bf ? 2560 : 1408)
+                                                 : M >= (bf ? 4608 : 2560) && u * M >= (bf ? 224 : 104) << 10))) {
     p = tiled(k128x128, 128, 128);
-    const double us = cut(p, bf ? 0.0105 : 0.025);
+    const double us = cut(p, bf ? 0.0105 : 0.025, bf ? 256 : 128);
     if (bf) {
       Plan w = tiled(k256x128, 256, 128);
-      if (cut(w, 0.0155) + 2 < us) p = w;
+      if (cut(w, 0.0155, 256) + 2 < us) p = w;
     }
   } else {
     p = tiled(k64x64, 64, 64);
-    const long t = (long)p.tiles_n * p.tiles_k;
-    p.splits = (int)std::max(1l, std::min((M >= 2560 && t * M >= 384 << 10 ? 512 : 256) / t, most));
+    if ((long)p.tiles_n * p.tiles_k <= 256 && M >= 256) {
+      p.groups = 2;
+      cut(p, bf ? 0.0041 : 0.0088, 192);
+    }
   }
-  p.per_split = ((M + p.splits - 1) / p.splits + TM - 1) / TM * TM;
+  const int unit = TM * p.groups;
+  p.per_split = ((M + p.splits - 1) / p.splits + unit - 1) / unit * unit;
   return p;
 }
 
-template <typename T, int BN, int BK, int WN, int WK, int OCC>
+template <typename T, int BN, int BK, int WN, int WK, int KG, int OCC>
 hipError_t run(const Wgrad8& a, const Plan& p, hipStream_t st) {
   const int n = p.splits > 1 ? (a.M + p.per_split - 1) / p.per_split : 1;
-  SR_LAUNCH((wgrad8_kernel<T, BN, BK, WN, WK, OCC>), dim3((unsigned)(p.tiles_n * p.tiles_k * n)), dim3(64 * WN * WK), 0,
-            st, a, p.tiles_n, p.tiles_k, n > 1 ? p.per_split : a.M);
+  SR_LAUNCH((wgrad8_kernel<T, BN, BK, WN, WK, KG, OCC>), dim3((unsigned)(p.tiles_n * p.tiles_k * n)),
+            dim3(64 * WN * WK * KG), 0, st, a, p.tiles_n, p.tiles_k, n > 1 ? p.per_split : a.M);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || n == 1) return e;
   const size_t n4 = (size_t)a.N * a.K / 4, b4 = a.db ? (size_t)a.N / 4 : 0;
@@ -365,10 +400,11 @@ template <typename T>
 hipError_t dispatch(const Wgrad8& a, const Plan& p, hipStream_t st) {
   constexpr bool F = sizeof(T) == 4;   // three parts of dy fill the LDS of a workgroup per CU
   switch (p.shape) {
-    case k64x64: return run<T, 64, 64, 2, 2, 2>(a, p, st);
-    case k128x128: return run<T, 128, 128, 2, 4, F ? 1 : 2>(a, p, st);
+    case k64x64:
+      return p.groups == 2 ? run<T, 64, 64, 2, 2, 2, 2>(a, p, st) : run<T, 64, 64, 2, 2, 1, 2>(a, p, st);
+    case k128x128: return run<T, 128, 128, 2, 4, 1, F ? 1 : 2>(a, p, st);
     case k256x128:
-      if constexpr (!F) return run<T, 256, 128, 4, 2, 1>(a, p, st);
+      if constexpr (!F) return run<T, 256, 128, 4, 2, 1, 1>(a, p, st);
   }
   return hipErrorInvalidValue;
 }
