@@ -220,3 +220,11 @@ def test_infinite_gradients_keep_their_sign(dtype):
     ("f32", 16200, 512, 512)])
 def test_weight_grad_on_every_tile_and_run(dtype, M, N, K):
     test_weight_grad_over_many_tokens(dtype, M, N, K)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,N,K", [(255, 72, 192), (256, 8, 64), (257, 72, 192), (383, 64, 64), (385, 200, 64), (1537, 136, 320),
+                                   (3001, 40, 128)])
+def test_weight_grad_where_groups_share_the_tokens(M, N, K, dtype):
+    # odd tiles of tokens over two groups, a group with none of its own, runs that end inside one
+    test_weight_grad_matches_oracle(M, N, K, dtype)
