@@ -90,6 +90,10 @@ def lib(path: str = LIB_PATH):
         return _lib
     if not os.path.exists(path):
         raise SrLibraryMissing(f"{path} is not built; run `python -m paper_2607_02829_amd.build`")
+    try:   # torch brings a HIP runtime of its own, which has to be the process's only one: libsr then binds to it
+        import torch  # noqa: F401
+    except ImportError:
+        pass
     L = ctypes.CDLL(path)
     P = ctypes.c_void_p
     I32, U64, SZ = ctypes.c_int32, ctypes.c_uint64, ctypes.c_size_t
