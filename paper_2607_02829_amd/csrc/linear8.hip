@@ -64,20 +64,20 @@ SR_DEV void put4(const Linear8& a, int m, int n, f32x4 v) {
   }
 }
 // z Phi(z) as max(z, 0) - |z| Phi(-|z|): an operation fewer than z times Phi(z), with the limits at the infinities
-// (a finite |z| times a Phi of 0).  The vector units are what the layer
-// with GELU waits for: 19 instructions an element, two of them at a quarter of the rate, 55 % of the time at
-// 16200 x 4096 x 1024, with the matrix pipes at 30 %.
-template <int DEG>
+// (a finite |z| times a Phi of 0).  Phi is fp32's fit for bf16 results too, so that they are the exact GELU rounded
+// once: the shorter fit, four instructions an element fewer, puts 0.23 % of them a step away (2e-5 with this one) and
+// takes 115 instead of 120 us with the tokens' codes at 16200 x 4096 x 1024.  The vector units are what the layer with
+// GELU waits for: 23 instructions an element, two of them at a quarter of the rate.
 SR_DEV float gelu8(float z) {
-  return fmaf(-fminf(fabsf(z), 3.4028234663852886e38f), half_erfc_of<DEG>(z, z * z), fmaxf(z, 0.f));
+  return fmaf(-fminf(fabsf(z), 3.4028234663852886e38f), half_erfc_of<9>(z, z * z), fmaxf(z, 0.f));
 }
-template <int ACT, typename T>
+template <int ACT>
 SR_DEV f32x4 finish4(float xs, const Cols& c, i32x4 acc) {
   f32x4 v;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     v[q] = fmaf((float)acc[q] * xs, c.ws[q], c.bias[q]);
-    if constexpr (ACT == SR_ACT_GELU) v[q] = gelu8<gelu_deg<T>()>(v[q]);
+    if constexpr (ACT == SR_ACT_GELU) v[q] = gelu8(v[q]);
   }
   return v;
 }
@@ -285,7 +285,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear8_tile_kernel(Li
           for (int q = 0; q < 4; ++q) {
             const Cols c = {*reinterpret_cast<const f32x4*>(sc + nb + 8 * q + 4 * h),
                             *reinterpret_cast<const f32x4*>(sc + BN + nb + 8 * q + 4 * h)};
-            v[q] = finish4<ACT, T>(xs, c, i32x4{acc[p + i][j][4 * q], acc[p + i][j][4 * q + 1], acc[p + i][j][4 * q + 2],
+            v[q] = finish4<ACT>(xs, c, i32x4{acc[p + i][j][4 * q], acc[p + i][j][4 * q + 1], acc[p + i][j][4 * q + 2],
                                                 acc[p + i][j][4 * q + 3]});
             store4<O>(row, nb + 8 * q + 4 * h, v[q]);
           }
@@ -344,7 +344,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear8_tile_kernel(Li
           i32x4 v = *reinterpret_cast<const i32x4*>(stg + lr * LD + c4);
 #pragma unroll
           for (int g = 1; g < KG; ++g) v += *reinterpret_cast<const i32x4*>(stg + (g * PR + lr) * LD + c4);
-          put4<ACT, T>(a, m, n, finish4<ACT, T>(xs[p][q], cols, v));
+          put4<ACT, T>(a, m, n, finish4<ACT>(xs[p][q], cols, v));
         }
       }
     }
@@ -389,7 +389,7 @@ __global__ __launch_bounds__(64 * W) void linear8_few_kernel(Linear8 a) {
       i32x4 v = *reinterpret_cast<const i32x4*>(&stg[0][lr][c4]);
 #pragma unroll
       for (int g = 1; g < W; ++g) v += *reinterpret_cast<const i32x4*>(&stg[g][lr][c4]);
-      put4<ACT, T>(a, m, n, finish4<ACT, T>(a.xs[m], load_cols<T>(a, n), v));
+      put4<ACT, T>(a, m, n, finish4<ACT>(a.xs[m], load_cols<T>(a, n), v));
     }
   }
 }
@@ -446,9 +446,9 @@ hipError_t run_shape(int shape, const Linear8& a, hipStream_t st) {
 //   workgroups are level or ahead: 4050 x 1024 x 1024 10.9 (10.5), 16200 x 256 x 1024 12.3 (14.4)
 //   256 x 256:  16200 x 4096 x 1024 95 (106), 16200 x 1024 x 4096 67 (80), 16200 x 2048 x 512 36 (32);  with half a
 //   round of them 8192 x 1024 x 4096 45 (42);  with GELU, whose vector work wants the second workgroup,
-//   16200 x 2048 x 2048 88 (94), 8192 x 4096 x 1024 62 (57)
-//   256 x 128 of 64-byte stages, two workgroups per CU, with GELU from two rounds of them:  16200 x 4096 x 1024 117
-//   (128 x 128 124, 256 x 256 122), 8192 x 4096 x 1024 55.8 (56.3), 4050 x 4096 x 1024 33.6 (32.7)
+//   16200 x 2048 x 2048 93 (97), 8192 x 4096 x 1024 66 (62)
+//   256 x 128 of 64-byte stages, two workgroups per CU, with GELU from two rounds of them:  16200 x 4096 x 1024 123
+//   (128 x 128 126, 256 x 256 130), 8192 x 4096 x 1024 62.1 (62.1), 4050 x 4096 x 1024 34.8 (34.4)
 // Elsewhere tiles of 256 x 128, and sixteen waves, lie within 4 % of these.
 int pick_shape(const Linear8& a) {
   auto tiles = [&](int bm, int bn) { return (long)((a.M + bm - 1) / bm) * ((a.N + bn - 1) / bn); };
