@@ -97,7 +97,9 @@ typedef enum { SR_BLOCK_PRELN = 0, SR_BLOCK_ADALN = 1 } sr_block_kind;
  * bf16, plus one block's worth of working buffers (34 KB per token, against 10).  The forward's output is bit
  * for bit that without the flag; the gradients are those of the kept values (block inputs, q, k, v, attention
  * output, residual and MLP pre-activation, each within half a step, 1/127 of the largest of its
- * 32 neighbours), with the forward's LayerNorm statistics and row log-sum-exps.  sr_workspace_bytes, the
+ * 32 neighbours), with the forward's LayerNorm statistics.  The backward runs the attention of the kept q, k and v
+ * again, so that its probabilities sum to one whatever the size of the logits; logits of deviation s differ from the
+ * forward's by about s / 80.  sr_workspace_bytes, the
  * sparse, dense and routed block calls take it, forward and backward alike (the same flag in both); a backward
  * also writes the working part of `saved`, so calls on one `saved` must not overlap.  sr_attention_colsums
  * returns SR_EUNSUPPORTED, and calls that do not read `kind` ignore it. */

@@ -73,12 +73,14 @@ def kept(t):
     return blocks_value(*quant_blocks(t2)).reshape(t.shape)
 
 
-def _kept_attention_bwd(q, k, v, O, lse, dO):
-    """dq, dk, dv (B, H, S, hd) with the probabilities exp(s - lse) of the kept q and k and the
-    forward's row log-sum-exps, and delta = rowsum(dO * O) of the kept O."""
+def _kept_attention_bwd(q, k, v, dO):
+    """dq, dk, dv (B, H, S, hd) of the attention of the kept q, k and v: its probabilities and output, not the
+    forward's, so that the rows of P sum to one and those of dS to zero."""
     scale = 1.0 / np.sqrt(q.shape[-1])
-    P = np.exp(q @ k.swapaxes(-1, -2) * scale - lse[..., None])
-    dS = P * (dO @ v.swapaxes(-1, -2) - (dO * O).sum(-1, keepdims=True))
+    s = q @ k.swapaxes(-1, -2) * scale
+    P = np.exp(s - s.max(-1, keepdims=True))
+    P /= P.sum(-1, keepdims=True)
+    dS = P * (dO @ v.swapaxes(-1, -2) - (dO * (P @ v)).sum(-1, keepdims=True))
     return dS @ k * scale, dS.swapaxes(-1, -2) @ q * scale, P.swapaxes(-1, -2) @ dO
 
 
@@ -91,7 +93,7 @@ def _shift(cache, n):
 def block_bwd_kept(dh_out, p, cache):
     """oracle.block.block_bwd from a cache whose block input, q, k, v, attention output, residual,
     MLP pre-activation (and adaLN branch outputs) were kept in the block format; LayerNorm
-    statistics and row log-sum-exps are the forward's."""
+    statistics are the forward's; the attention is that of the kept q, k and v."""
     H, ada = cache["H"], cache["kind"] == "adaln"
     B, S, D = cache["h"].shape
     stats = {}
@@ -103,8 +105,6 @@ def block_bwd_kept(dh_out, p, cache):
         stats[n] = (xhat, rstd, u)
     qkv = kept(np.concatenate([blk.merge_heads(cache[n]) for n in "qkv"], axis=-1))
     q, k, v = (blk.split_heads(qkv[..., i * D:(i + 1) * D], H) for i in range(3))
-    s = cache["q"] @ cache["k"].swapaxes(-1, -2) / np.sqrt(D // H)
-    lse = np.log(np.exp(s - s.max(-1, keepdims=True)).sum(-1)) + s.max(-1)
     O, z = kept(cache["O"]), kept(cache["z"])
     flat = lambda t: t.reshape(-1, t.shape[-1])  # noqa: E731
     g = {n: np.zeros_like(t) for n, t in p.items()}
@@ -121,7 +121,7 @@ def block_bwd_kept(dh_out, p, cache):
     dh1 = dh_out + dx
     da, dgate1 = (dh1 * cache["g1"], (dh1 * kept(cache["a_out"])).sum(1)) if ada else (dh1, None)
     g["w_o"], g["b_o"] = flat(da).T @ flat(O), flat(da).sum(0)
-    d3 = _kept_attention_bwd(q, k, v, blk.split_heads(O, H), lse, blk.split_heads(da @ p["w_o"], H))
+    d3 = _kept_attention_bwd(q, k, v, blk.split_heads(da @ p["w_o"], H))
     dqkv = np.concatenate([blk.merge_heads(t) for t in d3], axis=-1)
     g["w_qkv"], g["b_qkv"] = flat(dqkv).T @ flat(stats["1"][2]), flat(dqkv).sum(0)
     du = dqkv @ p["w_qkv"]

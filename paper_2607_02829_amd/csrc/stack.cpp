@@ -80,7 +80,7 @@ size_t layout_saved(const Dims& d, char* base, BlockSaved* out) {
   const size_t M = d.M, D = d.D, F = d.F, e = d.elt;
   if (d.save8) {
     // the activations in 8 bits per block (10.3 of 24.6 KB per token at D = 1024), then one block's worth of them in
-    // their own types, which the forward writes and the backward restores
+    // their own types, which the forward writes and the backward restores (O and the log-sum-exps: recomputes)
     auto keep = [&](size_t n) {
       Kept8 k;
       k.q = c.take<int8_t>(n);
@@ -102,7 +102,6 @@ size_t layout_saved(const Dims& d, char* base, BlockSaved* out) {
       }
       s.mean1 = c.take<float>(M * 4);
       s.rstd1 = c.take<float>(M * 4);
-      s.lse = c.take<float>((size_t)d.B * d.H * d.S * 4);
       s.mean2 = c.take<float>(M * 4);
       s.rstd2 = c.take<float>(M * 4);
     }
@@ -110,6 +109,7 @@ size_t layout_saved(const Dims& d, char* base, BlockSaved* out) {
     w.hin = c.take<float>(M * D * 4);
     w.qkv = c.take<void>(M * 3 * D * e);
     w.O = c.take<void>(M * D * e);
+    w.lse = c.take<float>((size_t)d.B * d.H * d.S * 4);
     w.h1 = c.take<float>(M * D * 4);
     w.z = c.take<void>(M * F * e);
     if (ada) {
@@ -121,7 +121,7 @@ size_t layout_saved(const Dims& d, char* base, BlockSaved* out) {
     if (out)
       for (int i = 0; i < d.nb; ++i) {
         BlockSaved& s = all[(size_t)i];
-        s.hin = w.hin; s.qkv = w.qkv; s.O = w.O; s.h1 = w.h1; s.z = w.z;
+        s.hin = w.hin; s.qkv = w.qkv; s.O = w.O; s.lse = w.lse; s.h1 = w.h1; s.z = w.z;
         s.a_out = w.a_out; s.m_out = w.m_out; s.u1 = w.u1; s.u2 = w.u2; s.gz = w.gz;
         out[i] = s;
       }
@@ -704,7 +704,16 @@ hipError_t stack_bwd(const Dims& d, const sr_block_params* p, const void* cond, 
         }
         return weight_grad("gemm_dw_o", d, g1, D, s.O, D, g.w_o, g.b_o, sc, kWgO, &jobs[kWgO], ss);
       }));
-      if (d.save8) SR_TRY(restore({q8_job(s.qkv, d.dtype, 3 * MD, s.k_qkv), q8_job(s.O, d.dtype, MD, s.k_O)}));
+      if (d.save8) {
+        // The attention of the kept q, k and v, whose output and log-sum-exps its backward takes: with the forward's,
+        // of other logits, the rows of P would not sum to one, by a factor that grows exponentially with the logits
+        // (0.5 to 1.6 at a deviation of 16).  Its planes lie where the forward's do, in buffers that nothing holds here.
+        SR_TRY(restore({q8_job(s.qkv, d.dtype, 3 * MD, s.k_qkv)}));
+        ProfScope ps("attn_fwd", 4.0 * d.B * (double)S * S * D, (double)M * D * e * 4, st);
+        AttnPart part;
+        const int runs = fwd_attn_part(d, s, &part);
+        SR_TRY(launch_attn_fwd(d.dtype, s.qkv, s.O, s.lse, d.B, S, d.H, D, st, runs, part));
+      }
       const bool fuse_delta = d.dtype == kBF16 && D / d.H == 64;
       {
         GemmDesc gd = desc(d, g1, true, D, (size_t)M * D * e, w.w_o, false, D, (size_t)D * D * e, M, D, D);

@@ -26,8 +26,8 @@ activations, and with them every gradient, are bit for bit those of the run with
 checkpointing; the price is one more forward of every block.
 
 Saved activations in 8 bits (optional): the stages keep what their backward reads as 8-bit codes
-with a power of two per 32 channels, less than half the bytes per block, and run no second forward;
-outputs are those without it, gradients those of the kept values.
+with a power of two per 32 channels, less than half the bytes per block, and run nothing of the forward
+again but the attention; outputs are those without it, gradients those of the kept values.
 """
 from __future__ import annotations
 
