@@ -88,8 +88,8 @@ size_t layout_saved(const Dims& d, char* base, BlockSaved* out) {
       return k;
     };
     const bool ada = d.kind == SR_BLOCK_ADALN;
-    std::vector<BlockSaved> all((size_t)d.nb);
-    for (BlockSaved& s : all) {
+    for (int i = 0; i < d.nb; ++i) {
+      BlockSaved s{};
       s.k_hin = keep(M * D);
       s.k_qkv = keep(M * 3 * D);
       s.k_O = keep(M * D);
@@ -104,6 +104,7 @@ size_t layout_saved(const Dims& d, char* base, BlockSaved* out) {
       s.rstd1 = c.take<float>(M * 4);
       s.mean2 = c.take<float>(M * 4);
       s.rstd2 = c.take<float>(M * 4);
+      if (out) out[i] = s;
     }
     BlockSaved w{};
     w.hin = c.take<float>(M * D * 4);
@@ -120,10 +121,9 @@ size_t layout_saved(const Dims& d, char* base, BlockSaved* out) {
     w.gz = c.take<void>(M * F * e);
     if (out)
       for (int i = 0; i < d.nb; ++i) {
-        BlockSaved& s = all[(size_t)i];
+        BlockSaved& s = out[i];
         s.hin = w.hin; s.qkv = w.qkv; s.O = w.O; s.lse = w.lse; s.h1 = w.h1; s.z = w.z;
         s.a_out = w.a_out; s.m_out = w.m_out; s.u1 = w.u1; s.u2 = w.u2; s.gz = w.gz;
-        out[i] = s;
       }
     return c.off;
   }
@@ -707,7 +707,7 @@ hipError_t stack_bwd(const Dims& d, const sr_block_params* p, const void* cond, 
       if (d.save8) {
         // The attention of the kept q, k and v, whose output and log-sum-exps its backward takes: with the forward's,
         // of other logits, the rows of P would not sum to one, by a factor that grows exponentially with the logits
-        // (0.5 to 1.6 at a deviation of 16).  Its planes lie where the forward's do, in buffers that nothing holds here.
+        // (0.6 to 1.9 at a deviation of 16).  Its planes lie where the forward's do, in buffers that nothing holds here.
         SR_TRY(restore({q8_job(s.qkv, d.dtype, 3 * MD, s.k_qkv)}));
         ProfScope ps("attn_fwd", 4.0 * d.B * (double)S * S * D, (double)M * D * e * 4, st);
         AttnPart part;
