@@ -87,7 +87,8 @@ class Trunk:
             for c in self.cfg:
                 c.kind |= abi.SR_BLOCK_SAVE8
         self.params8 = None
-        self.overwritten = False   # by a forecast, since the last forward
+        self.forecast_last = False       # the last eager pass was a forecast
+        self.forward_captured = False    # a graph holds a forward, whose replays are not seen here
         bounds = (0, n1, n1 + n2, n1 + n2 + n3)
         self.params = [device.DeviceParams(params_storage[bounds[i]:bounds[i + 1]], w.kind) for i in range(3)]
         self.grads = [device.DeviceGrads(w, n, skip_unused=True) for n in split]
@@ -116,10 +117,14 @@ class Trunk:
     def forward(self, x0, step: int):
         """x0: (B, L, D) storage tensor (not modified; with checkpointing the backward reads it
         again, so it must keep its values until then).  Returns the trunk output x3."""
+        import torch
         a, (ce, cm, cl), (pe, pm, pl) = abi, self.cfg, self.params
         K = self.K
         self.x0 = x0
-        self.overwritten = False
+        if torch.cuda.is_current_stream_capturing():   # nothing runs yet
+            self.forward_captured = True
+        else:
+            self.forecast_last = False
         a.sr_dense_blocks_fwd(ce, pe.array, None, x0, self.x1, self.saved[0], self.scratch)
         if self.select == "attn":
             a.sr_attention_colsums(ce, self.w.L, self.saved[0], self.split[0] - 1, self.colsum)
@@ -134,9 +139,11 @@ class Trunk:
 
     def backward(self, g3):
         """g3: (B, L, D) storage gradient of the trunk output (not modified).  Returns the
-        input gradient g0; the parameter gradients are in ``self.grads`` (early, middle, late)."""
-        if self.overwritten:
-            raise RuntimeError("a forecast has overwritten the forward's buffers: run forward again")
+        input gradient g0; the parameter gradients are in ``self.grads`` (early, middle, late).
+        Refused where the last eager pass was a forecast, unless a graph holds a forward (a replay
+        of which may have come since)."""
+        if self.forecast_last and not self.forward_captured:
+            raise RuntimeError("the last pass was a forecast, which has no backward: run forward again")
         a, (ce, cm, cl), (pe, pm, pl) = abi, self.cfg, self.params
         ge, gm, gl = (g.array for g in self.grads)
         K, ck = self.K, self.checkpoint
@@ -168,22 +175,28 @@ class Trunk:
         self.params8 = [device.DeviceParams8(p) for p in self.params]
         n = max(abi.sr_blocks8_scratch_bytes(c, s) for c, s in zip(self.cfg, (self.w.L, self.K, self.w.L)))
         self.scratch8 = torch.empty(n, dtype=torch.uint8, device="cuda")
+        # a forecast's own: the backward of a forward reads the others, whatever runs or is replayed in between
+        self.x1_8, self.idx_8, self.h0_8, self.h_8 = (torch.empty_like(t) for t in (self.x1, self.idx, self.h0, self.h))
 
     def forecast(self, x0, step: int):
         """The forward with weights and tokens in 8 bits (``quantize`` first), keeping nothing for a
-        backward: x0 (B, L, D) storage tensor, not modified.  Returns the trunk output x3; an earlier
-        ``forward``'s buffers (x1, x3, idx, h0, h) are overwritten, and with them its ``backward``."""
+        backward: x0 (B, L, D) storage tensor, not modified.  Returns the trunk output in x3, where an
+        earlier ``forward``'s was; its indices are in ``idx_8``.  What the backward of that forward reads
+        is left alone."""
+        import torch
         if self.params8 is None:
             raise RuntimeError("forecast needs quantize() first")
         a, (ce, cm, cl), (pe, pm, pl) = abi, self.cfg, self.params8
         K, L = self.K, self.w.L
-        self.overwritten = True
-        a.sr_blocks8_fwd(ce, L, pe.array, None, x0, self.x1, self.scratch8)
-        a.sr_select_indices(cm, K, a.SR_SEL_RANDOM, self.seed, step, None, None, self.idx)
-        a.sr_gather(cm, K, self.x1, self.idx, self.h0)
-        a.sr_blocks8_fwd(cm, K, pm.array, None, self.h0, self.h, self.scratch8)
-        a.sr_scatter_delta(cm, K, self.x1, self.h, self.h0, self.idx)
-        a.sr_blocks8_fwd(cl, L, pl.array, None, self.x1, self.x3, self.scratch8)
+        x1, idx, h0, h = self.x1_8, self.idx_8, self.h0_8, self.h_8
+        if not torch.cuda.is_current_stream_capturing():
+            self.forecast_last = True
+        a.sr_blocks8_fwd(ce, L, pe.array, None, x0, x1, self.scratch8)
+        a.sr_select_indices(cm, K, a.SR_SEL_RANDOM, self.seed, step, None, None, idx)
+        a.sr_gather(cm, K, x1, idx, h0)
+        a.sr_blocks8_fwd(cm, K, pm.array, None, h0, h, self.scratch8)
+        a.sr_scatter_delta(cm, K, x1, h, h0, idx)
+        a.sr_blocks8_fwd(cl, L, pl.array, None, x1, self.x3, self.scratch8)
         return self.x3
 
     def block_grads(self):
