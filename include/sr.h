@@ -102,7 +102,8 @@ typedef enum { SR_BLOCK_PRELN = 0, SR_BLOCK_ADALN = 1 } sr_block_kind;
  * forward's by about s / 80.  sr_workspace_bytes, the
  * sparse, dense and routed block calls take it, forward and backward alike (the same flag in both); a backward
  * also writes the working part of `saved`, so calls on one `saved` must not overlap.  sr_attention_colsums
- * returns SR_EUNSUPPORTED, and calls that do not read `kind` ignore it. */
+ * returns SR_EUNSUPPORTED.  Calls that do not read `kind` ignore it, the generative blocks' (sr_edm_*) among them:
+ * their `saved` keeps its full size. */
 enum { SR_BLOCK_SAVE8 = 16 };
 
 /* Selectors.

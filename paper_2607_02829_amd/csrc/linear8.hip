@@ -67,7 +67,8 @@ SR_DEV void put4(const Linear8& a, int m, int n, f32x4 v) {
 // (a finite |z| times a Phi of 0).  Phi is fp32's fit for bf16 results too, so that they are the exact GELU rounded
 // once: the shorter fit, four instructions an element fewer, puts 0.23 % of them a step away (2e-5 with this one) and
 // takes 115 instead of 120 us with the tokens' codes at 16200 x 4096 x 1024.  The vector units are what the layer with
-// GELU waits for: 23 instructions an element, two of them at a quarter of the rate.
+// GELU waits for: 23 instructions an element, two of them at a quarter of the rate, issuing in 51 % of the time there,
+// with the matrix pipes at 28 %.
 SR_DEV float gelu8(float z) {
   return fmaf(-fminf(fabsf(z), 3.4028234663852886e38f), half_erfc_of<9>(z, z * z), fmaxf(z, 0.f));
 }
@@ -443,7 +444,10 @@ hipError_t run_shape(int shape, const Linear8& a, hipStream_t st) {
 //   32 x 32, eight groups of waves:  128 x 1024 x 4096 6.7 (64 x 64 9.1);  x 256 3.6 (3.4)
 //   64 x 64, two groups:  1024 x 1024 x 1024 6.2 (64 x 128 7.3);  64 x 128:  2048 x 1024 x 1024 7.7 (8.7, 128 x 128 9.7)
 //   128 x 128, four stages, one workgroup per CU:  4050 x 1024 x 4096 22.9 (two 26.1);  with shorter rows two
-//   workgroups are level or ahead: 4050 x 1024 x 1024 10.9 (10.5), 16200 x 256 x 1024 12.3 (14.4)
+//   workgroups are level or ahead: 4050 x 1024 x 1024 10.7 (10.3), 16200 x 256 x 1024 12.3 (14.4), 4083 x 1024 x 256 6.4
+//   (6.8), fp32 8.6 (8.9).  Smaller tiles of four stages are behind where 128 x 128 is one round or just under it, which
+//   leaves the second slot of every CU empty:  4050 x 1024 x 1024 64 x 128 12.8, 64 x 64 15.2;  4083 x 1024 x 256 8.4,
+//   9.4, fp32 10.1, 10.1;  2500 x 1024 x 1024 11.4, 11.6 (9.7)
 //   256 x 256:  16200 x 4096 x 1024 95 (106), 16200 x 1024 x 4096 67 (80), 16200 x 2048 x 512 36 (32);  with half a
 //   round of them 8192 x 1024 x 4096 45 (42);  with GELU, whose vector work wants the second workgroup,
 //   16200 x 2048 x 2048 93 (97), 8192 x 4096 x 1024 66 (62)

@@ -12,9 +12,10 @@
 // out of the transposing LDS reads.  The codes are a byte each on their way from memory and are decoded once per
 // workgroup.  Few output tiles are cut over tokens into planes that a second launch adds in order.
 //
-// What bounds it: at 16200 x 1024 x 4096 the matrix pipes are busy 42 % of the time, the LDS 42 % and the vector
-// units 25 %; a wave issues in order, so fragment reads, decoding and writes are placed between its products
-// (256 x 128 tiles 177 us with the writes before the products, 157 so; 0.87 PFLOP/s).
+// What bounds it: at 16200 x 1024 x 4096 the matrix pipes are busy 46 % of the time, the LDS 46 % and the vector
+// units 28 %; a wave issues in order, so fragment reads, decoding and writes are placed between its products
+// (256 x 128 tiles 177 us with the writes before the products, 157 so).  A call takes 148 us, 8 of them the planes'
+// sum: 0.92 PFLOP/s.
 #include <algorithm>
 
 #include "common.h"

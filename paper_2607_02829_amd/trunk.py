@@ -116,7 +116,8 @@ class Trunk:
 
     def forward(self, x0, step: int):
         """x0: (B, L, D) storage tensor (not modified; with checkpointing the backward reads it
-        again, so it must keep its values until then).  Returns the trunk output x3."""
+        again, so it must keep its values until then; that of the last call, where a captured forward
+        is replayed after it).  Returns the trunk output x3."""
         import torch
         a, (ce, cm, cl), (pe, pm, pl) = abi, self.cfg, self.params
         K = self.K
