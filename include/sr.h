@@ -437,6 +437,136 @@ SR_API sr_status sr_blocks8_scratch_bytes(const sr_config* cfg, int32_t S, size_
 SR_API sr_status sr_blocks8_fwd(const sr_config* cfg, int32_t S, const sr_block_params8* params, const void* cond,
                          const void* h_in, void* h_out, void* scratch, size_t scratch_bytes, void* stream);
 
+/* Operators around the calls above, for blocks put together from them (rotary positions, dropout, the residual step
+ * with its norms, linear layers on 8-bit floating point).  They take their sizes directly or in structs of their own
+ * (no sr_config); any size from 1 up is taken unless a call says otherwise, also odd ones. */
+
+/* Rotary positions with several axes.  A token stands on a grid of up to three axes (time, height, width; the last one
+ * runs fastest: token l = (i_0 * grid[1] + i_1) * grid[2] + i_2) and every head turns `pairs` pairs of its channels by
+ *   angle(token, p) = (origin[a] + step[a] * i_a) * f_p      p = 0 .. P-1, a the axis that owns pair p,
+ * in 64 bits (a far position keeps its angle).  Axis 0 owns the first pairs[0] pairs, axis 1 the next, and so on;
+ * P = their sum, 2 P <= head_dim.  f_p = base^(-j / pairs[a]) for the axis's j-th pair, or freqs[p].
+ *   SR_ROT_HALVES: pair p is channels (p, P + p) of the head;  SR_ROT_NEIGHBOURS: channels (2 p, 2 p + 1).
+ *   (c0, c1) -> (c0 cos - c1 sin, c1 cos + c0 sin), in fp32 and rounded once; channels from 2 P on are unchanged. */
+typedef enum { SR_ROT_HALVES = 0, SR_ROT_NEIGHBOURS = 1 } sr_rotary_layout;
+typedef struct {
+  int32_t axes;                /* 1, 2 or 3 */
+  int32_t grid[3], pairs[3];   /* of each axis, slowest first; grid >= 1, pairs >= 0 */
+  int32_t layout;              /* sr_rotary_layout */
+  double base;                 /* > 0; not read with freqs */
+  double origin[3], step[3];   /* finite; origin: e.g. the time of a frame, or a window's corner */
+  const double* freqs;         /* HOST array of P values, read during the call, or NULL */
+} sr_rotary_cfg;
+
+/* x -> y: `heads` heads of head_dim channels side by side in each of B*S rows; row r starts ldx (ldy) elements after
+ * row r - 1, so the queries and keys in a row of q | k | v are one call with 2 H heads, in place.  Only those
+ * channels are read and written.  y may be x (with ldy = ldx) and may not overlap it otherwise.
+ *   idx: [B,S] int32 ([1,S] with idx_shared), the token index of each row, as sr_select_indices gives it (any order,
+ *        repeats allowed; entries in [0, grid product)), or NULL: row s of a sample is token s (S <= the grid product).
+ *   inverse: 1 turns by the negative angles: the gradient of x from that of y.
+ * 1 <= head_dim <= 256; ldx, ldy >= heads * head_dim.  Rows that start on multiples of 16 bytes, with P (SR_ROT_HALVES; 2 P
+ * otherwise) and head_dim multiples of 16 bytes too, are read 16 bytes at a time, others by element. */
+SR_API sr_status sr_rotary(const sr_rotary_cfg* rot, int32_t inverse, int32_t dtype, int32_t B, int32_t S, int32_t heads,
+                    int32_t head_dim, const void* x, int64_t ldx, const int32_t* idx, int32_t idx_shared, void* y,
+                    int64_t ldy, void* stream);
+
+/* Dropout whose mask is never stored: it is drawn anew, the same, wherever it is needed.  A value is dropped if its
+ * 16 bits are below t = p * 65536 to the nearest integer, and multiplied by 65536 / (65536 - t) (fp32) otherwise: the
+ * expectation is exact for every p (p = 1 drops all).  Draw e's bits are those from 16 (e % 4) up of the word
+ *   mix(key + (e / 4 + 1) gamma),   key = mix(seed + (step + 1) gamma)      (SplitMix64, as in SR_SEL_RANDOM)
+ *   group = 0: element (row, n) of N columns is draw (first_row + row) * N + n;
+ *   group > 0: the values of a row share the draw (first_row + row) / group (1: tokens; S: samples, that is
+ *              stochastic depth).
+ * first_row lets the ranks or pieces of a batch draw as the whole batch would.  step_dev (a device address, 8-byte
+ * aligned, or NULL) is read by the kernel and added to step, so that every replay of a captured graph can have a draw of its own. */
+typedef struct {
+  float p;                     /* in [0, 1]; 0: nothing is dropped */
+  int32_t group;
+  uint64_t seed, step, first_row;
+  const uint64_t* step_dev;
+} sr_drop;
+
+/* y = resid + drop(x), x, resid (or NULL) and y [M,N] of the storage type, one rounding.  Dropped values of x do not
+ * count, NaN or not.  y may be x or resid.  The gradient of x is the same call on the gradient of y with resid NULL; that
+ * of resid is the gradient of y itself. */
+SR_API sr_status sr_dropout(const sr_drop* drop, int32_t dtype, int32_t M, int32_t N, const void* x, const void* resid,
+                     void* y, void* stream);
+
+/* The residual step between two branches of a block, in one pass: the norm after one branch, its dropout, gate and
+ * residual scale, the sum, and the norm before the next branch.  Per row of D channels of sample b:
+ *   n  = post ? Norm(y) post_w + post_b : y
+ *   x1 = x + gate_b res_scale drop(n)                              rounded to the stream's type
+ *   u  = (Norm(x1) pre_w + pre_b) (1 + scale_b) + shift_b          rounded to the storage type
+ * SR_NORM_LAYER: Norm(z) = (z - mean) / sqrt(var + eps);  SR_NORM_RMS: z / sqrt(mean z^2 + eps).  fp32 throughout. */
+typedef enum { SR_NORM_LAYER = 0, SR_NORM_RMS = 1 } sr_norm;
+typedef struct {
+  int32_t B, S, D;             /* samples, rows per sample, channels (D <= 8192) */
+  int32_t dtype;               /* of y, u, the parameters post_w .. pre_b and their gradients' tokens */
+  int32_t stream_dtype;        /* of x, x1, dx1, dx: SR_F32, or dtype */
+  int32_t norm;                /* sr_norm, of both norms */
+  int32_t post;                /* 1: the branch output is normed; 0: n = y */
+  float eps;
+  int64_t mod_stride;          /* elements from one sample's gate (shift, scale) to the next's */
+  sr_drop drop;                /* of n; rows are numbered b S + s, columns D */
+} sr_residual_norm;
+/* Device pointers; a NULL member is left out of the formula (a factor of one, a summand of zero). */
+typedef struct {
+  const void *post_w, *post_b, *res_scale, *pre_w, *pre_b;   /* [D], storage type */
+  const float *gate, *shift, *scale;                         /* [B, mod_stride] rows, 4-byte aligned */
+} sr_residual_norm_params;
+/* fp32, OVERWRITTEN, a NULL member skips one: [D] (summed over the samples), and [B,D] for gate, shift and scale. */
+typedef struct {
+  float *post_w, *post_b, *res_scale, *pre_w, *pre_b, *gate, *shift, *scale;
+} sr_residual_norm_grads;
+
+/* x, y -> x1, u.  y NULL: x1 = x, not written (x1 may be NULL), the norm before a first branch.  x1 may be x.
+ *   u: [B,S,D], or NULL;  uq, ue: u as the rows of sr_quantize_f8 (SR_F8_ROW) give it, straight from the fp32 values (not
+ *      through the storage type), or NULL.  u, uq and ue all NULL: no norm before a next branch.
+ *   stats: [4, B*S] fp32 for the backward (mean and reciprocal deviation of y, then of x1; those that the call does not
+ *          compute are not written), or NULL. */
+SR_API sr_status sr_residual_norm_fwd(const sr_residual_norm* cfg, const sr_residual_norm_params* params, const void* x,
+                               const void* y, void* x1, void* u, uint8_t* uq, uint8_t* ue, float* stats, void* stream);
+
+/* Its vector-Jacobian product.  x1: the forward's (x where y was NULL).  dx1: gradient of x1 by what else reads it, or NULL
+ * for none; du: gradient of u, or NULL if the forward had no u (one of the two is needed).  dx (may be dx1) and dy out; dy, y NULL together.
+ * Column sums run in a fixed order (deterministic).  scratch: sr_residual_norm_scratch_bytes bytes. */
+SR_API sr_status sr_residual_norm_scratch_bytes(const sr_residual_norm* cfg, size_t* scratch_bytes);
+SR_API sr_status sr_residual_norm_bwd(const sr_residual_norm* cfg, const sr_residual_norm_params* params, const void* x1,
+                               const void* y, const float* stats, const void* dx1, const void* du, void* dx, void* dy,
+                               const sr_residual_norm_grads* grads, void* scratch, size_t scratch_bytes, void* stream);
+
+/* Linear layers on 8-bit floating point: codes of 4 exponent and 3 mantissa bits (e4m3: largest 448, no infinities), with
+ * a power of two per block of 128 values.  A block holds 2^e, e the smallest integer in [-126, 119] with
+ * max |x| <= 448 2^e, kept as the byte e + 127; a code is x 2^-e to the nearest e4m3 value, halves to the even one,
+ * within +-448 (which only a block with values above 1.75 * 2^127 meets).  A floating-point code gains
+ * nothing from a scale between two powers of two, and the matrix instructions apply these ones by themselves.
+ * A block with an Inf or NaN has NaN codes and e = 0.
+ *   SR_F8_ROW: blocks of 128 consecutive values (tokens and gradients);
+ *   SR_F8_TILE: blocks of 128 x 128 (weights: one code for both directions).
+ * Layout of R rows of C values: codes [R, Cp], Cp = C rounded up to 128, zeros past C; exponents [Cp / 128, Rp], Rp = R rounded up
+ * to 16, one per row and block (the rows of a tile repeat it; bytes past R belong to no value). */
+typedef enum { SR_F8_ROW = 0, SR_F8_TILE = 1 } sr_f8_kind;
+
+/* x [M,N] storage type, rows ldx elements apart -> its codes and exponents as M rows of N (q, e), and those of its
+ * transpose, N rows of M (qt, et; SR_F8_ROW: blocks of 128 rows of x).  Either pair may be NULL.  One pass over x.
+ * M * Np, N * Mp < 2^31;  ldx >= N. */
+SR_API sr_status sr_quantize_f8(int32_t f8_kind, int32_t dtype, int32_t M, int32_t N, const void* x, int64_t ldx, uint8_t* q,
+                         uint8_t* e, uint8_t* qt, uint8_t* et, void* stream);
+
+/* y[m,n] = act( sum_k x[m,k] w[n,k] + bias[n] ), x and w the values of codes (xq, xe: M rows of K; wq, we: N rows
+ * of K), sums in fp32, one rounding to y's type.  (bf16 results: the matrix instructions' sums of 8-bit floating point, which
+ * drop what lies 14 bits below the largest of eight products, about 1.5e-5 of the results' deviation.  fp32
+ * results: exact products and fp32 sums of them, at half the rate.)  The three products of a linear layer y = x w^T are
+ *   (M, N, K) on x and w;   dx: (M, K, N) on dy and the transposed codes of w;
+ *   dw: (N, K, M), SR_F32, on the transposed codes of dy and of x.
+ *   dtype: of bias (or NULL) and y [M,N];  act: sr_act.
+ *   scratch: sr_linear_f8_scratch_bytes bytes (NULL when 0), for the partial sums of long rows with few results.
+ * M, N >= 1; 1 <= K <= 2^24; M*Kp, N*Kp and M*N*elt < 2^31 bytes (Kp: K rounded up to 128). */
+SR_API sr_status sr_linear_f8_scratch_bytes(int32_t M, int32_t N, int32_t K, size_t* scratch_bytes);
+SR_API sr_status sr_linear_f8(int32_t dtype, int32_t act, int32_t M, int32_t N, int32_t K, const uint8_t* xq, const uint8_t* xe,
+                       const uint8_t* wq, const uint8_t* we, const void* bias, void* y, void* scratch,
+                       size_t scratch_bytes, void* stream);
+
 /* Launch timing for measurement (not needed by the method).  After
  * sr_profile_start, every library launch group whose name contains `name_filter`
  * ("" or NULL = all) is timed with HIP events bound to its first and last kernel at launch
@@ -453,7 +583,7 @@ SR_API sr_status sr_blocks8_fwd(const sr_config* cfg, int32_t S, const sr_block_
  * gemm_<op> (qkv, o, fc1, fc2, dx_fc2, dx_fc1, dx_o, dx_qkv, dw_<op>), attn_fwd,
  * attn_bwd_dkv, attn_bwd_dq, attn_bwd_f32 (both passes of fp32 storage), attn_bwd_delta, reduce,
  * colsum, convert, mod, quantize8, dequantize8, linear8, weight_grad8,
- * ln_quant.  Where few workgroups make dK/dV and dQ one launch (bf16, head dim 64),
+ * ln_quant, rotary, dropout, residual_norm_fwd, residual_norm_bwd, quantize_f8, linear_f8.  Where few workgroups make dK/dV and dQ one launch (bf16, head dim 64),
  * attn_bwd_dkv holds both passes. */
 SR_API sr_status sr_profile_start(const char* name_filter);
 SR_API sr_status sr_profile_stop(char* out, size_t out_bytes, size_t* needed);

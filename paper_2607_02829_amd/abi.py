@@ -20,6 +20,9 @@ SR_BLOCK_SAVE8 = 16
 SR_SEL_RANDOM, SR_SEL_TOPK_DIFFNORM = 0, 1
 SR_Q8_ROW, SR_Q8_BLOCK = 0, 1
 SR_ACT_NONE, SR_ACT_GELU = 0, 1
+SR_ROT_HALVES, SR_ROT_NEIGHBOURS = 0, 1
+SR_NORM_LAYER, SR_NORM_RMS = 0, 1
+SR_F8_ROW, SR_F8_TILE = 0, 1
 
 PARAM_FIELDS = ("ln1_w", "ln1_b", "w_qkv", "b_qkv", "w_o", "b_o", "ln2_w", "ln2_b",
                 "w_fc1", "b_fc1", "w_fc2", "b_fc2", "w_ada", "b_ada")
@@ -32,6 +35,8 @@ EXPORTS = ("sr_last_error", "sr_version", "sr_workspace_bytes", "sr_select_scrat
            "sr_edm_workspace_bytes", "sr_edm_blocks_fwd", "sr_edm_blocks_bwd",
            "sr_quantize8", "sr_dequantize8", "sr_linear8", "sr_weight_grad8", "sr_weight_grad8_scratch_bytes",
            "sr_blocks8_scratch_bytes", "sr_blocks8_fwd",
+           "sr_rotary", "sr_dropout", "sr_residual_norm_fwd", "sr_residual_norm_scratch_bytes", "sr_residual_norm_bwd",
+           "sr_quantize_f8", "sr_linear_f8_scratch_bytes", "sr_linear_f8",
            "sr_profile_start", "sr_profile_stop", "sr_probe_mfma_rate")
 
 
@@ -81,6 +86,48 @@ class SrBlockParams8(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in PARAM8_FIELDS]
 
 
+class SrRotary(ctypes.Structure):
+    """sr_rotary_cfg from sequences: one entry per axis, slowest first (freqs: one per pair, or None)."""
+    _fields_ = [("axes", ctypes.c_int32), ("grid", ctypes.c_int32 * 3), ("pairs", ctypes.c_int32 * 3),
+                ("layout", ctypes.c_int32), ("base", ctypes.c_double), ("origin", ctypes.c_double * 3),
+                ("step", ctypes.c_double * 3), ("freqs", ctypes.POINTER(ctypes.c_double))]
+
+    def __init__(self, grid, pairs, layout=SR_ROT_HALVES, base=10000.0, origin=None, step=None, freqs=None):
+        n = len(grid)
+        origin, step = origin or [0.0] * n, step or [1.0] * n
+        if not 1 <= n <= 3 or any(len(v) != n for v in (pairs, origin, step)):
+            raise ValueError("one to three axes, with an entry of pairs, origin and step for each")
+        if freqs is not None and len(freqs) != sum(pairs):
+            raise ValueError(f"{len(freqs)} frequencies for {sum(pairs)} pairs")
+        super().__init__(axes=n, layout=layout, base=base)
+        self.grid[:n], self.pairs[:n], self.origin[:n], self.step[:n] = grid, pairs, origin, step
+        if freqs is not None:
+            self._freqs = (ctypes.c_double * max(len(freqs), 1))(*freqs)
+            self.freqs = ctypes.cast(self._freqs, ctypes.POINTER(ctypes.c_double))
+
+
+class SrDrop(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_float), ("group", ctypes.c_int32), ("seed", ctypes.c_uint64), ("step", ctypes.c_uint64),
+                ("first_row", ctypes.c_uint64), ("step_dev", ctypes.c_void_p)]
+
+
+class SrResidualNorm(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("S", ctypes.c_int32), ("D", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("stream_dtype", ctypes.c_int32), ("norm", ctypes.c_int32), ("post", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("mod_stride", ctypes.c_int64), ("drop", SrDrop)]
+
+
+RESIDUAL_NORM_FIELDS = ("post_w", "post_b", "res_scale", "pre_w", "pre_b", "gate", "shift", "scale")
+
+
+class SrResidualNormParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in RESIDUAL_NORM_FIELDS]
+
+
+class SrResidualNormGrads(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in RESIDUAL_NORM_FIELDS]
+
+
 _lib = None
 
 
@@ -96,7 +143,7 @@ def lib(path: str = LIB_PATH):
         pass
     L = ctypes.CDLL(path)
     P = ctypes.c_void_p
-    I32, U64, SZ = ctypes.c_int32, ctypes.c_uint64, ctypes.c_size_t
+    I32, I64, U64, SZ = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_size_t
     CP = ctypes.POINTER(SrConfig)
     sig = {
         "sr_last_error": ([], ctypes.c_char_p),
@@ -128,6 +175,14 @@ def lib(path: str = LIB_PATH):
         "sr_weight_grad8": ([I32, I32, I32, I32, P, P, P, P, P, P, SZ, P], I32),
         "sr_blocks8_scratch_bytes": ([CP, I32, ctypes.POINTER(SZ)], I32),
         "sr_blocks8_fwd": ([CP, I32, P, P, P, P, P, SZ, P], I32),
+        "sr_rotary": ([P, I32, I32, I32, I32, I32, I32, P, I64, P, I32, P, I64, P], I32),
+        "sr_dropout": ([P, I32, I32, I32, P, P, P, P], I32),
+        "sr_residual_norm_fwd": ([P, P, P, P, P, P, P, P, P, P], I32),
+        "sr_residual_norm_scratch_bytes": ([P, ctypes.POINTER(SZ)], I32),
+        "sr_residual_norm_bwd": ([P, P, P, P, P, P, P, P, P, P, P, SZ, P], I32),
+        "sr_quantize_f8": ([I32, I32, I32, I32, P, I64, P, P, P, P, P], I32),
+        "sr_linear_f8_scratch_bytes": ([I32, I32, I32, ctypes.POINTER(SZ)], I32),
+        "sr_linear_f8": ([I32, I32, I32, I32, I32, P, P, P, P, P, P, P, SZ, P], I32),
         "sr_profile_start": ([ctypes.c_char_p], I32),
         "sr_profile_stop": ([ctypes.c_char_p, SZ, ctypes.POINTER(SZ)], I32),
         "sr_probe_mfma_rate": ([P, ctypes.POINTER(ctypes.c_double), P], I32),
@@ -326,6 +381,77 @@ def sr_blocks8_scratch_bytes(cfg: SrConfig, S: int) -> int:
 def sr_blocks8_fwd(cfg, S, params, cond, h_in, h_out, scratch, stream=None):
     _check(lib().sr_blocks8_fwd(ctypes.byref(cfg), S, params, _p(cond), _p(h_in), _p(h_out), _p(scratch),
                                 _nbytes(scratch), _stream(stream)))
+
+
+def sr_rotary(rot, inverse, dtype, B, S, heads, head_dim, x, ldx, idx, idx_shared, y, ldy, stream=None):
+    _check(lib().sr_rotary(ctypes.byref(rot), inverse, dtype, B, S, heads, head_dim, _p(x), ldx, _p(idx), idx_shared,
+                           _p(y), ldy, _stream(stream)))
+
+
+def sr_dropout(drop, dtype, M, N, x, resid, y, stream=None):
+    _check(lib().sr_dropout(ctypes.byref(drop), dtype, M, N, _p(x), _p(resid), _p(y), _stream(stream)))
+
+
+def _residual_norm_struct(cls, tensors):
+    s = cls(**{k: _p(t) for k, t in tensors.items()})
+    s._tensors = tensors   # alive as long as the struct that points at them
+    return s
+
+
+def residual_norm_params(**tensors):
+    """sr_residual_norm_params of tensors (post_w, post_b, res_scale, pre_w, pre_b, gate, shift, scale; what is left
+    out stays out of the formula)."""
+    return _residual_norm_struct(SrResidualNormParams, tensors)
+
+
+def residual_norm_grads(**tensors):
+    """sr_residual_norm_grads of fp32 tensors under the parameters' names."""
+    return _residual_norm_struct(SrResidualNormGrads, tensors)
+
+
+def sr_residual_norm_fwd(cfg, params, x, y, x1, u, uq=None, ue=None, stats=None, stream=None):
+    _check(lib().sr_residual_norm_fwd(ctypes.byref(cfg), ctypes.byref(params), _p(x), _p(y), _p(x1), _p(u), _p(uq),
+                                      _p(ue), _p(stats), _stream(stream)))
+
+
+def sr_residual_norm_scratch_bytes(cfg) -> int:
+    a = ctypes.c_size_t()
+    _check(lib().sr_residual_norm_scratch_bytes(ctypes.byref(cfg), ctypes.byref(a)))
+    return a.value
+
+
+def sr_residual_norm_bwd(cfg, params, x1, y, stats, dx1, du, dx, dy, grads, scratch, stream=None):
+    _check(lib().sr_residual_norm_bwd(ctypes.byref(cfg), ctypes.byref(params), _p(x1), _p(y), _p(stats), _p(dx1),
+                                      _p(du), _p(dx), _p(dy), ctypes.byref(grads), _p(scratch), _nbytes(scratch),
+                                      _stream(stream)))
+
+
+def f8_shapes(rows: int, cols: int):
+    """Shapes of the codes and exponents of `rows` rows of `cols` values (sr_quantize_f8)."""
+    blocks = (cols + 127) // 128
+    return (rows, 128 * blocks), (blocks, (rows + 15) // 16 * 16)
+
+
+def f8_buffers(M, N, rows=True, transposed=False, device="cuda"):
+    """(q, e, qt, et) of sr_quantize_f8 for an M x N matrix, as uint8 tensors; None for what is not asked for."""
+    import torch
+    shapes = (*(f8_shapes(M, N) if rows else (None, None)), *(f8_shapes(N, M) if transposed else (None, None)))
+    return tuple(None if s is None else torch.empty(s, dtype=torch.uint8, device=device) for s in shapes)
+
+
+def sr_quantize_f8(f8_kind, dtype, M, N, x, ldx, q, e, qt=None, et=None, stream=None):
+    _check(lib().sr_quantize_f8(f8_kind, dtype, M, N, _p(x), ldx, _p(q), _p(e), _p(qt), _p(et), _stream(stream)))
+
+
+def sr_linear_f8_scratch_bytes(M: int, N: int, K: int) -> int:
+    a = ctypes.c_size_t()
+    _check(lib().sr_linear_f8_scratch_bytes(M, N, K, ctypes.byref(a)))
+    return a.value
+
+
+def sr_linear_f8(dtype, act, M, N, K, xq, xe, wq, we, bias, y, scratch=None, stream=None):
+    _check(lib().sr_linear_f8(dtype, act, M, N, K, _p(xq), _p(xe), _p(wq), _p(we), _p(bias), _p(y), _p(scratch),
+                              _nbytes(scratch), _stream(stream)))
 
 
 def sr_profile_start(name_filter: str = "") -> None:

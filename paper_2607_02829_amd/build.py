@@ -15,7 +15,8 @@ BUILD = os.path.join(ROOT, "_build")
 
 SOURCES = ["select.hip", "routing.hip", "rowops.hip", "gemv.hip", "gemm.hip", "gemm_f32.hip", "attention.hip", "attention_f32.hip",
            "cross_attention.hip",
-           "edm.hip", "quant8.hip", "linear8.hip", "wgrad8.hip", "stack.cpp", "api.cpp", "profile.cpp"]
+           "edm.hip", "quant8.hip", "linear8.hip", "wgrad8.hip",
+           "rotary.hip", "dropout.hip", "residual_norm.hip", "quant_f8.hip", "linear_f8.hip", "stack.cpp", "api.cpp", "profile.cpp"]
 # Files whose floating-point results are part of a bit-exact contract (top-k score,
 # scatter rounding): no multiply-add contraction anywhere in them.
 NO_CONTRACT = {"select.hip", "routing.hip"}

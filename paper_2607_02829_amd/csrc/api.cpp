@@ -1,6 +1,7 @@
 // C ABI of libsr (declared and documented in include/sr.h): argument validation
 // on the host, then launches on the caller's stream.  Nothing is allocated here.
 #include <algorithm>
+#include <cmath>
 #include <cstdarg>
 #include <cstdlib>
 #include <cstdio>
@@ -9,6 +10,7 @@
 #include <vector>
 
 #include "../../include/sr.h"
+#include "block_ops.h"
 #include "edm.h"
 #include "profile.h"
 #include "quant8.h"
@@ -726,6 +728,266 @@ sr_status sr_weight_grad8(int32_t dtype, int32_t M, int32_t N, int32_t K, const 
   sr::ProfScope ps("weight_grad8", 2.0 * M * N * K,
                    (double)M * N * elt_of(dtype) + (double)M * K * 33 / 32 + (double)N * K * 4, st);
   return hip_status(sr::launch_wgrad8(dt, a, st), "weight_grad8");
+}
+
+namespace {
+#define SR_OPT(p, name)                                                                  \
+  do {                                                                                   \
+    if (p) SR_CHECK(aligned16(p), SR_EALIGN, "%s is not 16-byte aligned", name);         \
+  } while (0)
+
+int kernel_type(int32_t dtype) { return dtype == SR_BF16 ? sr::kBF16 : sr::kF32; }
+
+sr_status check_type(int32_t dtype, const char* what) {
+  SR_CHECK(dtype == SR_F32 || dtype == SR_BF16, SR_EDTYPE, "unknown %s %d", what, dtype);
+  return SR_OK;
+}
+
+sr_status check_drop(const sr_drop* d) {
+  SR_CHECK(d != nullptr, SR_EINVAL, "drop is NULL");
+  SR_CHECK(d->p >= 0.f && d->p <= 1.f, SR_EINVAL, "p=%g outside [0, 1]", (double)d->p);
+  SR_CHECK(d->group >= 0, SR_EINVAL, "group=%d must be >= 0", d->group);
+  SR_CHECK((reinterpret_cast<uintptr_t>(d->step_dev) & 7u) == 0, SR_EALIGN, "step_dev is not 8-byte aligned");
+  return SR_OK;
+}
+
+sr_status check_residual_norm(const sr_residual_norm* c) {
+  SR_CHECK(c != nullptr, SR_EINVAL, "cfg is NULL");
+  sr_status s = check_type(c->dtype, "dtype");
+  if (s != SR_OK) return s;
+  SR_CHECK(c->stream_dtype == SR_F32 || c->stream_dtype == c->dtype, SR_EDTYPE, "stream_dtype %d is neither SR_F32 nor dtype",
+           c->stream_dtype);
+  SR_CHECK(c->norm == SR_NORM_LAYER || c->norm == SR_NORM_RMS, SR_EINVAL, "unknown norm %d", c->norm);
+  SR_CHECK(c->post == 0 || c->post == 1, SR_EINVAL, "post must be 0 or 1");
+  SR_CHECK(c->B >= 1 && c->S >= 1 && c->D >= 1, SR_EINVAL, "sizes must be positive (B=%d S=%d D=%d)", c->B, c->S, c->D);
+  SR_CHECK(c->D <= sr::kMaxNormD, SR_EUNSUPPORTED, "D=%d > %d", c->D, sr::kMaxNormD);
+  SR_CHECK((int64_t)c->B * c->S < (1ll << 31), SR_EUNSUPPORTED, "2^31 rows or more are not supported (B=%d S=%d)", c->B, c->S);
+  SR_CHECK(c->eps > 0.f, SR_EINVAL, "eps must be > 0");
+  return check_drop(&c->drop);
+}
+
+sr_status residual_norm_args(const sr_residual_norm* c, const sr_residual_norm_params* w, sr::ResidualNorm* a) {
+  sr_status s = check_residual_norm(c);
+  if (s != SR_OK) return s;
+  SR_CHECK(w != nullptr, SR_EINVAL, "params is NULL");
+  for (const void* p : {w->post_w, w->post_b, w->res_scale, w->pre_w, w->pre_b})
+    SR_CHECK(aligned16(p), SR_EALIGN, "a parameter pointer is not 16-byte aligned");
+  for (const float* p : {w->gate, w->shift, w->scale}) {
+    SR_CHECK((reinterpret_cast<uintptr_t>(p) & 3u) == 0, SR_EALIGN, "gate, shift or scale is not 4-byte aligned");
+    SR_CHECK(!p || c->B == 1 || c->mod_stride >= c->D, SR_ESHAPE, "mod_stride=%lld < D=%d", (long long)c->mod_stride, c->D);
+  }
+  a->B = c->B; a->S = c->S; a->D = c->D;
+  a->norm = c->norm; a->post = c->post; a->eps = c->eps; a->mod_stride = c->B == 1 ? 0 : c->mod_stride;
+  a->drop = sr::drop_args(c->drop);
+  a->w = *w;
+  return SR_OK;
+}
+
+// codes of R rows of C values and their exponents fit the kernels' 31-bit offsets
+bool f8_fits(int64_t R, int64_t C) { return R * sr::f8_cols(C) < (1ll << 31); }
+
+sr_status check_linear_f8(int32_t M, int32_t N, int32_t K) {
+  SR_CHECK(M >= 1 && N >= 1 && K >= 1, SR_EINVAL, "sizes must be positive (M=%d N=%d K=%d)", M, N, K);
+  SR_CHECK(K <= 1 << 24, SR_EUNSUPPORTED, "K=%d > 2^24", K);
+  SR_CHECK(f8_fits(M, K) && f8_fits(N, K), SR_EUNSUPPORTED, "codes beyond 2 GiB are not supported (M=%d N=%d K=%d)", M, N, K);
+  return SR_OK;
+}
+}  // namespace
+
+sr_status sr_rotary(const sr_rotary_cfg* rot, int32_t inverse, int32_t dtype, int32_t B, int32_t S, int32_t heads,
+                    int32_t head_dim, const void* x, int64_t ldx, const int32_t* idx, int32_t idx_shared, void* y,
+                    int64_t ldy, void* stream) {
+  SR_CHECK(rot != nullptr, SR_EINVAL, "rot is NULL");
+  sr_status s = check_type(dtype, "dtype");
+  if (s != SR_OK) return s;
+  SR_CHECK(inverse == 0 || inverse == 1, SR_EINVAL, "inverse must be 0 or 1");
+  SR_CHECK(idx_shared == 0 || idx_shared == 1, SR_EINVAL, "idx_shared must be 0 or 1");
+  SR_CHECK(rot->layout == SR_ROT_HALVES || rot->layout == SR_ROT_NEIGHBOURS, SR_EINVAL, "unknown layout %d", rot->layout);
+  SR_CHECK(rot->axes >= 1 && rot->axes <= 3, SR_EINVAL, "axes=%d outside [1, 3]", rot->axes);
+  SR_CHECK(B >= 1 && S >= 1 && heads >= 1 && head_dim >= 1, SR_EINVAL,
+           "sizes must be positive (B=%d S=%d heads=%d head_dim=%d)", B, S, heads, head_dim);
+  SR_CHECK(head_dim <= 2 * sr::kMaxRotPairs, SR_EUNSUPPORTED, "head_dim=%d > %d", head_dim, 2 * sr::kMaxRotPairs);
+  const int64_t cols = (int64_t)heads * head_dim, rows = (int64_t)B * S;
+  SR_CHECK(cols <= 32768, SR_EUNSUPPORTED, "heads * head_dim = %lld > 32768", (long long)cols);
+  SR_CHECK(rows < (1ll << 31), SR_EUNSUPPORTED, "2^31 rows or more are not supported (B=%d S=%d)", B, S);
+  sr::Rotary a;
+  int64_t L = 1, P = 0;
+  for (int i = 0; i < rot->axes; ++i) {
+    SR_CHECK(rot->grid[i] >= 1 && rot->pairs[i] >= 0, SR_EINVAL, "axis %d: grid=%d must be >= 1, pairs=%d >= 0", i, rot->grid[i],
+             rot->pairs[i]);
+    SR_CHECK(std::isfinite(rot->origin[i]) && std::isfinite(rot->step[i]), SR_EINVAL, "axis %d: origin or step is not finite", i);
+    L *= rot->grid[i];
+    P += rot->pairs[i];
+    SR_CHECK(L < (1ll << 31), SR_EUNSUPPORTED, "a grid of 2^31 tokens or more is not supported");
+    a.grid[i] = rot->grid[i];
+    a.origin[i] = rot->origin[i];
+    a.step[i] = rot->step[i];
+  }
+  SR_CHECK(2 * P <= head_dim, SR_ESHAPE, "2 * %lld pairs > head_dim=%d", (long long)P, head_dim);
+  SR_CHECK(idx != nullptr || S <= L, SR_ESHAPE, "S=%d rows of a sample > %lld tokens of the grid", S, (long long)L);
+  SR_CHECK(ldx >= cols && ldy >= cols, SR_ESHAPE, "ldx=%lld or ldy=%lld < %lld channels", (long long)ldx, (long long)ldy,
+           (long long)cols);
+  SR_CHECK(rot->freqs != nullptr || (rot->base > 0 && std::isfinite(rot->base)), SR_EINVAL, "base must be > 0 and finite");
+  const uintptr_t elt = elt_of(dtype);
+  SR_CHECK(x != nullptr && y != nullptr, SR_EINVAL, "x or y is NULL");
+  SR_CHECK(((uintptr_t)x | (uintptr_t)y) % elt == 0, SR_EALIGN, "x or y is not aligned to its elements");
+  SR_CHECK((uintptr_t)idx % 4 == 0, SR_EALIGN, "idx is not 4-byte aligned");
+  SR_CHECK(x != y || ldx == ldy, SR_ESHAPE, "in place with ldx=%lld and ldy=%lld", (long long)ldx, (long long)ldy);
+  int p = 0;
+  for (int i = 0; i < 3; ++i) {
+    a.first[i] = p;
+    const int n = i < rot->axes ? rot->pairs[i] : 0;
+    for (int j = 0; j < n; ++j, ++p) {
+      a.freq[p] = rot->freqs ? rot->freqs[p] : std::pow(rot->base, -(double)j / n);
+      SR_CHECK(std::isfinite(a.freq[p]), SR_EINVAL, "the frequency of pair %d is not finite", p);
+    }
+  }
+  a.first[3] = p;
+  a.B = B; a.S = S; a.heads = heads; a.hd = head_dim;
+  a.axes = rot->axes;
+  a.neighbours = rot->layout == SR_ROT_NEIGHBOURS;
+  a.inverse = inverse; a.idx_shared = idx_shared;
+  a.x = x; a.y = y; a.idx = idx; a.ldx = ldx; a.ldy = ldy;
+  hipStream_t st = (hipStream_t)stream;
+  sr::ProfScope ps("rotary", 6.0 * rows * heads * (double)P, 2.0 * rows * cols * elt, st);
+  return hip_status(sr::launch_rotary(kernel_type(dtype), a, st), "rotary");
+}
+
+sr_status sr_dropout(const sr_drop* drop, int32_t dtype, int32_t M, int32_t N, const void* x, const void* resid, void* y,
+                     void* stream) {
+  sr_status s = check_type(dtype, "dtype");
+  if (s != SR_OK || (s = check_drop(drop)) != SR_OK) return s;
+  SR_CHECK(M >= 1 && N >= 1, SR_EINVAL, "sizes must be positive (M=%d N=%d)", M, N);
+  SR_PTR(x, "x");
+  SR_OPT(resid, "resid");
+  SR_PTR(y, "y");
+  sr::Dropout a;
+  a.M = M; a.N = N;
+  a.x = x; a.resid = resid; a.y = y;
+  a.drop = sr::drop_args(*drop);
+  hipStream_t st = (hipStream_t)stream;
+  sr::ProfScope ps("dropout", 0, (double)M * N * elt_of(dtype) * (resid ? 3 : 2), st);
+  return hip_status(sr::launch_dropout(kernel_type(dtype), a, st), "dropout");
+}
+
+sr_status sr_residual_norm_fwd(const sr_residual_norm* cfg, const sr_residual_norm_params* params, const void* x,
+                               const void* y, void* x1, void* u, uint8_t* uq, uint8_t* ue, float* stats, void* stream) {
+  sr::ResidualNorm a;
+  sr_status s = residual_norm_args(cfg, params, &a);
+  if (s != SR_OK) return s;
+  SR_PTR(x, "x");
+  SR_OPT(y, "y");
+  if (y) SR_PTR(x1, "x1");
+  SR_OPT(u, "u");
+  SR_CHECK((uq == nullptr) == (ue == nullptr), SR_EINVAL, "uq and ue go together");
+  SR_OPT(uq, "uq");
+  SR_OPT(ue, "ue");
+  SR_OPT(stats, "stats");
+  SR_CHECK(y || u || uq, SR_EINVAL, "nothing to compute: y, u and uq are NULL");
+  a.x = x; a.y = y; a.x1 = x1; a.u = u; a.uq = uq; a.ue = ue; a.stats = stats;
+  hipStream_t st = (hipStream_t)stream;
+  const double n = (double)a.B * a.S * a.D, e = elt_of(cfg->dtype), se = elt_of(cfg->stream_dtype);
+  sr::ProfScope ps("residual_norm_fwd", 0, n * (se + (y ? e + se : 0) + (u ? e : 0) + (uq ? 1 : 0)), st);
+  return hip_status(sr::launch_residual_norm_fwd(kernel_type(cfg->dtype), kernel_type(cfg->stream_dtype), a, st),
+                    "residual_norm_fwd");
+}
+
+sr_status sr_residual_norm_scratch_bytes(const sr_residual_norm* cfg, size_t* scratch_bytes) {
+  sr_status s = check_residual_norm(cfg);
+  if (s != SR_OK) return s;
+  SR_CHECK(scratch_bytes != nullptr, SR_EINVAL, "scratch_bytes is NULL");
+  *scratch_bytes = sr::residual_norm_scratch(cfg->B, cfg->S, cfg->D);
+  return SR_OK;
+}
+
+sr_status sr_residual_norm_bwd(const sr_residual_norm* cfg, const sr_residual_norm_params* params, const void* x1,
+                               const void* y, const float* stats, const void* dx1, const void* du, void* dx, void* dy,
+                               const sr_residual_norm_grads* grads, void* scratch, size_t scratch_bytes, void* stream) {
+  sr::ResidualNorm a;
+  sr_status s = residual_norm_args(cfg, params, &a);
+  if (s != SR_OK) return s;
+  SR_CHECK(dx1 || du, SR_EINVAL, "dx1 and du are NULL");
+  SR_CHECK((y == nullptr) == (dy == nullptr), SR_EINVAL, "y and dy go together");
+  if (du) SR_PTR(x1, "x1");
+  if (du || (y && cfg->post)) SR_PTR(stats, "stats");
+  SR_OPT(y, "y");
+  SR_OPT(dx1, "dx1");
+  SR_OPT(du, "du");
+  SR_PTR(dx, "dx");
+  SR_OPT(dy, "dy");
+  SR_CHECK(grads != nullptr, SR_EINVAL, "grads is NULL");
+  for (const float* p : {grads->post_w, grads->post_b, grads->res_scale, grads->pre_w, grads->pre_b, grads->gate,
+                         grads->shift, grads->scale})
+    SR_CHECK(aligned16(p), SR_EALIGN, "a gradient pointer is not 16-byte aligned");
+  const size_t need = sr::residual_norm_scratch(a.B, a.S, a.D);
+  SR_PTR(scratch, "scratch");
+  SR_CHECK(scratch_bytes >= need, SR_EWORKSPACE, "scratch buffer has %zu bytes, needs %zu", scratch_bytes, need);
+  a.x = x1; a.y = y; a.stats = const_cast<float*>(stats);
+  a.dx1 = dx1; a.du = du; a.dx = dx; a.dy = dy;
+  a.g = *grads;
+  a.part = (float*)scratch;
+  hipStream_t st = (hipStream_t)stream;
+  const double n = (double)a.B * a.S * a.D, e = elt_of(cfg->dtype), se = elt_of(cfg->stream_dtype);
+  sr::ProfScope ps("residual_norm_bwd", 0, n * ((dx1 ? se : 0) + (du ? se + e : 0) + se + (y ? 2 * e : 0)), st);
+  return hip_status(sr::launch_residual_norm_bwd(kernel_type(cfg->dtype), kernel_type(cfg->stream_dtype), a, st),
+                    "residual_norm_bwd");
+}
+
+sr_status sr_quantize_f8(int32_t f8_kind, int32_t dtype, int32_t M, int32_t N, const void* x, int64_t ldx, uint8_t* q,
+                         uint8_t* e, uint8_t* qt, uint8_t* et, void* stream) {
+  SR_CHECK(f8_kind == SR_F8_ROW || f8_kind == SR_F8_TILE, SR_EINVAL, "unknown kind %d", f8_kind);
+  sr_status s = check_type(dtype, "dtype");
+  if (s != SR_OK) return s;
+  SR_CHECK(M >= 1 && N >= 1, SR_EINVAL, "sizes must be positive (M=%d N=%d)", M, N);
+  SR_CHECK(f8_fits(M, N) && f8_fits(N, M), SR_EUNSUPPORTED, "codes beyond 2 GiB are not supported (M=%d N=%d)", M, N);
+  SR_CHECK(ldx >= N, SR_ESHAPE, "ldx=%lld < N=%d", (long long)ldx, N);
+  SR_CHECK((q == nullptr) == (e == nullptr) && (qt == nullptr) == (et == nullptr), SR_EINVAL,
+           "codes and their exponents go together");
+  SR_CHECK(q || qt, SR_EINVAL, "q and qt are NULL");
+  SR_CHECK(x != nullptr, SR_EINVAL, "x is NULL");
+  SR_CHECK((uintptr_t)x % elt_of(dtype) == 0, SR_EALIGN, "x is not aligned to its elements");
+  SR_OPT(q, "q");
+  SR_OPT(e, "e");
+  SR_OPT(qt, "qt");
+  SR_OPT(et, "et");
+  hipStream_t st = (hipStream_t)stream;
+  sr::ProfScope ps("quantize_f8", 0, (double)M * N * (elt_of(dtype) + (q ? 1 : 0) + (qt ? 1 : 0)), st);
+  return hip_status(sr::launch_quantize_f8(f8_kind, kernel_type(dtype), M, N, x, ldx, q, e, qt, et, st), "quantize_f8");
+}
+
+sr_status sr_linear_f8_scratch_bytes(int32_t M, int32_t N, int32_t K, size_t* scratch_bytes) {
+  sr_status s = check_linear_f8(M, N, K);
+  if (s != SR_OK) return s;
+  SR_CHECK(scratch_bytes != nullptr, SR_EINVAL, "scratch_bytes is NULL");
+  *scratch_bytes = sr::linear_f8_scratch(M, N, K);
+  return SR_OK;
+}
+
+sr_status sr_linear_f8(int32_t dtype, int32_t act, int32_t M, int32_t N, int32_t K, const uint8_t* xq, const uint8_t* xe,
+                       const uint8_t* wq, const uint8_t* we, const void* bias, void* y, void* scratch,
+                       size_t scratch_bytes, void* stream) {
+  sr_status s = check_type(dtype, "dtype");
+  if (s != SR_OK || (s = check_linear_f8(M, N, K)) != SR_OK) return s;
+  SR_CHECK(act == SR_ACT_NONE || act == SR_ACT_GELU, SR_EINVAL, "unknown activation %d", act);
+  SR_CHECK(fits31(M, N, (int64_t)elt_of(dtype)), SR_EUNSUPPORTED, "results beyond 2 GiB are not supported (M=%d N=%d)", M, N);
+  SR_PTR(xq, "xq");
+  SR_PTR(xe, "xe");
+  SR_PTR(wq, "wq");
+  SR_PTR(we, "we");
+  SR_OPT(bias, "bias");
+  SR_PTR(y, "y");
+  const size_t need = sr::linear_f8_scratch(M, N, K);
+  if (need) {
+    SR_PTR(scratch, "scratch");
+    SR_CHECK(scratch_bytes >= need, SR_EWORKSPACE, "scratch buffer has %zu bytes, needs %zu", scratch_bytes, need);
+  }
+  sr::LinearF8 a;
+  a.M = M; a.N = N; a.K = K;
+  a.xq = xq; a.xe = xe; a.wq = wq; a.we = we; a.bias = bias; a.y = y; a.act = act;
+  a.scratch = (float*)scratch;
+  hipStream_t st = (hipStream_t)stream;
+  sr::ProfScope ps("linear_f8", 2.0 * M * N * K, (double)M * K + (double)N * K + (double)M * N * elt_of(dtype), st);
+  return hip_status(sr::launch_linear_f8(kernel_type(dtype), a, st), "linear_f8");
 }
 
 sr_status sr_probe_mfma_rate(float* sink, double* tflops, void* stream) {

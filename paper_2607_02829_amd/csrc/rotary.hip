@@ -1,0 +1,189 @@
+// Rotary positions: every head of a row turns its channel pairs by the angles of the row's token (sr_rotary).
+//
+// A workgroup takes the rows of a few tokens.  Its threads first issue the loads of their channels, then form the
+// cosines and sines of all pairs of these tokens (in LDS, once for all heads), then turn and store.  The angle is a
+// 64-bit product, reduced to a quarter turn in 64 bits (a coordinate of 10^6 keeps 2^-33 of a turn), so that
+// 32-bit polynomials of |r| <= pi/4 finish it to the rounding of fp32.
+#include <algorithm>
+
+#include "block_ops.h"
+
+namespace sr {
+
+namespace {
+
+// (cos t, sin t): r = t - k pi/2 with pi/2 in two parts, Taylor polynomials of cos r and sin r (the first terms left
+// out are below 2^-30 of the results at pi/4), then the quadrant.
+SR_DEV float2 turn_of(double t) {
+  const double k = rint(t * 0.63661977236758134308);
+  const double rd = fma(-k, 6.123233995736766036e-17, fma(-k, 1.57079632679489655800, t));
+  const float r = (float)rd, z = r * r;
+  float s = fmaf(z, 2.7557319e-6f, -1.9841270e-4f);
+  s = fmaf(s, z, 8.3333333e-3f);
+  s = fmaf(s, z, -1.6666667e-1f);
+  s = fmaf(s * z, r, r);
+  float c = fmaf(z, -2.7557319e-7f, 2.4801587e-5f);
+  c = fmaf(c, z, -1.3888889e-3f);
+  c = fmaf(c, z, 4.1666667e-2f);
+  c = fmaf(c, z, -0.5f);
+  c = fmaf(c, z, 1.0f);
+  const int q = (int)(k - 4.0 * floor(k * 0.25));
+  const float a = q & 1 ? s : c, b = q & 1 ? c : s;
+  return float2{(q == 1 || q == 2) ? -a : a, q >= 2 ? -b : b};
+}
+
+constexpr int kThreads = 256, kUnroll = 4;
+
+template <typename T, int V>
+struct Pack {
+  T v[V];
+};
+template <>
+struct __attribute__((aligned(16))) Pack<bf16_t, 8> {
+  bf16_t v[8];
+};
+template <>
+struct __attribute__((aligned(16))) Pack<float, 4> {
+  float v[4];
+};
+
+// What is left of i after whole d's, and their number; magic = ceil(2^32 / d), exact for i d < 2^32.
+SR_DEV uint32_t quotient(uint32_t i, uint32_t magic, uint32_t d) { return d == 1 ? i : __umulhi(i, magic); }
+
+struct Units {
+  int tokens;         // of a workgroup
+  uint32_t per_head, per_token, rot;   // units of a head and of a row; those of a head that turn
+  uint32_t magic_head, magic_token;
+};
+
+// PAIRED: a unit turns V pairs, of channels c0 .. and c1 ..; otherwise V / 2 pairs of neighbours in V channels.
+template <typename T, int V, bool PAIRED>
+__global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary a, Units un) {
+  extern __shared__ float2 cs[];   // [tokens][P]
+  const int P = a.first[3];
+  const int64_t rows = (int64_t)a.B * a.S, row0 = (int64_t)blockIdx.x * un.tokens;
+  const uint32_t n = (uint32_t)un.tokens * un.per_token;
+  typedef Pack<T, V> Vec;
+  bool first = true;
+  for (uint32_t base = 0; base < n || first; base += kThreads * kUnroll) {
+    Vec lo[kUnroll], hi[kUnroll];
+    int64_t oy[kUnroll];
+    int c1[kUnroll], at[kUnroll];   // at: first pair in cs, -1: channels that do not turn, -2: nothing
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) {
+      const uint32_t i = base + threadIdx.x + kThreads * k;
+      const uint32_t t = quotient(i, un.magic_token, un.per_token), r = i - t * un.per_token;
+      const uint32_t h = quotient(r, un.magic_head, un.per_head), u = r - h * un.per_head;
+      at[k] = -2;
+      if (i < n && row0 + t < rows) {
+        int c0;
+        if (u < un.rot) {
+          const int p = (int)u * (PAIRED ? V : V / 2);
+          at[k] = (int)t * P + p;
+          c0 = a.neighbours ? 2 * p : p;
+          c1[k] = a.neighbours ? 1 : P;   // from c0
+        } else {
+          at[k] = -1;
+          c0 = 2 * P + (int)(u - un.rot) * V;
+          c1[k] = 0;
+        }
+        const T* xp = (const T*)a.x + (row0 + t) * a.ldx + (int64_t)h * a.hd + c0;
+        oy[k] = (row0 + t) * a.ldy + (int64_t)h * a.hd + c0;
+        lo[k] = *reinterpret_cast<const Vec*>(xp);
+        if (PAIRED && at[k] >= 0) hi[k] = *reinterpret_cast<const Vec*>(xp + c1[k]);
+      }
+    }
+    if (first) {
+      for (int i = threadIdx.x; i < un.tokens * P; i += kThreads) {
+        const int t = i / P, p = i - t * P;
+        const int64_t row = row0 + t;
+        if (row < rows) {
+          const int b = (int)(row / a.S), s = (int)(row - (int64_t)b * a.S);
+          int l = a.idx ? a.idx[(size_t)(a.idx_shared ? 0 : b) * a.S + s] : s;
+          int place[3] = {l, 0, 0};
+          if (a.axes == 2) {
+            place[0] = l / a.grid[1];
+            place[1] = l - place[0] * a.grid[1];
+          } else if (a.axes == 3) {
+            const int q = l / a.grid[2];
+            place[2] = l - q * a.grid[2];
+            place[0] = q / a.grid[1];
+            place[1] = q - place[0] * a.grid[1];
+          }
+          const int ax = (p >= a.first[1]) + (p >= a.first[2]);
+          const double at_ax = ax == 0   ? fma(a.step[0], (double)place[0], a.origin[0])
+                               : ax == 1 ? fma(a.step[1], (double)place[1], a.origin[1])
+                                         : fma(a.step[2], (double)place[2], a.origin[2]);
+          float2 c = turn_of(at_ax * a.freq[p]);
+          if (a.inverse) c.y = -c.y;
+          cs[i] = c;
+        }
+      }
+      __syncthreads();
+      first = false;
+    }
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) {
+      if (at[k] == -2) continue;
+      T* yp = (T*)a.y + oy[k];
+      if (at[k] >= 0) {
+        if constexpr (PAIRED) {
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            const float2 c = cs[at[k] + j];
+            const float x0 = to_f32<T>(lo[k].v[j]), x1 = to_f32<T>(hi[k].v[j]);
+            lo[k].v[j] = from_f32<T>(fmaf(x0, c.x, -x1 * c.y));
+            hi[k].v[j] = from_f32<T>(fmaf(x1, c.x, x0 * c.y));
+          }
+          *reinterpret_cast<Vec*>(yp + c1[k]) = hi[k];
+        } else {
+#pragma unroll
+          for (int j = 0; j < V / 2; ++j) {
+            const float2 c = cs[at[k] + j];
+            const float x0 = to_f32<T>(lo[k].v[2 * j]), x1 = to_f32<T>(lo[k].v[2 * j + 1]);
+            lo[k].v[2 * j] = from_f32<T>(fmaf(x0, c.x, -x1 * c.y));
+            lo[k].v[2 * j + 1] = from_f32<T>(fmaf(x1, c.x, x0 * c.y));
+          }
+        }
+      }
+      *reinterpret_cast<Vec*>(yp) = lo[k];
+    }
+  }
+}
+
+template <typename T, int V, bool PAIRED>
+hipError_t run(const Rotary& a, hipStream_t st) {
+  const int P = a.first[3];
+  Units un;
+  un.rot = (uint32_t)(PAIRED ? P / V : 2 * P / V);
+  const bool copies = a.x != a.y;   // in place the channels that do not turn stay
+  un.per_head = un.rot + (copies ? (uint32_t)((a.hd - 2 * P) / V) : 0);
+  un.per_token = un.per_head * (uint32_t)a.heads;
+  if (un.per_token == 0) return hipSuccess;
+  // about four units a thread, 16 tokens at most
+  un.tokens = (int)std::min(16u, std::max(1u, kThreads * kUnroll / un.per_token));
+  un.magic_head = (uint32_t)(((1ull << 32) + un.per_head - 1) / un.per_head);
+  un.magic_token = (uint32_t)(((1ull << 32) + un.per_token - 1) / un.per_token);
+  const int64_t rows = (int64_t)a.B * a.S, wgs = (rows + un.tokens - 1) / un.tokens;
+  SR_LAUNCH((rotary_kernel<T, V, PAIRED>), dim3((unsigned)wgs), dim3(kThreads),
+            (uint32_t)(un.tokens * P * sizeof(float2)), st, a, un);
+  return hipGetLastError();
+}
+
+template <typename T, int V>
+hipError_t run_type(const Rotary& a, hipStream_t st) {
+  const int P = a.first[3];
+  auto whole = [](const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld * sizeof(T) % 16 == 0; };
+  // 16 bytes at a time where rows, heads and the turning channels start and end on them
+  if (whole(a.x, a.ldx) && whole(a.y, a.ldy) && a.hd % V == 0 && (a.neighbours ? 2 * P : P) % V == 0)
+    return a.neighbours ? run<T, V, false>(a, st) : run<T, V, true>(a, st);
+  return run<T, 1, true>(a, st);
+}
+
+}  // namespace
+
+hipError_t launch_rotary(int dtype, const Rotary& a, hipStream_t st) {
+  return dtype == kBF16 ? run_type<bf16_t, 8>(a, st) : run_type<float, 4>(a, st);
+}
+
+}  // namespace sr

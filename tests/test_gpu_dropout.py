@@ -1,0 +1,114 @@
+"""sr_dropout against its 64-bit form: which values stay is exact; those are resid + x f with the product and the
+sum in fp32 (2^-24 of each) and one rounding to the storage type."""
+import numpy as np
+import pytest
+
+from oracle import block_ops as ob
+from paper_2607_02829_amd import abi
+
+pytestmark = pytest.mark.gpu
+
+BIG = (1 << 63) + 12345
+
+
+def _run(M, N, p, dtype, resid, seed=3, step=4, first_row=0, group=0, step_dev=None, inplace=None):
+    import torch
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    g = torch.Generator().manual_seed(M * 7919 + N)
+    x = torch.randn((M, N), generator=g).to(dt)
+    r = torch.randn((M, N), generator=g).to(dt) if resid else None
+    xd, rd = x.cuda(), None if r is None else r.cuda()
+    buf = torch.full((M * N + 16,), 55.0, dtype=dt, device="cuda")
+    y = {"x": xd, "resid": rd}.get(inplace)
+    y = buf[:M * N].view(M, N) if y is None else y
+    d = abi.SrDrop(p=p, seed=seed, step=step, first_row=first_row, group=group,
+                   step_dev=None if step_dev is None else step_dev.data_ptr())
+    abi.sr_dropout(d, abi.SR_BF16 if dtype == "bf16" else abi.SR_F32, M, N, xd, rd, y)
+    out = y.cpu()
+    assert (buf[M * N:] == 55).all()
+    extra = 0 if step_dev is None else int(step_dev.item())
+    keep = ob.drop_keep(M, N, p, seed, step + extra, first_row, group)
+    f = ob.drop_factor(p)
+    kept = np.where(keep, x.double().numpy() * f, 0.0)
+    want = kept + (r.double().numpy() if resid else 0.0)
+    got = out.double().numpy()
+    eps = torch.finfo(dt).eps / 2
+    assert (np.abs(got - want) <= eps * np.abs(want) + 2.0 ** -23 * (np.abs(kept) + np.abs(want))).all()
+    gone = ~keep
+    assert np.array_equal(got[gone], r.double().numpy()[gone] if resid else np.zeros(gone.sum()))
+    assert (got[keep] != 0).any() or not keep.any()
+    return out
+
+
+@pytest.mark.parametrize("M,N", [(1, 1), (1, 7), (3, 8), (5, 1), (33, 277), (64, 256), (7, 1024), (1000, 66)])
+@pytest.mark.parametrize("dtype,resid,p", [("bf16", False, 0.1), ("bf16", True, 0.5), ("f32", True, 0.25), ("f32", False, 0.9)])
+@pytest.mark.parametrize("group", [0, 1, 3])
+def test_dropout(M, N, dtype, resid, p, group):
+    _run(M, N, p, dtype, resid, group=group)
+
+
+@pytest.mark.parametrize("first_row", [1, 2, 3, (1 << 40) + 1, (1 << 62) + 3])   # draws that start inside a word, far ones
+@pytest.mark.parametrize("N", [13, 16, 18])
+def test_first_row(first_row, N):
+    for group in (0, 5):
+        _run(21, N, 0.3, "f32", True, seed=BIG, step=2 ** 64 - 2, first_row=first_row, group=group)
+
+
+def test_all_and_nothing():
+    for dtype in ("bf16", "f32"):
+        for group in (0, 2):
+            _run(9, 40, 0.0, dtype, True, group=group)
+            _run(9, 40, 1.0, dtype, True, group=group)
+            _run(9, 40, 2.0 ** -18, dtype, False, group=group)     # below the draws' resolution: nothing is dropped
+
+
+def test_in_place_and_a_step_from_memory():
+    import torch
+    for where in ("x", "resid"):
+        _run(17, 72, 0.2, "bf16", True, inplace=where)
+    s = torch.tensor([6], dtype=torch.int64, device="cuda")
+    a = _run(17, 72, 0.2, "bf16", True, step_dev=s)
+    assert not torch.equal(a, _run(17, 72, 0.2, "bf16", True))
+    assert torch.equal(a, _run(17, 72, 0.2, "bf16", True, step=10))
+
+
+def test_dropped_values_do_not_count():
+    import torch
+    for group in (0, 1):
+        keep = ob.drop_keep(40, 24, 0.5, 1, 2, group=group)
+        x = torch.where(torch.from_numpy(keep), 1.0, float("nan"))
+        y = torch.empty((40, 24), device="cuda")
+        abi.sr_dropout(abi.SrDrop(p=0.5, seed=1, step=2, group=group), abi.SR_F32, 40, 24, x.cuda(), None, y)
+        assert torch.equal(y.cpu(), torch.from_numpy(keep).float() * 2)
+
+
+def test_more_than_2_31_draws():
+    # the last rows of a tensor of 2^31 + elements draw as their number says
+    import torch
+    M, N = (1 << 21) + 3, 1024
+    x = torch.ones((M, N), dtype=torch.bfloat16, device="cuda")
+    abi.sr_dropout(abi.SrDrop(p=0.25, seed=8, step=1), abi.SR_BF16, M, N, x, None, x)
+    for r0 in (0, (1 << 21) - 2):
+        keep = ob.drop_keep(4, N, 0.25, 8, 1, first_row=r0)
+        assert np.array_equal((x[r0:r0 + 4].float() != 0).cpu().numpy(), keep)
+
+
+def test_a_replayed_graph_draws_anew():
+    import torch
+    x = torch.ones((64, 256), device="cuda")
+    y, step = torch.empty_like(x), torch.zeros(1, dtype=torch.int64, device="cuda")
+    d = abi.SrDrop(p=0.5, seed=4, step=10, step_dev=step.data_ptr())
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        abi.sr_dropout(d, abi.SR_F32, 64, 256, x, None, y)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        abi.sr_dropout(d, abi.SR_F32, 64, 256, x, None, y)
+        step += 1
+    step.zero_()
+    for k in range(4):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert np.array_equal((y != 0).cpu().numpy(), ob.drop_keep(64, 256, 0.5, 4, 10 + k)), k
+        assert int(step) == k + 1

@@ -1,0 +1,116 @@
+"""sr_rotary against its 64-bit form.  Tolerance: one rounding to the storage type (half a step of the result), and in
+fp32 the sine and cosine (2^-23 each, polynomial and rounding together) and three roundings of products of both channels:
+(|x0| + |x1|) 2^-21; the angle in 64 bits is off by at most a few units of its own rounding, |t| 2^-50."""
+import numpy as np
+import pytest
+
+from oracle import block_ops as ob
+from paper_2607_02829_amd import abi
+
+pytestmark = pytest.mark.gpu
+
+CASES = [
+    # B, S, heads, hd, grid, pairs, neighbours, routed, inverse, dtype, extra columns, frame
+    (1, 1, 1, 2, [1], [1], False, False, 0, "bf16", 0, 0),
+    (1, 1, 16, 64, [4, 16, 32], [8, 12, 12], False, False, 0, "bf16", 0, 7),
+    (2, 90, 32, 64, [90, 180], [16, 16], False, True, 0, "bf16", 0, 0),
+    (2, 33, 4, 128, [3, 5, 7], [16, 24, 24], True, True, 1, "bf16", 512, 0),
+    (3, 20, 5, 80, [4, 5], [8, 8], False, False, 1, "bf16", 8, -3),          # channels that do not turn
+    (3, 20, 5, 80, [4, 5], [8, 8], True, False, 0, "f32", 4, 1),
+    (1, 17, 3, 30, [17], [15], False, False, 0, "bf16", 0, 1000000),         # odd strides, a far position
+    (2, 13, 7, 33, [13], [11], True, False, 0, "bf16", 1, 0),                # an odd head: by element
+    (2, 13, 7, 33, [13], [11], False, True, 1, "f32", 3, 123456),
+    (1, 40, 2, 256, [2, 4, 5], [40, 48, 40], False, False, 0, "f32", 0, 0),
+    (1, 9, 128, 256, [9], [128], False, False, 0, "bf16", 0, 0),             # the widest row
+    (1, 700, 1, 8, [700], [4], True, False, 0, "bf16", 0, 0),                # many tokens of few channels
+    (4, 6, 3, 64, [2, 3], [0, 32], False, False, 0, "bf16", 0, 0),           # an axis without pairs
+    (1, 5, 3, 64, [5], [0], False, False, 0, "bf16", 0, 0),                  # nothing turns
+]
+
+
+def _check(got, x, idx, c, **kw):
+    import torch
+    B, S, H, hd, grid, pairs, nb, _, inv, dtype, _, frame = c
+    kw.setdefault("origin", [float(frame)] + [0.0] * (len(grid) - 1))
+    want, t = ob.rotary(x, idx, grid, pairs, nb, inverse=bool(inv), **kw)
+    eps = torch.finfo(torch.bfloat16 if dtype == "bf16" else torch.float32).eps / 2
+    P = sum(pairs)
+    mag = np.abs(x)
+    lo, hi = (slice(0, 2 * P, 2), slice(1, 2 * P, 2)) if nb else (slice(0, P), slice(P, 2 * P))
+    both = mag[..., lo] + mag[..., hi]
+    fp = np.zeros_like(mag)
+    fp[..., lo] = fp[..., hi] = both
+    tol = eps * np.abs(want) + fp * (2.0 ** -21 + t * 2.0 ** -50)
+    assert (np.abs(got - want) <= tol).all(), float((np.abs(got - want) / np.maximum(tol, 1e-300)).max())
+
+
+@pytest.mark.parametrize("c", CASES, ids=lambda c: "-".join(map(str, c)).replace(" ", ""))
+@pytest.mark.parametrize("inplace", [False, True])
+def test_rotary(c, inplace):
+    import torch
+    B, S, H, hd, grid, pairs, nb, routed, inv, dtype, extra, frame = c
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    g = torch.Generator().manual_seed(5)
+    n, ld = H * hd, H * hd + extra
+    x = torch.randn((B * S, ld), generator=g).to(dt)
+    idx = torch.stack([torch.randperm(int(np.prod(grid)), generator=g)[:S].sort().values for _ in range(B)]).int() if routed else None
+    rot = abi.SrRotary(grid, pairs, abi.SR_ROT_NEIGHBOURS if nb else abi.SR_ROT_HALVES,
+                       origin=[float(frame)] + [0.0] * (len(grid) - 1))
+    xd = x.cuda()
+    y = xd if inplace else torch.full((B * S + 1, ld), 77.0, dtype=dt, device="cuda")
+    abi.sr_rotary(rot, inv, abi.SR_BF16 if dtype == "bf16" else abi.SR_F32, B, S, H, hd, xd, ld,
+                  None if idx is None else idx.cuda(), 0, y, ld)
+    out = y.cpu()
+    rest = x if inplace else torch.full_like(x, 77.0)
+    assert torch.equal(out[:B * S, n:], rest[:, n:])             # columns behind the heads stay
+    if not inplace:
+        assert torch.equal(out[B * S], torch.full((ld,), 77.0, dtype=dt)) and torch.equal(xd.cpu(), x)
+    got = out[:B * S, :n].double().numpy().reshape(B, S, H, hd)
+    _check(got, x[:, :n].double().numpy().reshape(B, S, H, hd), None if idx is None else idx.numpy(), c)
+    if 2 * sum(pairs) < hd:
+        p2 = 2 * sum(pairs)
+        assert torch.equal(out[:B * S, :n].view(-1, H, hd)[..., p2:], x[:, :n].reshape(-1, H, hd)[..., p2:])
+
+
+def test_shared_indices_repeats_and_given_frequencies():
+    import torch
+    c = (3, 6, 2, 16, [5, 9], [3, 5], False, True, 0, "f32", 0, 0)
+    g = torch.Generator().manual_seed(9)
+    x = torch.randn((18, 32), generator=g)
+    idx = torch.tensor([[44, 0, 7, 7, 44, 3]], dtype=torch.int32)
+    freqs = [2 * np.pi * k / 9 for k in range(8)]                # whole turns around the second axis
+    rot = abi.SrRotary([5, 9], [3, 5], origin=[-0.5, 2.25], step=[0.25, -3.0], freqs=freqs)
+    y = torch.empty((18, 32), device="cuda")
+    abi.sr_rotary(rot, 0, abi.SR_F32, 3, 6, 2, 16, x.cuda(), 32, idx.cuda(), 1, y, 32)
+    _check(y.cpu().double().numpy().reshape(3, 6, 2, 16), x.double().numpy().reshape(3, 6, 2, 16), idx.numpy(), c,
+           origin=[-0.5, 2.25], step=[0.25, -3.0], freqs=freqs)
+
+
+def test_unaligned_rows_and_a_window_of_qkv():
+    # the queries and keys of q | k | v rows in place, and a view that starts off 16 bytes
+    import torch
+    g = torch.Generator().manual_seed(2)
+    qkv = torch.randn((2 * 10, 3 * 128), generator=g).bfloat16()
+    d = qkv.cuda()
+    rot = abi.SrRotary([2, 5], [16, 16])
+    abi.sr_rotary(rot, 0, abi.SR_BF16, 2, 10, 4, 64, d, 384, None, 0, d, 384)
+    c = (2, 10, 4, 64, [2, 5], [16, 16], False, False, 0, "bf16", 0, 0)
+    _check(d[:, :256].cpu().double().numpy().reshape(2, 10, 4, 64), qkv[:, :256].double().numpy().reshape(2, 10, 4, 64), None, c)
+    assert torch.equal(d[:, 256:].cpu(), qkv[:, 256:])
+    flat = torch.randn(1 + 20 * 256, generator=g).bfloat16()
+    f, y = flat.cuda(), torch.zeros(20 * 256 + 3, dtype=torch.bfloat16, device="cuda")
+    abi.sr_rotary(rot, 0, abi.SR_BF16, 2, 10, 4, 64, f[1:], 256, None, 0, y[3:], 256)
+    _check(y[3:].cpu().double().numpy().reshape(2, 10, 4, 64), flat[1:].double().numpy().reshape(2, 10, 4, 64), None, c)
+    assert (y[:3] == 0).all()
+
+
+def test_inverse_is_the_gradient():
+    import torch
+    g = torch.Generator().manual_seed(3)
+    x, dy = torch.randn((12, 64), generator=g), torch.randn((12, 64), generator=g)
+    rot = abi.SrRotary([3, 4], [10, 20], abi.SR_ROT_NEIGHBOURS)
+    y, dx = torch.empty((12, 64), device="cuda"), torch.empty((12, 64), device="cuda")
+    abi.sr_rotary(rot, 0, abi.SR_F32, 1, 12, 1, 64, x.cuda(), 64, None, 0, y, 64)
+    abi.sr_rotary(rot, 1, abi.SR_F32, 1, 12, 1, 64, dy.cuda(), 64, None, 0, dx, 64)
+    a, b = float((y.double().cpu() * dy.double()).sum()), float((x.double() * dx.double().cpu()).sum())
+    assert abs(a - b) <= 2.0 ** -20 * float((x.abs() * dy.abs()).sum()) * 2
