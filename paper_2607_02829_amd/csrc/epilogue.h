@@ -57,8 +57,9 @@ SR_DEV float gelu_f(float z) {
 }
 // z Phi(z) as max(z, 0) - |z| Phi(-|z|), with the limits at the infinities (a finite |z| times a Phi of 0), for layers
 // that round z and GELU(z) once together.
+template <int DEG>
 SR_DEV float gelu_lim(float z) {
-  return fmaf(-fminf(fabsf(z), 3.4028234663852886e38f), half_erfc_of<9>(z, z * z), fmaxf(z, 0.f));
+  return fmaf(-fminf(fabsf(z), 3.4028234663852886e38f), half_erfc_of<DEG>(z, z * z), fmaxf(z, 0.f));
 }
 template <int DEG>
 SR_DEV float gelu_grad_f(float z) {

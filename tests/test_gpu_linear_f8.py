@@ -132,11 +132,11 @@ def _check(got, z, P, K, dtype, act=0):
     assert np.isfinite(got).all()
     tol = P * (7 * 2.0 ** -13 if dtype == "bf16" else (K / 8 + 16) * U)
     want = z
-    if act:   # the derivative of GELU is at most 1.13; its fit is good to 4e-7 of the value, 2e-5 of z Phi(-|z|) in the tails
+    if act:   # the derivative of GELU is at most 1.13; its fit is good to 4e-7 of the value and 5e-5 of z Phi(-|z|)
         zt = torch.from_numpy(z)
         phi = torch.special.ndtr(-zt.abs()).numpy()
         want = z * torch.special.ndtr(zt).numpy()
-        tol = 1.13 * tol + 4e-7 * np.abs(want) + 2e-5 * np.abs(z) * phi
+        tol = 1.13 * tol + 4e-7 * np.abs(want) + 5e-5 * np.abs(z) * phi
     err = np.abs(got - want)
     tol = tol * (1 + 2.0 ** -7) + torch.finfo(_dt(dtype)).eps / 2 * np.abs(want) + 1e-37
     assert (err <= tol).all(), float((err / tol).max())
