@@ -39,6 +39,20 @@ SR_DEV uint64_t drop_word(uint64_t key, uint64_t w) { return drop_mix(key + (w +
 SR_DEV bool drop_keep1(uint64_t key, uint64_t e, uint32_t thresh) {
   return ((uint32_t)(drop_word(key, e >> 2) >> (16 * (uint32_t)(e & 3))) & 0xFFFFu) >= thresh;
 }
+// Bit j: draw e + j is kept, j = 0 .. 3.  One word of the generator where e is a multiple of four, else two.
+SR_DEV uint32_t drop_keep4(uint64_t key, uint64_t e, uint32_t thresh) {
+  uint64_t v = drop_word(key, e >> 2);
+  const uint32_t sh = 16 * (uint32_t)(e & 3);
+  if (sh) v = v >> sh | drop_word(key, (e >> 2) + 1) << (64 - sh);
+  const uint32_t w[2] = {(uint32_t)v, (uint32_t)(v >> 32)};
+  uint32_t keep = 0;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    keep |= (uint32_t)((w[j] & 0xFFFFu) >= thresh) << (2 * j);
+    keep |= (uint32_t)((w[j] >> 16) >= thresh) << (2 * j + 1);
+  }
+  return keep;
+}
 // Bit j: draw e + j is kept, j = 0 .. 7.  Two words of the generator where e is a multiple of four, else three.
 SR_DEV uint32_t drop_keep8(uint64_t key, uint64_t e, uint32_t thresh) {
   uint64_t lo = drop_word(key, e >> 2), hi = drop_word(key, (e >> 2) + 1);

@@ -1,7 +1,7 @@
 // The residual step between two branches (sr_residual_norm_fwd / _bwd): norm of the branch output, dropout, gate and
 // residual scale, the sum, and the next branch's norm, in one pass over the rows per direction.
 //
-// A row lives in the registers of a team of LPR lanes, NV runs of eight channels each, so every tensor is read once and the
+// A row lives in the registers of a team of LPR lanes, NV runs of four channels each, so every tensor is read once and the
 // deviations are summed from values whose mean is already taken off.  The backward keeps four column sums per
 // channel in registers while its team walks the rows of one sample:
 //   S1 = sum du,  S2 = sum du v,  S3 = sum d,  S4 = sum d n     v = Norm(x1), n = Norm(y) (or y), d = keep f (dx1 + ..)
@@ -17,55 +17,97 @@ namespace sr {
 
 namespace {
 
-// Eight channels c .. c + 7 of a row of D as fp32; `fill` past the row, where the row is absent (!on) or p is NULL.
-// vec: every such run starts on 16 bytes and lies inside the row or past it.
+// Rows of a tensor as a raw buffer: the rows of a workgroup's teams from `row` on, `rows` of them.  What lies past them, or
+// past a row (kPast), reads as zero and is not written, so neither needs a branch; a NULL tensor has no rows.
+constexpr uint32_t kPast = 0x20000000u;   // in elements: 2^30 bytes or 2^31
 template <typename T>
-SR_DEV void get8(const T* p, int c, int D, bool vec, bool on, float fill, float (&v)[8]) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = fill;
-  if (!on || !p || c >= D) return;
-  p += c;
-  if (!vec) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (c + j < D) v[j] = to_f32<T>(p[j]);
-  } else if constexpr (sizeof(T) == 2) {
-    const i32x4 w = *reinterpret_cast<const i32x4*>(p);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      v[2 * j] = __uint_as_float((uint32_t)w[j] << 16);
-      v[2 * j + 1] = __uint_as_float((uint32_t)w[j] & 0xFFFF0000u);
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const f32x4 w = *reinterpret_cast<const f32x4*>(p + 4 * j);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[4 * j + i] = w[i];
-    }
-  }
-}
-template <typename T>
-SR_DEV void put8(T* p, int c, int D, bool vec, const float (&v)[8]) {
-  if (c >= D) return;
-  p += c;
-  if (!vec) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (c + j < D) p[j] = from_f32<T>(v[j]);
-  } else if constexpr (sizeof(T) == 2) {
-    i32x4 w;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = (int)f2bf2(v[2 * j], v[2 * j + 1]);
-    *reinterpret_cast<i32x4*>(p) = w;
-  } else {
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-      *reinterpret_cast<f32x4*>(p + 4 * j) = f32x4{v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
-  }
+SR_DEV __amdgpu_buffer_rsrc_t rows_of(const void* p, int64_t row, int rows, int D) {
+  return make_rsrc((const T*)p + row * D, p ? (uint32_t)rows * (uint32_t)D * (uint32_t)sizeof(T) : 0u);
 }
 
-// Sums over the LPR lanes of a team (16, 32 or 64 neighbouring lanes, or whole waves).
+// Four channels as they lie in memory, so that they can be on their way while the row before is computed.  off: element
+// offset of the first; without VEC runs of four may start anywhere and end past the row, left: channels up to its end.
+template <typename T, bool VEC>
+struct Four;
+template <bool VEC>
+struct Four<float, VEC> {
+  f32x4 r;
+  SR_DEV void load(__amdgpu_buffer_rsrc_t b, uint32_t off, int left) {
+    if constexpr (VEC) {
+      r = __builtin_bit_cast(f32x4, buf_load16(b, off * 4));
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        r[j] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(b, (j < left ? off + j : kPast) * 4, 0, 0));
+    }
+  }
+  SR_DEV void fill(float v) { r = f32x4{v, v, v, v}; }
+  SR_DEV float at(int j) const { return r[j]; }
+};
+template <bool VEC>
+struct Four<bf16_t, VEC> {
+  i32x2 r;
+  SR_DEV void load(__amdgpu_buffer_rsrc_t b, uint32_t off, int left) {
+    if constexpr (VEC) {
+      r = buf_load8(b, off * 2);
+    } else {
+      uint32_t h[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        h[j] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(b, (j < left ? off + j : kPast) * 2, 0, 0);
+      r = i32x2{(int)(h[0] | h[1] << 16), (int)(h[2] | h[3] << 16)};
+    }
+  }
+  SR_DEV void fill(float v) {
+    const int f = (int)f2bf2(v, v);
+    r = i32x2{f, f};
+  }
+  SR_DEV float at(int j) const { return __uint_as_float(j & 1 ? (uint32_t)r[j / 2] & 0xFFFF0000u : (uint32_t)r[j / 2] << 16); }
+};
+template <typename T, bool VEC>
+SR_DEV void put4(__amdgpu_buffer_rsrc_t b, uint32_t off, int left, const float (&v)[4]) {
+  if constexpr (VEC && sizeof(T) == 2) {
+    i32x2 w;
+    w[0] = (int)f2bf2(v[0], v[1]);
+    w[1] = (int)f2bf2(v[2], v[3]);
+    __builtin_amdgcn_raw_buffer_store_b64(w, b, off * 2, 0, 0);
+  } else if constexpr (VEC) {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i32x4, f32x4{v[0], v[1], v[2], v[3]}), b, off * 4, 0, 0);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t o = (j < left ? off + j : kPast) * (uint32_t)sizeof(T);
+      if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16((short)f2bf(v[j]), b, o, 0, 0);
+      else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(int, v[j]), b, o, 0, 0);
+    }
+  }
+}
+// A parameter's channels ([D], or a sample's row of it), `fill` where it is NULL.
+template <typename T, bool VEC>
+SR_DEV Four<T, VEC> param4(const void* p, int D, uint32_t c, int left, float fill) {
+  Four<T, VEC> v;
+  if (p) v.load(rows_of<T>(p, 0, 1, D), c, left);
+  else v.fill(fill);
+  return v;
+}
+// The same of gate, shift and scale, whose rows need not start on 16 bytes.
+template <bool VEC>
+SR_DEV Four<float, VEC> mod4(const float* p, int D, uint32_t c, int left, bool aligned, float fill) {
+  Four<float, VEC> v;
+  v.fill(fill);
+  if (!p) return v;
+  const __amdgpu_buffer_rsrc_t b = rows_of<float>(p, 0, 1, D);
+  if (aligned) {
+    v.load(b, c, left);
+  } else {
+    Four<float, false> w;
+    w.load(b, c, left);
+    v.r = w.r;
+  }
+  return v;
+}
+
+// Sums over the LPR lanes of a team (32 neighbouring lanes, or whole waves).
 template <int LPR>
 SR_DEV float lanes_sum(float v) {
   if constexpr (LPR >= 64) return wave_sum(v);
@@ -73,11 +115,8 @@ SR_DEV float lanes_sum(float v) {
   v += dppf<0x4E>(v);
   v += dppf<0x141>(v);
   v += dppf<0x140>(v);
-  if constexpr (LPR == 32) {
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-  }
-  return v;
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
 template <int LPR>
@@ -117,121 +156,166 @@ struct TeamSum {
 
 // z -> Norm(z) in place, with the row's mean and reciprocal deviation; channels past D come out as zeros.
 template <int LPR, int NV>
-SR_DEV void norm_row(float (&z)[NV][8], const int (&c)[NV], int D, bool layer, float eps, TeamSum<LPR>& sum, float& mean,
-                     float& rstd) {
+SR_DEV void norm_row(float (&z)[NV][4], const int (&left)[NV], float rD, bool layer, float eps, TeamSum<LPR>& sum,
+                     float& mean, float& rstd) {
   mean = 0.f;
   if (layer) {
     float s = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s += z[i][j];
+      for (int j = 0; j < 4; ++j) s += z[i][j];
     sum(s);
-    mean = s / (float)D;
+    mean = s * rD;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) z[i][j] = c[i] + j < D ? z[i][j] - mean : 0.f;
+      for (int j = 0; j < 4; ++j) z[i][j] = j < left[i] ? z[i][j] - mean : 0.f;
   }
   float q = 0.f;
 #pragma unroll
   for (int i = 0; i < NV; ++i)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) q = fmaf(z[i][j], z[i][j], q);
+    for (int j = 0; j < 4; ++j) q = fmaf(z[i][j], z[i][j], q);
   sum(q);
-  rstd = 1.0f / sqrtf(q / (float)D + eps);
+  rstd = 1.0f / sqrtf(fmaf(q, rD, eps));
 #pragma unroll
   for (int i = 0; i < NV; ++i)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) z[i][j] *= rstd;
+    for (int j = 0; j < 4; ++j) z[i][j] *= rstd;
 }
 
-// Bit j: channel c + j of the row keeps its value.
+// Bit j: channel c + j of the row keeps its value (c a multiple of four).
 SR_DEV uint32_t keep_of(const DropArgs& d, uint64_t key, int64_t row, int D, int c) {
   const uint64_t r = d.first_row + (uint64_t)row;
-  if (d.group) return drop_keep1(key, r / (uint64_t)d.group, d.thresh) ? 0xFFu : 0u;
-  return drop_keep8(key, r * (uint64_t)D + (uint64_t)c, d.thresh);
+  if (d.group) return drop_keep1(key, r / (uint64_t)d.group, d.thresh) ? 0xFu : 0u;
+  return drop_keep4(key, r * (uint64_t)D + (uint64_t)c, d.thresh);
 }
 
-struct Flags {
-  bool vec;      // rows of every tensor and the parameters start on 16 bytes
-  bool modvec;   // gate, shift and scale too
+// A thread's channels: first of each run, its offset from a workgroup's first row, and the channels from it to the row's end
+// (0 or less: none; with VEC 4 or more otherwise).
+template <int LPR, int NV>
+struct Place {
+  uint32_t c[NV], off[NV];
+  int left[NV];
+  SR_DEV Place(int t, int team, int D) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int k = (i * LPR + t) * 4;
+      left[i] = D - k;
+      c[i] = k < D ? (uint32_t)k : kPast;
+      off[i] = k < D ? (uint32_t)(team * D + k) : kPast;
+    }
+  }
 };
 
-template <typename T, typename X, int LPR, int NV>
-__global__ __launch_bounds__(threads_of<LPR>()) void residual_norm_fwd_kernel(ResidualNorm a, Flags f) {
+// Workgroup (b, k): rows k R .. of sample b, a team every TEAMS-th of them; the next row's values are on their way while
+// one is computed.  A sample's parameters become one factor and one summand per channel and norm:
+//   x1 = x + keep (n w1 + b1),  w1 = f gate res_scale post_w, b1 alike;   u = v w2 + b2,  w2 = (1 + scale) pre_w, ..
+template <typename T, typename X, int LPR, int NV, bool VEC>
+__global__ __launch_bounds__(threads_of<LPR>()) void residual_norm_fwd_kernel(ResidualNorm a, bool modvec, int chunks) {
   constexpr int NT = threads_of<LPR>(), TEAMS = NT / LPR;
   __shared__ float slots[2][2][16];
   TeamSum<LPR> sum{slots};
-  const int t = threadIdx.x % LPR, team = threadIdx.x / LPR, D = a.D;
+  const int t = threadIdx.x % LPR, team = LPR < 64 ? (int)threadIdx.x / LPR : wave_index() / (LPR / 64 > 0 ? LPR / 64 : 1), D = a.D;
   const int64_t M = (int64_t)a.B * a.S;
-  const bool layer = a.norm == SR_NORM_LAYER, drops = a.y && a.drop.thresh;
+  const int b = (int)(blockIdx.x / (unsigned)chunks), k = (int)(blockIdx.x - (unsigned)b * (unsigned)chunks);
+  const int R = (a.S + chunks - 1) / chunks, s0 = (int)min((long)k * R, (long)a.S), s1 = min(a.S - s0, R) + s0;
+  const bool layer = a.norm == SR_NORM_LAYER, drops = a.y && a.drop.thresh, next = a.u || a.uq;
+  const float rD = 1.0f / (float)D;
+  const Place<LPR, NV> at(t, team, D);
+  Four<X, VEC> xr[NV];
+  Four<T, VEC> yr[NV];
+  auto load = [&](int sb) {
+    const int rows = min(TEAMS, s1 - sb);
+    const int64_t row0 = (int64_t)b * a.S + sb;
+    const __amdgpu_buffer_rsrc_t bx = rows_of<X>(a.x, row0, rows, D), by = rows_of<T>(a.y, row0, rows, D);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      xr[i].load(bx, at.off[i], at.left[i]);
+      yr[i].load(by, at.off[i], at.left[i]);
+    }
+  };
+  if (s0 < s1) load(s0);
   const uint64_t key = drops ? drop_key(a.drop) : 0;
-  int c[NV];
+  float w1[NV][4], b1[NV][4], w2[NV][4], b2[NV][4];
+  {
+    auto mod = [&](const float* p) { return p ? p + b * a.mod_stride : nullptr; };
 #pragma unroll
-  for (int i = 0; i < NV; ++i) c[i] = (i * LPR + t) * 8;
+    for (int i = 0; i < NV; ++i) {
+      const uint32_t c = at.c[i];
+      const int left = at.left[i];
+      const Four<T, VEC> pw = param4<T, VEC>(a.post ? a.w.post_w : nullptr, D, c, left, 1.f);
+      const Four<T, VEC> pb = param4<T, VEC>(a.post ? a.w.post_b : nullptr, D, c, left, 0.f);
+      const Four<T, VEC> rs = param4<T, VEC>(a.w.res_scale, D, c, left, 1.f);
+      const Four<T, VEC> nw = param4<T, VEC>(a.w.pre_w, D, c, left, 1.f), nb = param4<T, VEC>(a.w.pre_b, D, c, left, 0.f);
+      const Four<float, VEC> g = mod4<VEC>(mod(a.w.gate), D, c, left, modvec, 1.f);
+      const Four<float, VEC> sc = mod4<VEC>(mod(a.w.scale), D, c, left, modvec, 0.f);
+      const Four<float, VEC> sh = mod4<VEC>(mod(a.w.shift), D, c, left, modvec, 0.f);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float ga = g.at(j) * rs.at(j) * a.drop.factor;
+        w1[i][j] = ga * pw.at(j);
+        b1[i][j] = ga * pb.at(j);
+        w2[i][j] = (1.f + sc.at(j)) * nw.at(j);
+        b2[i][j] = fmaf(1.f + sc.at(j), nb.at(j), sh.at(j));
+      }
+    }
+  }
 
-  for (int64_t row0 = (int64_t)blockIdx.x * TEAMS; row0 < M; row0 += (int64_t)gridDim.x * TEAMS) {
-    const int64_t row = row0 + team;
-    const bool on = row < M;
-    const int64_t b = on ? row / a.S : 0;
-    float x[NV][8];
+  for (int sb = s0; sb < s1; sb += TEAMS) {
+    const int rows = min(TEAMS, s1 - sb);
+    const int64_t row0 = (int64_t)b * a.S + sb, row = row0 + team;
+    const bool on = team < rows;
+    float x[NV][4], n[NV][4];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) get8<X>((const X*)a.x + row * D, c[i], D, f.vec, on, 0.f, x[i]);
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        x[i][j] = xr[i].at(j);
+        n[i][j] = yr[i].at(j);
+      }
+    if (sb + TEAMS < s1) load(sb + TEAMS);
     if (a.y) {
-      float n[NV][8];
-#pragma unroll
-      for (int i = 0; i < NV; ++i) get8<T>((const T*)a.y + row * D, c[i], D, f.vec, on, 0.f, n[i]);
       if (a.post) {
         float mean, rstd;
-        norm_row<LPR, NV>(n, c, D, layer, a.eps, sum, mean, rstd);
+        norm_row<LPR, NV>(n, at.left, rD, layer, a.eps, sum, mean, rstd);
         if (a.stats && on && t == 0) {
           a.stats[row] = mean;
           a.stats[M + row] = rstd;
         }
       }
+      const __amdgpu_buffer_rsrc_t bx1 = rows_of<X>(a.x1, row0, rows, D);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        float w[8], bias[8], rs[8], g[8];
-        get8<T>((const T*)a.w.post_w, c[i], D, f.vec, a.post, 1.f, w);
-        get8<T>((const T*)a.w.post_b, c[i], D, f.vec, a.post, 0.f, bias);
-        get8<T>((const T*)a.w.res_scale, c[i], D, f.vec, true, 1.f, rs);
-        get8<float>(a.w.gate ? a.w.gate + b * a.mod_stride : nullptr, c[i], D, f.modvec, true, 1.f, g);
-        const uint32_t keep = drops ? keep_of(a.drop, key, row, D, c[i]) : 0xFFu;
-        float o[8];
+        const uint32_t keep = drops ? keep_of(a.drop, key, row, D, (i * LPR + t) * 4) : 0xFu;
+        float o[4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          float v = fmaf(n[i][j], w[j], bias[j]);
-          v = keep >> j & 1u ? v * a.drop.factor : 0.f;
-          o[j] = fmaf(g[j] * rs[j], v, x[i][j]);
-        }
-        if (on) put8<X>((X*)a.x1 + row * D, c[i], D, f.vec, o);
+        for (int j = 0; j < 4; ++j) o[j] = x[i][j] + (keep >> j & 1u ? fmaf(n[i][j], w1[i][j], b1[i][j]) : 0.f);
+        put4<X, VEC>(bx1, at.off[i], at.left[i], o);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[i][j] = c[i] + j < D ? to_f32<X>(from_f32<X>(o[j])) : 0.f;   // the next norm's input is what is kept
+        for (int j = 0; j < 4; ++j) x[i][j] = j < at.left[i] ? to_f32<X>(from_f32<X>(o[j])) : 0.f;   // the next norm's input is what is kept
       }
     }
-    if (!a.u && !a.uq) continue;
+    if (!next) continue;
     float mean, rstd;
-    norm_row<LPR, NV>(x, c, D, layer, a.eps, sum, mean, rstd);
+    norm_row<LPR, NV>(x, at.left, rD, layer, a.eps, sum, mean, rstd);
     if (a.stats && on && t == 0) {
       a.stats[2 * M + row] = mean;
       a.stats[3 * M + row] = rstd;
     }
+    const __amdgpu_buffer_rsrc_t bu = rows_of<T>(a.u, row0, rows, D);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      float w[8], bias[8], sc[8], sh[8], o[8];
-      get8<T>((const T*)a.w.pre_w, c[i], D, f.vec, true, 1.f, w);
-      get8<T>((const T*)a.w.pre_b, c[i], D, f.vec, true, 0.f, bias);
-      get8<float>(a.w.scale ? a.w.scale + b * a.mod_stride : nullptr, c[i], D, f.modvec, true, 0.f, sc);
-      get8<float>(a.w.shift ? a.w.shift + b * a.mod_stride : nullptr, c[i], D, f.modvec, true, 0.f, sh);
+      float o[4];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) o[j] = fmaf(fmaf(x[i][j], w[j], bias[j]), 1.f + sc[j], sh[j]);
-      if (a.u && on) put8<T>((T*)a.u + row * D, c[i], D, f.vec, o);
-      if (a.uq) {   // blocks of 128 channels: 16 neighbouring lanes
+      for (int j = 0; j < 4; ++j) o[j] = fmaf(x[i][j], w2[i][j], b2[i][j]);
+      put4<T, VEC>(bu, at.off[i], at.left[i], o);
+      if (a.uq) {   // blocks of 128 channels: 32 neighbouring lanes
         uint32_t m = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          if (c[i] + j >= D) o[j] = 0.f;
+        for (int j = 0; j < 4; ++j) {
+          if (j >= at.left[i]) o[j] = 0.f;
           m = max(m, __float_as_uint(o[j]) & 0x7FFFFFFFu);
         }
         auto over = [&](auto ctl) {
@@ -241,110 +325,135 @@ __global__ __launch_bounds__(threads_of<LPR>()) void residual_norm_fwd_kernel(Re
         over(IC<0x4E>{});
         over(IC<0x141>{});
         over(IC<0x140>{});
+        const auto r = __builtin_amdgcn_permlane16_swap(m, m, false, false);
+        m = max(r[0], r[1]);
         const uint32_t E = f8_exponent(m);
         const float inv = f8_inverse(m, E);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) o[j] = f8_clamp(o[j] * inv);
-        const int Dp = (D + 127) / 128 * 128;
-        if (on && c[i] < Dp) {
-          i32x2 q;
-          q[0] = (int)f8_code4(o[0], o[1], o[2], o[3]);
-          q[1] = (int)f8_code4(o[4], o[5], o[6], o[7]);
-          *reinterpret_cast<i32x2*>(a.uq + row * Dp + c[i]) = q;
-          if ((t & 15) == 0) a.ue[(int64_t)(c[i] / 128) * ((M + 15) / 16 * 16) + row] = (uint8_t)E;
+        const int Dp = (D + 127) / 128 * 128, ch = (i * LPR + t) * 4;
+        if (on && ch < Dp) {
+          *reinterpret_cast<uint32_t*>(a.uq + row * Dp + ch) =
+              f8_code4(f8_clamp(o[0] * inv), f8_clamp(o[1] * inv), f8_clamp(o[2] * inv), f8_clamp(o[3] * inv));
+          if ((t & 31) == 0) a.ue[(int64_t)(ch / 128) * ((M + 15) / 16 * 16) + row] = (uint8_t)E;
         }
       }
     }
   }
 }
 
-// Workgroup (b, k): rows k R .. of sample b; its part of the four column sums at part[((b chunks + k) 4 + i) D].
-template <typename T, typename X, int LPR, int NV>
-__global__ __launch_bounds__(threads_of<LPR>()) void residual_norm_bwd_kernel(ResidualNorm a, Flags f, int chunks) {
-  constexpr int NT = threads_of<LPR>(), TEAMS = NT / LPR, COLS = LPR * NV * 8;
+// Workgroup (b, k): rows k R .. of sample b; its part of the four column sums at part[((b chunks + k) 4 + i) D].  As in
+// the forward the next row is on its way while a row is computed.  Rows and channels that are not there read as zeros in
+// every tensor and statistic, and add nothing.
+template <typename T, typename X, int LPR, int NV, bool VEC>
+__global__ __launch_bounds__(threads_of<LPR>(), 2) void residual_norm_bwd_kernel(ResidualNorm a, bool modvec, int chunks) {
+  constexpr int NT = threads_of<LPR>(), TEAMS = NT / LPR, COLS = LPR * NV * 4;
   __shared__ float slots[2][2][16];
-  __shared__ float cols[TEAMS > 1 ? TEAMS : 1][TEAMS > 1 ? COLS : 1];
+  __shared__ __attribute__((aligned(16))) float cols[TEAMS > 1 ? TEAMS : 1][TEAMS > 1 ? COLS : 4];
   TeamSum<LPR> sum{slots};
-  const int t = threadIdx.x % LPR, team = threadIdx.x / LPR, D = a.D;
+  const int t = threadIdx.x % LPR, team = LPR < 64 ? (int)threadIdx.x / LPR : wave_index() / (LPR / 64 > 0 ? LPR / 64 : 1), D = a.D;
   const int64_t M = (int64_t)a.B * a.S;
   const int b = (int)(blockIdx.x / (unsigned)chunks), k = (int)(blockIdx.x - (unsigned)b * (unsigned)chunks);
   const int R = (a.S + chunks - 1) / chunks, s0 = (int)min((long)k * R, (long)a.S), s1 = min(a.S - s0, R) + s0;
   const bool layer = a.norm == SR_NORM_LAYER, drops = a.y && a.drop.thresh;
   const uint64_t key = drops ? drop_key(a.drop) : 0;
   const float rD = 1.0f / (float)D;
-  int c[NV];
-  float acc[4][NV][8];
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    c[i] = (i * LPR + t) * 8;
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) acc[q][i][j] = 0.f;
-  }
-
-  for (int sb = s0; sb < s1; sb += TEAMS) {
-    const int s = sb + team;
-    const bool on = s < s1;
-    const int64_t row = (int64_t)b * a.S + (on ? s : s0);
-    float dx[NV][8];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) get8<X>((const X*)a.dx1 + (a.dx1 ? row * D : 0), c[i], D, f.vec, on, 0.f, dx[i]);
-    if (a.du) {
-      float v[NV][8], g[NV][8], c1 = 0.f, c2 = 0.f;
-      const float mean = layer ? a.stats[2 * M + row] : 0.f, rstd = a.stats[3 * M + row];
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        float w[8], sc[8];
-        get8<X>((const X*)a.x + row * D, c[i], D, f.vec, on, mean, v[i]);
-        get8<T>((const T*)a.du + row * D, c[i], D, f.vec, on, 0.f, g[i]);
-        get8<T>((const T*)a.w.pre_w, c[i], D, f.vec, true, 1.f, w);
-        get8<float>(a.w.scale ? a.w.scale + b * a.mod_stride : nullptr, c[i], D, f.modvec, true, 0.f, sc);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          v[i][j] = (v[i][j] - mean) * rstd;
-          acc[0][i][j] += g[i][j];
-          acc[1][i][j] = on ? fmaf(g[i][j], v[i][j], acc[1][i][j]) : acc[1][i][j];
-          g[i][j] *= (1.f + sc[j]) * w[j];
-          c1 += g[i][j];
-          c2 = fmaf(g[i][j], v[i][j], c2);
-        }
-      }
-      sum(c1, c2);
-      c1 = layer ? c1 * rD : 0.f;
-      c2 *= rD;
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) dx[i][j] = fmaf(rstd, g[i][j] - fmaf(v[i][j], c2, c1), dx[i][j]);
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (on) put8<X>((X*)a.dx + row * D, c[i], D, f.vec, dx[i]);
-    if (!a.y) continue;
-    float n[NV][8], g[NV][8], c1 = 0.f, c2 = 0.f, mean = 0.f, rstd = 1.f;
-    if (a.post) {
-      if (layer) mean = a.stats[row];
-      rstd = a.stats[M + row];
-    }
+  const Place<LPR, NV> at(t, team, D);
+  float acc[4][NV][4], wpre[NV][4], wpost[NV][4];   // sums; (1 + scale) pre_w and gate res_scale post_w of the sample
+  {
+    const float *scale = a.w.scale ? a.w.scale + b * a.mod_stride : nullptr, *gate = a.w.gate ? a.w.gate + b * a.mod_stride : nullptr;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      float w[8], rs[8], gt[8];
-      get8<T>((const T*)a.y + row * D, c[i], D, f.vec, on, mean, n[i]);
-      get8<T>((const T*)a.w.post_w, c[i], D, f.vec, a.post, 1.f, w);
-      get8<T>((const T*)a.w.res_scale, c[i], D, f.vec, true, 1.f, rs);
-      get8<float>(a.w.gate ? a.w.gate + b * a.mod_stride : nullptr, c[i], D, f.modvec, true, 1.f, gt);
-      const uint32_t keep = drops ? keep_of(a.drop, key, row, D, c[i]) : 0xFFu;
+      const Four<T, VEC> pw = param4<T, VEC>(a.w.pre_w, D, at.c[i], at.left[i], 1.f), rs = param4<T, VEC>(a.w.res_scale, D, at.c[i], at.left[i], 1.f);
+      const Four<T, VEC> ow = param4<T, VEC>(a.post ? a.w.post_w : nullptr, D, at.c[i], at.left[i], 1.f);
+      const Four<float, VEC> sc = mod4<VEC>(scale, D, at.c[i], at.left[i], modvec, 0.f), gt = mod4<VEC>(gate, D, at.c[i], at.left[i], modvec, 1.f);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        n[i][j] = (n[i][j] - mean) * rstd;
-        const float d = on && c[i] + j < D && (keep >> j & 1u) ? dx[i][j] * a.drop.factor : 0.f;
-        acc[2][i][j] += d;
-        // a dropped value does not count, not even a NaN
-        acc[3][i][j] = on && (keep >> j & 1u) ? fmaf(d, n[i][j], acc[3][i][j]) : acc[3][i][j];
-        g[i][j] = d * (gt[j] * rs[j]) * w[j];
+      for (int j = 0; j < 4; ++j) {
+        wpre[i][j] = (1.f + sc.at(j)) * pw.at(j);
+        wpost[i][j] = gt.at(j) * rs.at(j) * ow.at(j);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) acc[q][i][j] = 0.f;
+      }
+    }
+  }
+  Four<X, VEC> dxr[NV], xr[NV];
+  Four<T, VEC> dur[NV], yr[NV];
+  float mx, rx, my, ry;   // the row's statistics
+  const bool has_y = a.y && a.post;
+  auto load = [&](int sb) {
+    const int rows = min(TEAMS, s1 - sb);
+    const int64_t row0 = (int64_t)b * a.S + sb;
+    const __amdgpu_buffer_rsrc_t bdx = rows_of<X>(a.dx1, row0, rows, D), bx = rows_of<X>(a.du ? a.x : nullptr, row0, rows, D);
+    const __amdgpu_buffer_rsrc_t bdu = rows_of<T>(a.du, row0, rows, D), by = rows_of<T>(a.y, row0, rows, D);
+    auto stat = [&](int q, bool has) {
+      return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rows_of<float>(has ? a.stats + q * M : nullptr, row0, rows, 1), (uint32_t)team * 4, 0, 0));
+    };
+    mx = stat(2, a.du && layer);
+    rx = stat(3, a.du);
+    my = stat(0, has_y && layer);
+    ry = stat(1, has_y);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      xr[i].load(bx, at.off[i], at.left[i]);
+      dur[i].load(bdu, at.off[i], at.left[i]);
+      dxr[i].load(bdx, at.off[i], at.left[i]);
+      yr[i].load(by, at.off[i], at.left[i]);
+    }
+  };
+  if (s0 < s1) load(s0);
+
+  for (int sb = s0; sb < s1; sb += TEAMS) {
+    const int rows = min(TEAMS, s1 - sb);
+    const int64_t row0 = (int64_t)b * a.S + sb;
+    float dx[NV][4], v[NV][4], g[NV][4];
+    Four<T, VEC> yc[NV];
+    const float rstd = rx, pmean = my, prstd = a.post ? ry : 1.f;
+    float c1 = 0.f, c2 = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      yc[i] = yr[i];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        dx[i][j] = dxr[i].at(j);
+        v[i][j] = (xr[i].at(j) - mx) * rx;
+        g[i][j] = dur[i].at(j);
+      }
+    }
+    if (sb + TEAMS < s1) load(sb + TEAMS);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        acc[0][i][j] += g[i][j];
+        acc[1][i][j] = fmaf(g[i][j], v[i][j], acc[1][i][j]);
+        g[i][j] *= wpre[i][j];
         c1 += g[i][j];
-        c2 = fmaf(g[i][j], n[i][j], c2);
+        c2 = fmaf(g[i][j], v[i][j], c2);
+      }
+    sum(c1, c2);
+    c1 = layer ? c1 * rD : 0.f;
+    c2 *= rD;
+    const __amdgpu_buffer_rsrc_t bdx = rows_of<X>(a.dx, row0, rows, D);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) dx[i][j] = fmaf(rstd, g[i][j] - fmaf(v[i][j], c2, c1), dx[i][j]);
+      put4<X, VEC>(bdx, at.off[i], at.left[i], dx[i]);
+    }
+    if (!a.y) continue;
+    c1 = c2 = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const uint32_t keep = drops ? keep_of(a.drop, key, row0 + team, D, (i * LPR + t) * 4) : 0xFu;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bool in = team < rows && j < at.left[i] && (keep >> j & 1u);
+        const float d = in ? dx[i][j] * a.drop.factor : 0.f;
+        const float n = (yc[i].at(j) - pmean) * prstd;
+        v[i][j] = n;
+        acc[2][i][j] += d;
+        acc[3][i][j] = in ? fmaf(d, n, acc[3][i][j]) : acc[3][i][j];   // a dropped value does not count, not even a NaN
+        g[i][j] = d * wpost[i][j];
+        c1 += g[i][j];
+        c2 = fmaf(g[i][j], n, c2);
       }
     }
     if (a.post) {
@@ -354,11 +463,11 @@ __global__ __launch_bounds__(threads_of<LPR>()) void residual_norm_bwd_kernel(Re
 #pragma unroll
       for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) g[i][j] = rstd * (g[i][j] - fmaf(n[i][j], c2, c1));
+        for (int j = 0; j < 4; ++j) g[i][j] = prstd * (g[i][j] - fmaf(v[i][j], c2, c1));
     }
+    const __amdgpu_buffer_rsrc_t bdy = rows_of<T>(a.dy, row0, rows, D);
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (on) put8<T>((T*)a.dy + row * D, c[i], D, f.vec, g[i]);
+    for (int i = 0; i < NV; ++i) put4<T, VEC>(bdy, at.off[i], at.left[i], g[i]);
   }
 
   float* part = a.part + (size_t)blockIdx.x * 4 * D;
@@ -366,16 +475,12 @@ __global__ __launch_bounds__(threads_of<LPR>()) void residual_norm_bwd_kernel(Re
   for (int q = 0; q < 4; ++q) {
     if constexpr (TEAMS == 1) {
 #pragma unroll
-      for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (c[i] + j < D) part[(size_t)q * D + c[i] + j] = acc[q][i][j];
+      for (int i = 0; i < NV; ++i) put4<float, VEC>(rows_of<float>(part, q, 1, D), at.c[i], at.left[i], acc[q][i]);
     } else {
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) cols[team][c[i] + j] = acc[q][i][j];
+        *reinterpret_cast<f32x4*>(&cols[team][(i * LPR + t) * 4]) = f32x4{acc[q][i][0], acc[q][i][1], acc[q][i][2], acc[q][i][3]};
       __syncthreads();
       for (int d = threadIdx.x; d < D; d += NT) {
         float s = 0.f;
@@ -387,54 +492,65 @@ __global__ __launch_bounds__(threads_of<LPR>()) void residual_norm_bwd_kernel(Re
   }
 }
 
-// The workgroups' parts to the gradients.  A workgroup takes 32 channels and one of the two pairs of sums: thread (g, d)
-// adds the parts g, g + 8, .. of channel d, the eight groups meet in LDS, and the first one goes on with the sample.
+// The workgroups' parts to the gradients.  A workgroup takes 32 channels and one of the two pairs of sums, 32 samples at a
+// time: its 32 groups of threads share the samples (G to a sample, thread (g, d) adds the parts g, g + G, .. of channel d),
+// meet in LDS, and one group per sample goes on with it; the parameters' sums over the samples follow in their order.
 template <typename T>
-__global__ __launch_bounds__(256) void residual_norm_grads_kernel(ResidualNorm a, int chunks) {
-  constexpr int G = 8;
-  __shared__ float sm[2][G][32];
-  const int dl = threadIdx.x & 31, g = threadIdx.x >> 5, D = a.D, d = blockIdx.x * 32 + dl, pair = blockIdx.y;
+__global__ __launch_bounds__(1024) void residual_norm_grads_kernel(ResidualNorm a, int chunks) {
+  __shared__ float sm[2][32][33], cb[3][32][33];
+  const int dl = threadIdx.x & 31, grp = threadIdx.x >> 5, D = a.D, d = blockIdx.x * 32 + dl, pair = blockIdx.y;
   const bool in = d < D;
   auto w = [&](const void* p, float fill) { return p && in ? to_f32<T>(((const T*)p)[d]) : fill; };
   const float pre_w = w(a.w.pre_w, 1.f), pre_b = w(a.w.pre_b, 0.f), rs = w(a.w.res_scale, 1.f);
   const float post_w = w(a.post ? a.w.post_w : nullptr, 1.f), post_b = w(a.post ? a.w.post_b : nullptr, 0.f);
   float tw = 0.f, tb = 0.f, tr = 0.f;
-  for (int b = 0; b < a.B; ++b) {
+  for (int b0 = 0; b0 < a.B; b0 += 32) {
+    const int nb = min(a.B - b0, 32);
+    int G = 32;   // groups of a sample: the largest power of two that gives every sample one
+    while (G * nb > 32) G >>= 1;
+    const int bl = grp / G, g = grp - bl * G;
     float s0 = 0.f, s1 = 0.f;
-    if (in)
+    if (in && bl < nb) {
+      const float* p = a.part + ((size_t)(b0 + bl) * chunks * 4 + 2 * pair) * D + d;
+#pragma unroll 8
       for (int k = g; k < chunks; k += G) {
-        const float* p = a.part + (((size_t)b * chunks + k) * 4 + 2 * pair) * D + d;
-        s0 += p[0];
-        s1 += p[D];
+        s0 += p[(size_t)k * 4 * D];
+        s1 += p[(size_t)k * 4 * D + D];
       }
-    sm[0][g][dl] = s0;
-    sm[1][g][dl] = s1;
+    }
+    sm[0][grp][dl] = s0;
+    sm[1][grp][dl] = s1;
     __syncthreads();
-    if (g == 0 && in) {
+    if (grp < nb && in) {
       s0 = s1 = 0.f;
-#pragma unroll
       for (int k = 0; k < G; ++k) {
-        s0 += sm[0][k][dl];
-        s1 += sm[1][k][dl];
+        s0 += sm[0][grp * G + k][dl];
+        s1 += sm[1][grp * G + k][dl];
       }
-      const size_t o = (size_t)b * D + d, om = (size_t)b * a.mod_stride + d;
+      const size_t o = (size_t)(b0 + grp) * D + d, om = (size_t)(b0 + grp) * a.mod_stride + d;
       if (pair == 0) {
         const float sc = 1.f + (a.w.scale ? a.w.scale[om] : 0.f);
         if (a.g.shift) a.g.shift[o] = s0;
         if (a.g.scale) a.g.scale[o] = fmaf(pre_w, s1, pre_b * s0);
-        tb = fmaf(sc, s0, tb);
-        tw = fmaf(sc, s1, tw);
+        cb[0][grp][dl] = sc * s0;
+        cb[1][grp][dl] = sc * s1;
       } else {
         const float gt = a.w.gate ? a.w.gate[om] : 1.f, v = fmaf(post_w, s1, post_b * s0);
         if (a.g.gate) a.g.gate[o] = rs * v;
-        tr = fmaf(gt, v, tr);
-        tb = fmaf(gt * rs, s0, tb);
-        tw = fmaf(gt * rs, s1, tw);
+        cb[0][grp][dl] = gt * rs * s0;
+        cb[1][grp][dl] = gt * rs * s1;
+        cb[2][grp][dl] = gt * v;
       }
     }
     __syncthreads();
+    if (grp == 0 && in)
+      for (int k = 0; k < nb; ++k) {
+        tb += cb[0][k][dl];
+        tw += cb[1][k][dl];
+        if (pair) tr += cb[2][k][dl];
+      }
   }
-  if (g == 0 && in) {
+  if (grp == 0 && in) {
     if (pair == 0) {
       if (a.g.pre_w) a.g.pre_w[d] = tw;
       if (a.g.pre_b) a.g.pre_b[d] = tb;
@@ -446,47 +562,44 @@ __global__ __launch_bounds__(256) void residual_norm_grads_kernel(ResidualNorm a
   }
 }
 
-int lanes_of(int D) { return D <= 128 ? 16 : D <= 256 ? 32 : D <= 1024 ? 64 : D <= 2048 ? 128 : D <= 4096 ? 256 : 512; }
+int lanes_of(int D) { return D <= 128 ? 32 : D <= 1024 ? 64 : D <= 2048 ? 128 : D <= 4096 ? 256 : 512; }
+int teams_of(int D) { return std::max(256, lanes_of(D)) / lanes_of(D); }
 
-// Workgroups of the backward per sample: about 1024 in all, four rows or more to a team.
-int chunks_of(int B, int S, int D) {
-  const int lpr = lanes_of(D), teams = (lpr > 256 ? lpr : 256) / lpr;
-  const int64_t most = std::max<int64_t>(1, ((int64_t)S + 4 * teams - 1) / (4 * teams));
-  return (int)std::min<int64_t>(most, std::max<int64_t>(1, 1024 / B));
+// Workgroups per sample, so that about `wgs` of them are one round on the CUs.
+int chunks_of(int B, int S, int D, int wgs) {
+  const int teams = teams_of(D);
+  const int64_t rows = std::max<int64_t>(1, ((int64_t)B * S + (int64_t)wgs * teams - 1) / ((int64_t)wgs * teams));   // of a team
+  return (int)((S + rows * teams - 1) / (rows * teams));
 }
+constexpr int kFwdWgs = 768, kBwdWgs = 512;   // three and two of 256 threads per CU
 
-Flags flags_of(const ResidualNorm& a) {
-  auto al = [](const void* p) { return ((uintptr_t)p & 15) == 0; };
-  Flags f;
-  f.vec = a.D % 8 == 0;   // the tensors themselves start on 16 bytes
-  f.modvec = f.vec && al(a.w.gate) && al(a.w.shift) && al(a.w.scale) && a.mod_stride % 4 == 0;
-  return f;
-}
-
-template <typename T, typename X, int LPR, int NV>
+template <typename T, typename X, int LPR, int NV, bool VEC>
 hipError_t run_rows(const ResidualNorm& a, bool bwd, hipStream_t st) {
-  constexpr int NT = threads_of<LPR>(), TEAMS = NT / LPR;
-  if (!bwd) {
-    const int64_t M = (int64_t)a.B * a.S, wgs = std::min<int64_t>((M + TEAMS - 1) / TEAMS, 1 << 16);
-    SR_LAUNCH((residual_norm_fwd_kernel<T, X, LPR, NV>), dim3((unsigned)wgs), dim3(NT), 0, st, a, flags_of(a));
-  } else {
-    const int chunks = chunks_of(a.B, a.S, a.D);
-    SR_LAUNCH((residual_norm_bwd_kernel<T, X, LPR, NV>), dim3((unsigned)a.B * (unsigned)chunks), dim3(NT), 0, st, a,
-              flags_of(a), chunks);
-  }
+  constexpr int NT = threads_of<LPR>();
+  auto al = [](const void* p) { return ((uintptr_t)p & 15) == 0; };
+  const bool modvec = VEC && al(a.w.gate) && al(a.w.shift) && al(a.w.scale) && a.mod_stride % 4 == 0;
+  const int chunks = chunks_of(a.B, a.S, a.D, bwd ? kBwdWgs : kFwdWgs);
+  const dim3 grid((unsigned)a.B * (unsigned)chunks);
+  if (bwd) SR_LAUNCH((residual_norm_bwd_kernel<T, X, LPR, NV, VEC>), grid, dim3(NT), 0, st, a, modvec, chunks);
+  else SR_LAUNCH((residual_norm_fwd_kernel<T, X, LPR, NV, VEC>), grid, dim3(NT), 0, st, a, modvec, chunks);
   return hipGetLastError();
 }
 
-template <typename T, typename X>
-hipError_t run(const ResidualNorm& a, bool bwd, hipStream_t st) {
+template <typename T, typename X, bool VEC>
+hipError_t run_width(const ResidualNorm& a, bool bwd, hipStream_t st) {
   switch (lanes_of(a.D)) {
-    case 16: return run_rows<T, X, 16, 1>(a, bwd, st);
-    case 32: return run_rows<T, X, 32, 1>(a, bwd, st);
-    case 64: return a.D <= 512 ? run_rows<T, X, 64, 1>(a, bwd, st) : run_rows<T, X, 64, 2>(a, bwd, st);
-    case 128: return run_rows<T, X, 128, 2>(a, bwd, st);
-    case 256: return run_rows<T, X, 256, 2>(a, bwd, st);
-    default: return run_rows<T, X, 512, 2>(a, bwd, st);
+    case 32: return run_rows<T, X, 32, 1, VEC>(a, bwd, st);
+    case 64:
+      if (a.D <= 256) return run_rows<T, X, 64, 1, VEC>(a, bwd, st);
+      return a.D <= 512 ? run_rows<T, X, 64, 2, VEC>(a, bwd, st) : run_rows<T, X, 64, 4, VEC>(a, bwd, st);
+    case 128: return run_rows<T, X, 128, 4, VEC>(a, bwd, st);
+    case 256: return run_rows<T, X, 256, 4, VEC>(a, bwd, st);
+    default: return run_rows<T, X, 512, 4, VEC>(a, bwd, st);
   }
+}
+template <typename T, typename X>
+hipError_t run(const ResidualNorm& a, bool bwd, hipStream_t st) {   // the tensors themselves start on 16 bytes
+  return a.D % 4 == 0 ? run_width<T, X, true>(a, bwd, st) : run_width<T, X, false>(a, bwd, st);
 }
 
 hipError_t run_types(int dtype, int stream_dtype, const ResidualNorm& a, bool bwd, hipStream_t st) {
@@ -496,7 +609,7 @@ hipError_t run_types(int dtype, int stream_dtype, const ResidualNorm& a, bool bw
 
 }  // namespace
 
-size_t residual_norm_scratch(int B, int S, int D) { return (size_t)B * chunks_of(B, S, D) * 4 * D * sizeof(float); }
+size_t residual_norm_scratch(int B, int S, int D) { return (size_t)B * chunks_of(B, S, D, kBwdWgs) * 4 * D * sizeof(float); }
 
 hipError_t launch_residual_norm_fwd(int dtype, int stream_dtype, const ResidualNorm& a, hipStream_t st) {
   return run_types(dtype, stream_dtype, a, false, st);
@@ -506,9 +619,9 @@ hipError_t launch_residual_norm_bwd(int dtype, int stream_dtype, const ResidualN
   hipError_t e = run_types(dtype, stream_dtype, a, true, st);
   if (e != hipSuccess) return e;
   const dim3 grid((unsigned)((a.D + 31) / 32), 2);
-  const int chunks = chunks_of(a.B, a.S, a.D);
-  if (dtype == kBF16) SR_LAUNCH((residual_norm_grads_kernel<bf16_t>), grid, dim3(256), 0, st, a, chunks);
-  else SR_LAUNCH((residual_norm_grads_kernel<float>), grid, dim3(256), 0, st, a, chunks);
+  const int chunks = chunks_of(a.B, a.S, a.D, kBwdWgs);
+  if (dtype == kBF16) SR_LAUNCH((residual_norm_grads_kernel<bf16_t>), grid, dim3(1024), 0, st, a, chunks);
+  else SR_LAUNCH((residual_norm_grads_kernel<float>), grid, dim3(1024), 0, st, a, chunks);
   return hipGetLastError();
 }
 
