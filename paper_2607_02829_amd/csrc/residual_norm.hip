@@ -119,10 +119,11 @@ SR_DEV float lanes_sum(float v) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-template <int LPR>
-constexpr int threads_of() {
-  return LPR > 256 ? LPR : 256;
-}
+// Threads of a workgroup.  The backward's holds twice as many teams of up to a wave, whose column sums leave as one part (16200 x
+// 1024 with the join 72.7 -> 70.5 us); teams of several waves meet at barriers, where more of them wait for each other (4 x 1000 x
+// 4096: 76 us, with twice as many 89).
+constexpr int fwd_threads(int lpr) { return lpr > 256 ? lpr : 256; }
+constexpr int bwd_threads(int lpr) { return lpr <= 64 || lpr > 256 ? 512 : 256; }
 
 // Two sums at once over a team.  Teams of several waves meet in LDS: the slots alternate, so that one barrier a sum
 // is enough (a slot is written again only behind the other one's barrier).
@@ -213,8 +214,8 @@ struct Place {
 // one is computed.  A sample's parameters become one factor and one summand per channel and norm:
 //   x1 = x + keep (n w1 + b1),  w1 = f gate res_scale post_w, b1 alike;   u = v w2 + b2,  w2 = (1 + scale) pre_w, ..
 template <typename T, typename X, int LPR, int NV, bool VEC>
-__global__ __launch_bounds__(threads_of<LPR>()) void residual_norm_fwd_kernel(ResidualNorm a, bool modvec, int chunks) {
-  constexpr int NT = threads_of<LPR>(), TEAMS = NT / LPR;
+__global__ __launch_bounds__(fwd_threads(LPR)) void residual_norm_fwd_kernel(ResidualNorm a, bool modvec, int chunks) {
+  constexpr int NT = fwd_threads(LPR), TEAMS = NT / LPR;
   __shared__ float slots[2][2][16];
   TeamSum<LPR> sum{slots};
   const int t = threadIdx.x % LPR, team = LPR < 64 ? (int)threadIdx.x / LPR : wave_index() / (LPR / 64 > 0 ? LPR / 64 : 1), D = a.D;
@@ -344,8 +345,8 @@ __global__ __launch_bounds__(threads_of<LPR>()) void residual_norm_fwd_kernel(Re
 // the forward the next row is on its way while a row is computed.  Rows and channels that are not there read as zeros in
 // every tensor and statistic, and add nothing.
 template <typename T, typename X, int LPR, int NV, bool VEC>
-__global__ __launch_bounds__(threads_of<LPR>(), 2) void residual_norm_bwd_kernel(ResidualNorm a, bool modvec, int chunks) {
-  constexpr int NT = threads_of<LPR>(), TEAMS = NT / LPR, COLS = LPR * NV * 4;
+__global__ __launch_bounds__(bwd_threads(LPR), 2) void residual_norm_bwd_kernel(ResidualNorm a, bool modvec, int chunks) {
+  constexpr int NT = bwd_threads(LPR), TEAMS = NT / LPR, COLS = LPR * NV * 4;
   __shared__ float slots[2][2][16];
   __shared__ __attribute__((aligned(16))) float cols[TEAMS > 1 ? TEAMS : 1][TEAMS > 1 ? COLS : 4];
   TeamSum<LPR> sum{slots};
@@ -492,22 +493,23 @@ __global__ __launch_bounds__(threads_of<LPR>(), 2) void residual_norm_bwd_kernel
   }
 }
 
-// The workgroups' parts to the gradients.  A workgroup takes 32 channels and one of the two pairs of sums, 32 samples at a
-// time: its 32 groups of threads share the samples (G to a sample, thread (g, d) adds the parts g, g + G, .. of channel d),
+// The workgroups' parts to the gradients.  A workgroup takes kCols channels and one of the two pairs of sums, kGroups
+// samples at a time: its kGroups groups of threads share the samples (G to a sample, thread (g, d) adds the parts g, g + G, .. of channel d),
 // meet in LDS, and one group per sample goes on with it; the parameters' sums over the samples follow in their order.
+constexpr int kCols = 32, kGroups = 1024 / kCols;
 template <typename T>
 __global__ __launch_bounds__(1024) void residual_norm_grads_kernel(ResidualNorm a, int chunks) {
-  __shared__ float sm[2][32][33], cb[3][32][33];
-  const int dl = threadIdx.x & 31, grp = threadIdx.x >> 5, D = a.D, d = blockIdx.x * 32 + dl, pair = blockIdx.y;
+  __shared__ float sm[2][kGroups][kCols + 1], cb[3][kGroups][kCols + 1];
+  const int dl = threadIdx.x % kCols, grp = threadIdx.x / kCols, D = a.D, d = blockIdx.x * kCols + dl, pair = blockIdx.y;
   const bool in = d < D;
   auto w = [&](const void* p, float fill) { return p && in ? to_f32<T>(((const T*)p)[d]) : fill; };
   const float pre_w = w(a.w.pre_w, 1.f), pre_b = w(a.w.pre_b, 0.f), rs = w(a.w.res_scale, 1.f);
   const float post_w = w(a.post ? a.w.post_w : nullptr, 1.f), post_b = w(a.post ? a.w.post_b : nullptr, 0.f);
   float tw = 0.f, tb = 0.f, tr = 0.f;
-  for (int b0 = 0; b0 < a.B; b0 += 32) {
-    const int nb = min(a.B - b0, 32);
-    int G = 32;   // groups of a sample: the largest power of two that gives every sample one
-    while (G * nb > 32) G >>= 1;
+  for (int b0 = 0; b0 < a.B; b0 += kGroups) {
+    const int nb = min(a.B - b0, kGroups);
+    int G = kGroups;   // groups of a sample: the largest power of two that gives every sample one
+    while (G * nb > kGroups) G >>= 1;
     const int bl = grp / G, g = grp - bl * G;
     float s0 = 0.f, s1 = 0.f;
     if (in && bl < nb) {
@@ -563,25 +565,30 @@ __global__ __launch_bounds__(1024) void residual_norm_grads_kernel(ResidualNorm 
 }
 
 int lanes_of(int D) { return D <= 128 ? 32 : D <= 1024 ? 64 : D <= 2048 ? 128 : D <= 4096 ? 256 : 512; }
-int teams_of(int D) { return std::max(256, lanes_of(D)) / lanes_of(D); }
 
-// Workgroups per sample, so that about `wgs` of them are one round on the CUs.
-int chunks_of(int B, int S, int D, int wgs) {
-  const int teams = teams_of(D);
-  const int64_t rows = std::max<int64_t>(1, ((int64_t)B * S + (int64_t)wgs * teams - 1) / ((int64_t)wgs * teams));   // of a team
+// Workgroups per sample, so that there are about `wgs` of them: in the backward 512 threads per CU, all that its registers leave room for; in the forward, where three fit,
+// a little more (16200 x 1024: 768 42.3 us, 1024 41.0, 1536 42.0).
+int chunks_of(int B, int S, int D, int threads, int wgs) {
+  const int teams = threads / lanes_of(D);
+  const int64_t M = (int64_t)B * S;
+  // rows of a team: two at least once every CU has a workgroup, so that one loads under the other (8 x 512 x 1024 forward 14.1 -> 12.1 us)
+  const int64_t rows = std::max<int64_t>(M > 256 * teams ? 2 : 1, (M + (int64_t)wgs * teams - 1) / ((int64_t)wgs * teams));
   return (int)((S + rows * teams - 1) / (rows * teams));
 }
-constexpr int kFwdWgs = 768, kBwdWgs = 512;   // three and two of 256 threads per CU
+int fwd_chunks(int B, int S, int D) { return chunks_of(B, S, D, fwd_threads(lanes_of(D)), 1024); }
+int bwd_chunks(int B, int S, int D) {
+  const int threads = bwd_threads(lanes_of(D));
+  return chunks_of(B, S, D, threads, 512 * 256 / threads);
+}
 
 template <typename T, typename X, int LPR, int NV, bool VEC>
 hipError_t run_rows(const ResidualNorm& a, bool bwd, hipStream_t st) {
-  constexpr int NT = threads_of<LPR>();
   auto al = [](const void* p) { return ((uintptr_t)p & 15) == 0; };
   const bool modvec = VEC && al(a.w.gate) && al(a.w.shift) && al(a.w.scale) && a.mod_stride % 4 == 0;
-  const int chunks = chunks_of(a.B, a.S, a.D, bwd ? kBwdWgs : kFwdWgs);
+  const int chunks = bwd ? bwd_chunks(a.B, a.S, a.D) : fwd_chunks(a.B, a.S, a.D);
   const dim3 grid((unsigned)a.B * (unsigned)chunks);
-  if (bwd) SR_LAUNCH((residual_norm_bwd_kernel<T, X, LPR, NV, VEC>), grid, dim3(NT), 0, st, a, modvec, chunks);
-  else SR_LAUNCH((residual_norm_fwd_kernel<T, X, LPR, NV, VEC>), grid, dim3(NT), 0, st, a, modvec, chunks);
+  if (bwd) SR_LAUNCH((residual_norm_bwd_kernel<T, X, LPR, NV, VEC>), grid, dim3(bwd_threads(LPR)), 0, st, a, modvec, chunks);
+  else SR_LAUNCH((residual_norm_fwd_kernel<T, X, LPR, NV, VEC>), grid, dim3(fwd_threads(LPR)), 0, st, a, modvec, chunks);
   return hipGetLastError();
 }
 
@@ -609,7 +616,7 @@ hipError_t run_types(int dtype, int stream_dtype, const ResidualNorm& a, bool bw
 
 }  // namespace
 
-size_t residual_norm_scratch(int B, int S, int D) { return (size_t)B * chunks_of(B, S, D, kBwdWgs) * 4 * D * sizeof(float); }
+size_t residual_norm_scratch(int B, int S, int D) { return (size_t)B * bwd_chunks(B, S, D) * 4 * D * sizeof(float); }
 
 hipError_t launch_residual_norm_fwd(int dtype, int stream_dtype, const ResidualNorm& a, hipStream_t st) {
   return run_types(dtype, stream_dtype, a, false, st);
@@ -618,8 +625,8 @@ hipError_t launch_residual_norm_fwd(int dtype, int stream_dtype, const ResidualN
 hipError_t launch_residual_norm_bwd(int dtype, int stream_dtype, const ResidualNorm& a, hipStream_t st) {
   hipError_t e = run_types(dtype, stream_dtype, a, true, st);
   if (e != hipSuccess) return e;
-  const dim3 grid((unsigned)((a.D + 31) / 32), 2);
-  const int chunks = chunks_of(a.B, a.S, a.D, kBwdWgs);
+  const dim3 grid((unsigned)((a.D + kCols - 1) / kCols), 2);
+  const int chunks = bwd_chunks(a.B, a.S, a.D);
   if (dtype == kBF16) SR_LAUNCH((residual_norm_grads_kernel<bf16_t>), grid, dim3(1024), 0, st, a, chunks);
   else SR_LAUNCH((residual_norm_grads_kernel<float>), grid, dim3(1024), 0, st, a, chunks);
   return hipGetLastError();
