@@ -59,7 +59,9 @@ SR_DEV float gelu_f(float z) {
 // that round z and GELU(z) once together.
 template <int DEG>
 SR_DEV float gelu_lim(float z) {
-  return fmaf(-fminf(fabsf(z), 3.4028234663852886e38f), half_erfc_of<DEG>(z, z * z), fmaxf(z, 0.f));
+  // the median leaves out the canonicalisations of fminf and fmaxf; of a NaN it is a number, but its Phi is NaN
+  return fmaf(-__builtin_amdgcn_fmed3f(fabsf(z), 0.f, 3.4028234663852886e38f), half_erfc_of<DEG>(z, z * z),
+              __builtin_amdgcn_fmed3f(z, 0.f, __builtin_inff()));
 }
 template <int DEG>
 SR_DEV float gelu_grad_f(float z) {

@@ -48,10 +48,11 @@ SR_DEV float bias_at(const LinearF8& a, int n) {
   return a.bias && n < a.N ? to_f32<T>(((const T*)a.bias)[n]) : 0.f;
 }
 // GELU's fit follows the type of the results (epilogue.h): for bf16 ones it is off by less than 5e-5 of z Phi(-|z|).
-template <typename T>
-SR_DEV float finish(const LinearF8& a, float acc, float bias) {
+// ACT is a constant, so that the elements of a lane interleave (16200 x 4096 x 1024: with a branch each 109 us, without 105).
+template <typename T, int ACT>
+SR_DEV float finish(float acc, float bias) {
   const float v = acc + bias;
-  return a.act == SR_ACT_GELU ? gelu_lim<gelu_deg<T>()>(v) : v;
+  return ACT == SR_ACT_GELU ? gelu_lim<gelu_deg<T>()>(v) : v;
 }
 template <typename O>
 SR_DEV void store4(char* p, f32x4 v) {
@@ -103,6 +104,7 @@ SR_DEV void fill_tile(const uint32_t* off, __amdgpu_buffer_rsrc_t rs, char* lds,
 template <int BM, int BN, int WM, int WN, int KG, int NST, int OCC, typename T>
 __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear_f8_tile_kernel(LinearF8 a, int tiles_m, int tiles_n, int splits) {
   constexpr bool WIDE = sizeof(T) == 4;
+  constexpr bool GELU = WIDE || BM * BN < 256 * 256;   // tiles of 256 x 256 on 8-bit products have no registers to spare for it
   constexpr int NW = WM * WN, NT = 64 * NW * KG;
   constexpr int MI = BM / (32 * WM), NJ = BN / (32 * WN);
   constexpr int SB = (BM + BN) * KB;               // bytes of a stage: the token tile, then the weight tile
@@ -278,9 +280,10 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear_f8_tile_kernel(
   wait_vm_lgkm0<0>();
   __syncthreads();
 
-  // Results, as O: the storage type, or fp32 sums of a run (done: finished with bias and activation).
-  auto write = [&](auto otype, void* dst, bool done) {
+  // Results, as O: the storage type, or fp32 sums of a run (whose bias is zero).
+  auto write = [&](auto otype, void* dst, auto actv) {
     typedef decltype(otype) O;
+    constexpr int ACT = decltype(actv)::value;
     O* out = (O*)dst;
     const bool vec = a.N % (16 / (int)sizeof(O)) == 0;   // rows start on 16 bytes
     if constexpr (KG == 1) {
@@ -306,7 +309,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear_f8_tile_kernel(
               const f32x4 b = *reinterpret_cast<const f32x4*>(bias + nb0 + 8 * q + 4 * h);
               f32x4 v;
 #pragma unroll
-              for (int r = 0; r < 4; ++r) v[r] = done ? finish<T>(a, acc[p + i][j][4 * q + r], b[r]) : acc[p + i][j][4 * q + r];
+              for (int r = 0; r < 4; ++r) v[r] = finish<T, ACT>(acc[p + i][j][4 * q + r], b[r]);
               store4<O>(row + (nb0 + 8 * q + 4 * h) * E, v);
             }
           }
@@ -352,9 +355,8 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear_f8_tile_kernel(
             f32x4 v = *reinterpret_cast<const f32x4*>(stg + lr * LD + c4);
 #pragma unroll
             for (int g = 1; g < KG; ++g) v += *reinterpret_cast<const f32x4*>(stg + (g * PR + lr) * LD + c4);
-            if (done)
 #pragma unroll
-              for (int r = 0; r < 4; ++r) v[r] = finish<T>(a, v[r], bias[c4 + r]);
+            for (int r = 0; r < 4; ++r) v[r] = finish<T, ACT>(v[r], bias[c4 + r]);
             O* o = out + (size_t)m * a.N + n;
             if (vec) {
               store4<O>((char*)o, v);
@@ -368,8 +370,9 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear_f8_tile_kernel(
       }
     }
   };
-  if (splits == 1) write(T{}, a.y, true);
-  else write(float{}, a.scratch + (size_t)split * a.M * a.N, false);
+  if (splits > 1) write(float{}, a.scratch + (size_t)split * a.M * a.N, IC<SR_ACT_NONE>{});
+  else if (!GELU || a.act == SR_ACT_NONE) write(T{}, a.y, IC<SR_ACT_NONE>{});
+  else if constexpr (GELU) write(T{}, a.y, IC<SR_ACT_GELU>{});
 }
 
 // The sums of `splits` runs, in order, finished.
@@ -379,7 +382,8 @@ __global__ __launch_bounds__(256) void linear_f8_join_kernel(LinearF8 a, int spl
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
     float v = a.scratch[i];
     for (int s = 1; s < splits; ++s) v += a.scratch[s * n + i];
-    ((T*)a.y)[i] = from_f32<T>(finish<T>(a, v, bias_at<T>(a, (int)(i % a.N))));
+    const float b = bias_at<T>(a, (int)(i % a.N));
+    ((T*)a.y)[i] = from_f32<T>(a.act == SR_ACT_GELU ? finish<T, SR_ACT_GELU>(v, b) : finish<T, SR_ACT_NONE>(v, b));
   }
 }
 
@@ -440,7 +444,8 @@ __global__ __launch_bounds__(64 * W) void linear_f8_few_kernel(LinearF8 a) {
       float v = stg[0][lr][lc];
 #pragma unroll
       for (int g = 1; g < W; ++g) v += stg[g][lr][lc];
-      ((T*)a.y)[(size_t)m * a.N + n] = from_f32<T>(finish<T>(a, v, bias_at<T>(a, n)));
+      const float b = bias_at<T>(a, n);
+      ((T*)a.y)[(size_t)m * a.N + n] = from_f32<T>(a.act == SR_ACT_GELU ? finish<T, SR_ACT_GELU>(v, b) : finish<T, SR_ACT_NONE>(v, b));
     }
   }
 }
@@ -470,7 +475,7 @@ int64_t tiles_of(int M, int N, int bm, int bn) { return ((int64_t)(M + bm - 1) /
 //   1024 x 1024 x 16200 39 (64 x 64 49, one run 101)
 //   256 x 128:  8192 x 1024 x 1024 13.9 (128 x 128 14.6, 256 x 256 18.9)
 //   256 x 256:  16200 x 4096 x 1024 80 (86), 16200 x 1024 x 4096 57 (67), 4050 x 4096 x 1024 23.7 (24.5), fp32 16200 x 4096 x 1024 134
-//   (146);  with GELU, whose vector work wants a second workgroup's products beside it, 16200 x 4096 x 1024 115 (112)
+//   (146);  with GELU, whose vector work wants a second workgroup's products beside it, 16200 x 4096 x 1024 105 with two of 128 x 128
 Plan plan_of(int M, int N, int K) {
   auto tiles = [&](int bm, int bn) { return tiles_of(M, N, bm, bn); };
   const int kb = (K + KB - 1) / KB;
@@ -520,7 +525,8 @@ hipError_t run(const LinearF8& a, hipStream_t st) {
     case k128x2: return run_tile<128, 128, 2, 4, 1, 2, 2, T>(a, s, st);
     case k256x128: return run_tile<256, 128, 4, 2, 1, 3, 1, T>(a, s, st);
     case k256:
-      return a.act == SR_ACT_GELU ? run_tile<128, 128, 2, 4, 1, 2, 2, T>(a, s, st) : run_tile<256, 256, 2, 4, 1, 2, 1, T>(a, s, st);
+      if (!WIDE && a.act == SR_ACT_GELU) return run_tile<128, 128, 2, 2, 1, 2, 2, T>(a, s, st);
+      return run_tile<256, 256, 2, 4, 1, 2, 1, T>(a, s, st);
   }
   return hipErrorInvalidValue;
 }
