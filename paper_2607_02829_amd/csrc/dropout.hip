@@ -31,16 +31,16 @@ struct Eight {
       }
     }
   }
-  SR_DEV void store(T* p) const {
+  SR_DEV void store(T* p, bool past) const {
     if constexpr (sizeof(T) == 2) {
       i32x4 w;
 #pragma unroll
       for (int j = 0; j < 4; ++j) w[j] = (int)f2bf2(v[2 * j], v[2 * j + 1]);
-      *reinterpret_cast<i32x4*>(p) = w;
+      store16(p, w, past);
     } else {
 #pragma unroll
       for (int j = 0; j < 2; ++j)
-        *reinterpret_cast<f32x4*>(p + 4 * j) = f32x4{v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
+        store16(p + 4 * j, __builtin_bit_cast(i32x4, f32x4{v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]}), past);
     }
   }
 };
@@ -49,6 +49,7 @@ struct Eight {
 template <typename T>
 __global__ __launch_bounds__(kThreads) void dropout_kernel(Dropout a) {
   const int64_t n = a.M * a.N, whole = n / 8;
+  const bool past = n * (int64_t)sizeof(T) >= kStreamBytes;
   const uint64_t key = drop_key(a.drop), e0 = a.drop.first_row * (uint64_t)a.N;
   const T *x = (const T*)a.x, *r = (const T*)a.resid;
   T* y = (T*)a.y;
@@ -62,7 +63,7 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(Dropout a) {
       const float t = keep >> j & 1u ? v.v[j] * a.drop.factor : 0.f;
       v.v[j] = r ? w.v[j] + t : t;
     }
-    v.store(y + 8 * i);
+    v.store(y + 8 * i, past);
   }
   const int64_t i = 8 * whole + threadIdx.x;
   if (blockIdx.x == 0 && i < n) {
@@ -77,6 +78,7 @@ template <typename T>
 __global__ __launch_bounds__(kThreads) void dropout_rows_kernel(Dropout a) {
   const uint64_t key = drop_key(a.drop);
   const int lane = threadIdx.x & 63;
+  const bool past = a.M * a.N * (int64_t)sizeof(T) >= kStreamBytes;
   const bool vec = a.N % (16 / (int)sizeof(T)) == 0;   // rows start on 16 bytes
   const int64_t step = (int64_t)gridDim.x * (kThreads / 64);
   for (int64_t row = (int64_t)blockIdx.x * (kThreads / 64) + wave_index(); row < a.M; row += step) {
@@ -93,7 +95,7 @@ __global__ __launch_bounds__(kThreads) void dropout_rows_kernel(Dropout a) {
         const float t = keep ? v.v[j] * a.drop.factor : 0.f;
         v.v[j] = r ? w.v[j] + t : t;
       }
-      v.store(y + c);
+      v.store(y + c, past);
     }
     for (int64_t c = whole + lane; c < a.N; c += 64) {
       const float t = keep ? to_f32<T>(x[c]) * a.drop.factor : 0.f;

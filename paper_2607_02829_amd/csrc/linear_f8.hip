@@ -286,6 +286,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear_f8_tile_kernel(
     constexpr int ACT = decltype(actv)::value;
     O* out = (O*)dst;
     const bool vec = a.N % (16 / (int)sizeof(O)) == 0;   // rows start on 16 bytes
+    const bool past = splits == 1 && (int64_t)a.M * a.N * (int64_t)sizeof(O) >= kStreamBytes;
     if constexpr (KG == 1) {
       // one group: the weight is the first operand, so that a lane has four consecutive channels of one token in each
       // register quad (register r: channel 8 (r/4) + 4 h + r%4, token lane % 32).  The results go through LDS, IPP blocks of
@@ -323,7 +324,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear_f8_tile_kernel(
             const char* s = smem + lr * LDB + col * E;
             O* o = out + (size_t)m * a.N + n;
             if (vec) {
-              *reinterpret_cast<i32x4*>(o) = *reinterpret_cast<const i32x4*>(s);
+              store16(o, *reinterpret_cast<const i32x4*>(s), past);
             } else {
 #pragma unroll
               for (int r = 0; r < 16 / E; ++r)

@@ -64,6 +64,11 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary a, Units un) {
   const int64_t rows = (int64_t)a.B * a.S, row0 = (int64_t)blockIdx.x * un.tokens;
   const uint32_t n = (uint32_t)un.tokens * un.per_token;
   typedef Pack<T, V> Vec;
+  const bool past = rows * a.heads * a.hd * (int64_t)sizeof(T) >= kStreamBytes;
+  auto put = [&](T* p, const Vec& v) {
+    if constexpr (V > 1) store16(p, __builtin_bit_cast(i32x4, v), past);
+    else *reinterpret_cast<Vec*>(p) = v;
+  };
   bool first = true;
   for (uint32_t base = 0; base < n || first; base += kThreads * kUnroll) {
     Vec lo[kUnroll], hi[kUnroll];
@@ -135,7 +140,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary a, Units un) {
             lo[k].v[j] = from_f32<T>(fmaf(x0, c.x, -x1 * c.y));
             hi[k].v[j] = from_f32<T>(fmaf(x1, c.x, x0 * c.y));
           }
-          *reinterpret_cast<Vec*>(yp + c1[k]) = hi[k];
+          put(yp + c1[k], hi[k]);
         } else {
 #pragma unroll
           for (int j = 0; j < V / 2; ++j) {
@@ -146,7 +151,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary a, Units un) {
           }
         }
       }
-      *reinterpret_cast<Vec*>(yp) = lo[k];
+      put(yp, lo[k]);
     }
   }
 }
