@@ -464,8 +464,7 @@ typedef struct {
  *   idx: [B,S] int32 ([1,S] with idx_shared), the token index of each row, as sr_select_indices gives it (any order,
  *        repeats allowed; entries in [0, grid product)), or NULL: row s of a sample is token s (S <= the grid product).
  *   inverse: 1 turns by the negative angles: the gradient of x from that of y.
- * 1 <= head_dim <= 256; ldx, ldy >= heads * head_dim.  Rows that start on multiples of 16 bytes, with P (SR_ROT_HALVES; 2 P
- * otherwise) and head_dim multiples of 16 bytes too, are read 16 bytes at a time, others by element. */
+ * 1 <= head_dim <= 256, heads * head_dim <= 32768; ldx, ldy >= heads * head_dim.  x and y need the alignment of their elements only. */
 SR_API sr_status sr_rotary(const sr_rotary_cfg* rot, int32_t inverse, int32_t dtype, int32_t B, int32_t S, int32_t heads,
                     int32_t head_dim, const void* x, int64_t ldx, const int32_t* idx, int32_t idx_shared, void* y,
                     int64_t ldy, void* stream);

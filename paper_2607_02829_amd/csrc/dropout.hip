@@ -16,7 +16,7 @@ struct Eight {
   float v[8];
   SR_DEV void load(const T* p) {
     if constexpr (sizeof(T) == 2) {
-      const i32x4 w = *reinterpret_cast<const i32x4*>(p);
+      const i32x4 w = load16(p);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         v[2 * j] = __uint_as_float((uint32_t)w[j] << 16);
@@ -25,7 +25,7 @@ struct Eight {
     } else {
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const f32x4 w = *reinterpret_cast<const f32x4*>(p + 4 * j);
+        const f32x4 w = __builtin_bit_cast(f32x4, load16(p + 4 * j));
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[4 * j + i] = w[i];
       }
@@ -79,13 +79,12 @@ __global__ __launch_bounds__(kThreads) void dropout_rows_kernel(Dropout a) {
   const uint64_t key = drop_key(a.drop);
   const int lane = threadIdx.x & 63;
   const bool past = a.M * a.N * (int64_t)sizeof(T) >= kStreamBytes;
-  const bool vec = a.N % (16 / (int)sizeof(T)) == 0;   // rows start on 16 bytes
   const int64_t step = (int64_t)gridDim.x * (kThreads / 64);
   for (int64_t row = (int64_t)blockIdx.x * (kThreads / 64) + wave_index(); row < a.M; row += step) {
     const bool keep = drop_keep1(key, (a.drop.first_row + (uint64_t)row) / (uint64_t)a.drop.group, a.drop.thresh);
     const T *x = (const T*)a.x + row * a.N, *r = a.resid ? (const T*)a.resid + row * a.N : nullptr;
     T* y = (T*)a.y + row * a.N;
-    const int64_t whole = vec ? a.N / 8 * 8 : 0;
+    const int64_t whole = a.N / 8 * 8;
     for (int64_t c = 8 * lane; c < whole; c += 512) {
       Eight<T> v, w;
       if (keep) v.load(x + c);

@@ -57,12 +57,12 @@ SR_DEV float finish(float acc, float bias) {
 template <typename O>
 SR_DEV void store4(char* p, f32x4 v) {
   if constexpr (sizeof(O) == 4) {
-    *reinterpret_cast<f32x4*>(p) = v;
+    store16(p, __builtin_bit_cast(i32x4, v));
   } else {
     i32x2 w;
     w[0] = (int)f2bf2(v[0], v[1]);
     w[1] = (int)f2bf2(v[2], v[3]);
-    *reinterpret_cast<i32x2*>(p) = w;
+    store8(p, w);
   }
 }
 
@@ -285,7 +285,6 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear_f8_tile_kernel(
     typedef decltype(otype) O;
     constexpr int ACT = decltype(actv)::value;
     O* out = (O*)dst;
-    const bool vec = a.N % (16 / (int)sizeof(O)) == 0;   // rows start on 16 bytes
     const bool past = splits == 1 && (int64_t)a.M * a.N * (int64_t)sizeof(O) >= kStreamBytes;
     if constexpr (KG == 1) {
       // one group: the weight is the first operand, so that a lane has four consecutive channels of one token in each
@@ -323,7 +322,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear_f8_tile_kernel(
           if (m < a.M && n < a.N) {
             const char* s = smem + lr * LDB + col * E;
             O* o = out + (size_t)m * a.N + n;
-            if (vec) {
+            if (n + 16 / E <= a.N) {
               store16(o, *reinterpret_cast<const i32x4*>(s), past);
             } else {
 #pragma unroll
@@ -359,7 +358,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear_f8_tile_kernel(
 #pragma unroll
             for (int r = 0; r < 4; ++r) v[r] = finish<T, ACT>(v[r], bias[c4 + r]);
             O* o = out + (size_t)m * a.N + n;
-            if (vec) {
+            if (n + 4 <= a.N) {
               store4<O>((char*)o, v);
             } else {
 #pragma unroll

@@ -31,7 +31,7 @@ struct Row8<bf16_t> {
   static constexpr int W = 4;   // words
   uint32_t w[4];
   SR_DEV void load(const bf16_t* p) {
-    const i32x4 r = *reinterpret_cast<const i32x4*>(p);
+    const i32x4 r = load16(p);
 #pragma unroll
     for (int j = 0; j < 4; ++j) w[j] = (uint32_t)r[j];
   }
@@ -51,7 +51,7 @@ struct Row8<float> {
   SR_DEV void load(const float* p) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      const i32x4 r = *reinterpret_cast<const i32x4*>(p + 4 * k);
+      const i32x4 r = load16(p + 4 * k);
 #pragma unroll
       for (int j = 0; j < 4; ++j) w[4 * k + j] = (uint32_t)r[j];
     }
@@ -91,7 +91,7 @@ SR_DEV i32x2 codes8(const float (&v)[8], const float (&inv)[8], bool clamps) {
 }
 
 template <typename T, bool TILE, bool ROWS, bool COLS>
-__global__ __launch_bounds__(256) void quantize_f8_kernel(QuantF8 a, int vec) {
+__global__ __launch_bounds__(256) void quantize_f8_kernel(QuantF8 a) {
   typedef Row8<T> R;
   __shared__ __attribute__((aligned(16))) uint8_t tr[COLS ? 128 * kPitch : 16];
   __shared__ uint32_t top[4][COLS ? 128 : 16];
@@ -110,7 +110,7 @@ __global__ __launch_bounds__(256) void quantize_f8_kernel(QuantF8 a, int vec) {
 #pragma unroll
     for (int j = 0; j < R::W; ++j) v[i].w[j] = 0;
     if (m < a.M) {
-      if (vec && n + 8 <= a.N) {
+      if (n + 8 <= a.N) {
         v[i].load(p);
       } else {
 #pragma unroll
@@ -208,10 +208,9 @@ __global__ __launch_bounds__(256) void quantize_f8_kernel(QuantF8 a, int vec) {
 template <typename T, bool TILE>
 hipError_t run(const QuantF8& a, hipStream_t st) {
   const dim3 grid((unsigned)((a.M + 127) / 128) * (unsigned)((a.N + 127) / 128));
-  const int vec = ((uintptr_t)a.x & 15) == 0 && a.ldx * sizeof(T) % 16 == 0;
-  if (!a.qt) SR_LAUNCH((quantize_f8_kernel<T, TILE, true, false>), grid, dim3(256), 0, st, a, vec);
-  else if (!a.q) SR_LAUNCH((quantize_f8_kernel<T, TILE, false, true>), grid, dim3(256), 0, st, a, vec);
-  else SR_LAUNCH((quantize_f8_kernel<T, TILE, true, true>), grid, dim3(256), 0, st, a, vec);
+  if (!a.qt) SR_LAUNCH((quantize_f8_kernel<T, TILE, true, false>), grid, dim3(256), 0, st, a);
+  else if (!a.q) SR_LAUNCH((quantize_f8_kernel<T, TILE, false, true>), grid, dim3(256), 0, st, a);
+  else SR_LAUNCH((quantize_f8_kernel<T, TILE, true, true>), grid, dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

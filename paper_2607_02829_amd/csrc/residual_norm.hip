@@ -25,36 +25,64 @@ SR_DEV __amdgpu_buffer_rsrc_t rows_of(const void* p, int64_t row, int rows, int 
   return make_rsrc((const T*)p + row * D, p ? (uint32_t)rows * (uint32_t)D * (uint32_t)sizeof(T) : 0u);
 }
 
-// Four channels as they lie in memory, so that they can be on their way while the row before is computed.  off: element
-// offset of the first; without VEC runs of four may start anywhere and end past the row, left: channels up to its end.
-template <typename T, bool VEC>
+// How a row is cut into runs of four channels.  kWhole: D is a multiple of four.  kShifted: the last run starts at D - 4
+// instead, so that every load is whole (buffer accesses need no alignment here); its first channels belong to the run
+// before, count there and are left out here.  kSingle: D < 4, channel by channel.
+enum Cut { kWhole, kShifted, kSingle };
+
+// A thread's runs: offset from a workgroup's first row (kPast: none), first channel, and which of the four are its own.
+template <int LPR, int NV, int CUT>
+struct Place {
+  uint32_t off[NV];
+  int t, D;
+  uint32_t row;
+  SR_DEV Place(int t_, int team, int D_) : t(t_), D(D_), row((uint32_t)(team * D_)) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int k = natural(i);
+      off[i] = k < D ? row + (uint32_t)(CUT == kShifted ? min(k, D - 4) : k) : kPast;
+    }
+  }
+  SR_DEV int natural(int i) const { return (i * LPR + t) * 4; }
+  SR_DEV uint32_t c(int i) const { return off[i] - row; }   // D or more where there is none
+  SR_DEV int lo(int i) const { return CUT == kShifted ? natural(i) - (int)c(i) : 0; }
+  SR_DEV int hi(int i) const { return CUT == kSingle ? D - natural(i) : 4; }
+  SR_DEV bool own(int i, int j) const {
+    if constexpr (CUT == kWhole) return off[i] < kPast;
+    if constexpr (CUT == kShifted) return off[i] < kPast && j >= lo(i);
+    return j < hi(i);
+  }
+};
+
+// Four channels as they lie in memory, so that they can be on their way while the row before is computed.
+template <typename T, int CUT>
 struct Four;
-template <bool VEC>
-struct Four<float, VEC> {
+template <int CUT>
+struct Four<float, CUT> {
   f32x4 r;
-  SR_DEV void load(__amdgpu_buffer_rsrc_t b, uint32_t off, int left) {
-    if constexpr (VEC) {
+  SR_DEV void load(__amdgpu_buffer_rsrc_t b, uint32_t off, int hi) {
+    if constexpr (CUT != kSingle) {
       r = __builtin_bit_cast(f32x4, buf_load16(b, off * 4));
     } else {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        r[j] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(b, (j < left ? off + j : kPast) * 4, 0, 0));
+        r[j] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(b, (j < hi ? off + j : kPast) * 4, 0, 0));
     }
   }
   SR_DEV void fill(float v) { r = f32x4{v, v, v, v}; }
   SR_DEV float at(int j) const { return r[j]; }
 };
-template <bool VEC>
-struct Four<bf16_t, VEC> {
+template <int CUT>
+struct Four<bf16_t, CUT> {
   i32x2 r;
-  SR_DEV void load(__amdgpu_buffer_rsrc_t b, uint32_t off, int left) {
-    if constexpr (VEC) {
+  SR_DEV void load(__amdgpu_buffer_rsrc_t b, uint32_t off, int hi) {
+    if constexpr (CUT != kSingle) {
       r = buf_load8(b, off * 2);
     } else {
       uint32_t h[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        h[j] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(b, (j < left ? off + j : kPast) * 2, 0, 0);
+        h[j] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(b, (j < hi ? off + j : kPast) * 2, 0, 0);
       r = i32x2{(int)(h[0] | h[1] << 16), (int)(h[2] | h[3] << 16)};
     }
   }
@@ -66,49 +94,33 @@ struct Four<bf16_t, VEC> {
 };
 // past: past the caches.
 constexpr int kPastCaches = 2;   // the buffer instructions' non-temporal bit
-template <typename T, bool VEC>
-SR_DEV void put4(__amdgpu_buffer_rsrc_t b, uint32_t off, int left, const float (&v)[4], bool past = false) {
-  if constexpr (VEC && sizeof(T) == 2) {
-    i32x2 w;
-    w[0] = (int)f2bf2(v[0], v[1]);
-    w[1] = (int)f2bf2(v[2], v[3]);
-    if (past) __builtin_amdgcn_raw_buffer_store_b64(w, b, off * 2, 0, kPastCaches);
-    else __builtin_amdgcn_raw_buffer_store_b64(w, b, off * 2, 0, 0);
-  } else if constexpr (VEC) {
-    const i32x4 w = __builtin_bit_cast(i32x4, f32x4{v[0], v[1], v[2], v[3]});
-    if (past) __builtin_amdgcn_raw_buffer_store_b128(w, b, off * 4, 0, kPastCaches);
-    else __builtin_amdgcn_raw_buffer_store_b128(w, b, off * 4, 0, 0);
+template <typename T, int CUT>
+SR_DEV void put4(__amdgpu_buffer_rsrc_t b, uint32_t off, int lo, int hi, const float (&v)[4], bool past = false) {
+  if (CUT == kWhole || (CUT == kShifted && lo == 0)) {
+    if constexpr (sizeof(T) == 2) {
+      const i32x2 w = {(int)f2bf2(v[0], v[1]), (int)f2bf2(v[2], v[3])};
+      if (past) __builtin_amdgcn_raw_buffer_store_b64(w, b, off * 2, 0, kPastCaches);
+      else __builtin_amdgcn_raw_buffer_store_b64(w, b, off * 2, 0, 0);
+    } else {
+      const i32x4 w = __builtin_bit_cast(i32x4, f32x4{v[0], v[1], v[2], v[3]});
+      if (past) __builtin_amdgcn_raw_buffer_store_b128(w, b, off * 4, 0, kPastCaches);
+      else __builtin_amdgcn_raw_buffer_store_b128(w, b, off * 4, 0, 0);
+    }
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint32_t o = (j < left ? off + j : kPast) * (uint32_t)sizeof(T);
+      const uint32_t o = (j >= lo && j < hi ? off + j : kPast) * (uint32_t)sizeof(T);
       if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16((short)f2bf(v[j]), b, o, 0, 0);
       else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(int, v[j]), b, o, 0, 0);
     }
   }
 }
 // A parameter's channels ([D], or a sample's row of it), `fill` where it is NULL.
-template <typename T, bool VEC>
-SR_DEV Four<T, VEC> param4(const void* p, int D, uint32_t c, int left, float fill) {
-  Four<T, VEC> v;
-  if (p) v.load(rows_of<T>(p, 0, 1, D), c, left);
+template <typename T, int CUT>
+SR_DEV Four<T, CUT> param4(const void* p, int D, uint32_t c, int hi, float fill) {
+  Four<T, CUT> v;
+  if (p) v.load(rows_of<T>(p, 0, 1, D), c, hi);
   else v.fill(fill);
-  return v;
-}
-// The same of gate, shift and scale, whose rows need not start on 16 bytes.
-template <bool VEC>
-SR_DEV Four<float, VEC> mod4(const float* p, int D, uint32_t c, int left, bool aligned, float fill) {
-  Four<float, VEC> v;
-  v.fill(fill);
-  if (!p) return v;
-  const __amdgpu_buffer_rsrc_t b = rows_of<float>(p, 0, 1, D);
-  if (aligned) {
-    v.load(b, c, left);
-  } else {
-    Four<float, false> w;
-    w.load(b, c, left);
-    v.r = w.r;
-  }
   return v;
 }
 
@@ -161,8 +173,8 @@ struct TeamSum {
 };
 
 // z -> Norm(z) in place, with the row's mean and reciprocal deviation; channels past D come out as zeros.
-template <int LPR, int NV>
-SR_DEV void norm_row(float (&z)[NV][4], const int (&left)[NV], float rD, bool layer, float eps, TeamSum<LPR>& sum,
+template <int LPR, int NV, int CUT>
+SR_DEV void norm_row(float (&z)[NV][4], const Place<LPR, NV, CUT>& at, float rD, bool layer, float eps, TeamSum<LPR>& sum,
                      float& mean, float& rstd) {
   mean = 0.f;
   if (layer) {
@@ -176,7 +188,7 @@ SR_DEV void norm_row(float (&z)[NV][4], const int (&left)[NV], float rD, bool la
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) z[i][j] = j < left[i] ? z[i][j] - mean : 0.f;
+      for (int j = 0; j < 4; ++j) z[i][j] = at.own(i, j) ? z[i][j] - mean : 0.f;
   }
   float q = 0.f;
 #pragma unroll
@@ -191,35 +203,18 @@ SR_DEV void norm_row(float (&z)[NV][4], const int (&left)[NV], float rD, bool la
     for (int j = 0; j < 4; ++j) z[i][j] *= rstd;
 }
 
-// Bit j: channel c + j of the row keeps its value (c a multiple of four).
+// Bit j: channel c + j of the row keeps its value.
 SR_DEV uint32_t keep_of(const DropArgs& d, uint64_t key, int64_t row, int D, int c) {
   const uint64_t r = d.first_row + (uint64_t)row;
   if (d.group) return drop_keep1(key, r / (uint64_t)d.group, d.thresh) ? 0xFu : 0u;
   return drop_keep4(key, r * (uint64_t)D + (uint64_t)c, d.thresh);
 }
 
-// A thread's channels: first of each run, its offset from a workgroup's first row, and the channels from it to the row's end
-// (0 or less: none; with VEC 4 or more otherwise).
-template <int LPR, int NV>
-struct Place {
-  uint32_t c[NV], off[NV];
-  int left[NV];
-  SR_DEV Place(int t, int team, int D) {
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int k = (i * LPR + t) * 4;
-      left[i] = D - k;
-      c[i] = k < D ? (uint32_t)k : kPast;
-      off[i] = k < D ? (uint32_t)(team * D + k) : kPast;
-    }
-  }
-};
-
 // Workgroup (b, k): rows k R .. of sample b, a team every TEAMS-th of them; the next row's values are on their way while
 // one is computed.  A sample's parameters become one factor and one summand per channel and norm:
 //   x1 = x + keep (n w1 + b1),  w1 = f gate res_scale post_w, b1 alike;   u = v w2 + b2,  w2 = (1 + scale) pre_w, ..
-template <typename T, typename X, int LPR, int NV, bool VEC>
-__global__ __launch_bounds__(fwd_threads(LPR)) void residual_norm_fwd_kernel(ResidualNorm a, bool modvec, int chunks) {
+template <typename T, typename X, int LPR, int NV, int CUT>
+__global__ __launch_bounds__(fwd_threads(LPR)) void residual_norm_fwd_kernel(ResidualNorm a, int chunks) {
   constexpr int NT = fwd_threads(LPR), TEAMS = NT / LPR;
   __shared__ float slots[2][2][16];
   TeamSum<LPR> sum{slots};
@@ -231,17 +226,17 @@ __global__ __launch_bounds__(fwd_threads(LPR)) void residual_norm_fwd_kernel(Res
   // x1 stays in the caches where a backward is to read it (16200 x 1024, both directions: 96 us, with x1 past them 103; forward alone 41, 38)
   const bool past = M * D * (int64_t)sizeof(T) >= kStreamBytes, past_x1 = past && !a.stats;
   const float rD = 1.0f / (float)D;
-  const Place<LPR, NV> at(t, team, D);
-  Four<X, VEC> xr[NV];
-  Four<T, VEC> yr[NV];
+  const Place<LPR, NV, CUT> at(t, team, D);
+  Four<X, CUT> xr[NV];
+  Four<T, CUT> yr[NV];
   auto load = [&](int sb) {
     const int rows = min(TEAMS, s1 - sb);
     const int64_t row0 = (int64_t)b * a.S + sb;
     const __amdgpu_buffer_rsrc_t bx = rows_of<X>(a.x, row0, rows, D), by = rows_of<T>(a.y, row0, rows, D);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      xr[i].load(bx, at.off[i], at.left[i]);
-      yr[i].load(by, at.off[i], at.left[i]);
+      xr[i].load(bx, at.off[i], at.hi(i));
+      yr[i].load(by, at.off[i], at.hi(i));
     }
   };
   if (s0 < s1) load(s0);
@@ -251,15 +246,15 @@ __global__ __launch_bounds__(fwd_threads(LPR)) void residual_norm_fwd_kernel(Res
     auto mod = [&](const float* p) { return p ? p + b * a.mod_stride : nullptr; };
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const uint32_t c = at.c[i];
-      const int left = at.left[i];
-      const Four<T, VEC> pw = param4<T, VEC>(a.post ? a.w.post_w : nullptr, D, c, left, 1.f);
-      const Four<T, VEC> pb = param4<T, VEC>(a.post ? a.w.post_b : nullptr, D, c, left, 0.f);
-      const Four<T, VEC> rs = param4<T, VEC>(a.w.res_scale, D, c, left, 1.f);
-      const Four<T, VEC> nw = param4<T, VEC>(a.w.pre_w, D, c, left, 1.f), nb = param4<T, VEC>(a.w.pre_b, D, c, left, 0.f);
-      const Four<float, VEC> g = mod4<VEC>(mod(a.w.gate), D, c, left, modvec, 1.f);
-      const Four<float, VEC> sc = mod4<VEC>(mod(a.w.scale), D, c, left, modvec, 0.f);
-      const Four<float, VEC> sh = mod4<VEC>(mod(a.w.shift), D, c, left, modvec, 0.f);
+      const uint32_t c = at.c(i);
+      const int left = at.hi(i);
+      const Four<T, CUT> pw = param4<T, CUT>(a.post ? a.w.post_w : nullptr, D, c, left, 1.f);
+      const Four<T, CUT> pb = param4<T, CUT>(a.post ? a.w.post_b : nullptr, D, c, left, 0.f);
+      const Four<T, CUT> rs = param4<T, CUT>(a.w.res_scale, D, c, left, 1.f);
+      const Four<T, CUT> nw = param4<T, CUT>(a.w.pre_w, D, c, left, 1.f), nb = param4<T, CUT>(a.w.pre_b, D, c, left, 0.f);
+      const Four<float, CUT> g = param4<float, CUT>(mod(a.w.gate), D, c, left, 1.f);
+      const Four<float, CUT> sc = param4<float, CUT>(mod(a.w.scale), D, c, left, 0.f);
+      const Four<float, CUT> sh = param4<float, CUT>(mod(a.w.shift), D, c, left, 0.f);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const float ga = g.at(j) * rs.at(j) * a.drop.factor;
@@ -280,14 +275,14 @@ __global__ __launch_bounds__(fwd_threads(LPR)) void residual_norm_fwd_kernel(Res
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        x[i][j] = xr[i].at(j);
-        n[i][j] = yr[i].at(j);
+        x[i][j] = CUT != kShifted || at.own(i, j) ? xr[i].at(j) : 0.f;
+        n[i][j] = CUT != kShifted || at.own(i, j) ? yr[i].at(j) : 0.f;
       }
     if (sb + TEAMS < s1) load(sb + TEAMS);
     if (a.y) {
       if (a.post) {
         float mean, rstd;
-        norm_row<LPR, NV>(n, at.left, rD, layer, a.eps, sum, mean, rstd);
+        norm_row(n, at, rD, layer, a.eps, sum, mean, rstd);
         if (a.stats && on && t == 0) {
           a.stats[row] = mean;
           a.stats[M + row] = rstd;
@@ -296,18 +291,18 @@ __global__ __launch_bounds__(fwd_threads(LPR)) void residual_norm_fwd_kernel(Res
       const __amdgpu_buffer_rsrc_t bx1 = rows_of<X>(a.x1, row0, rows, D);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const uint32_t keep = drops ? keep_of(a.drop, key, row, D, (i * LPR + t) * 4) : 0xFu;
+        const uint32_t keep = drops ? keep_of(a.drop, key, row, D, (int)at.c(i)) : 0xFu;
         float o[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[j] = x[i][j] + (keep >> j & 1u ? fmaf(n[i][j], w1[i][j], b1[i][j]) : 0.f);
-        put4<X, VEC>(bx1, at.off[i], at.left[i], o, past_x1);
+        put4<X, CUT>(bx1, at.off[i], at.lo(i), at.hi(i), o, past_x1);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[i][j] = j < at.left[i] ? to_f32<X>(from_f32<X>(o[j])) : 0.f;   // the next norm's input is what is kept
+        for (int j = 0; j < 4; ++j) x[i][j] = at.own(i, j) ? to_f32<X>(from_f32<X>(o[j])) : 0.f;   // the next norm's input is what is kept
       }
     }
     if (!next) continue;
     float mean, rstd;
-    norm_row<LPR, NV>(x, at.left, rD, layer, a.eps, sum, mean, rstd);
+    norm_row(x, at, rD, layer, a.eps, sum, mean, rstd);
     if (a.stats && on && t == 0) {
       a.stats[2 * M + row] = mean;
       a.stats[3 * M + row] = rstd;
@@ -318,12 +313,12 @@ __global__ __launch_bounds__(fwd_threads(LPR)) void residual_norm_fwd_kernel(Res
       float o[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[j] = fmaf(x[i][j], w2[i][j], b2[i][j]);
-      put4<T, VEC>(bu, at.off[i], at.left[i], o, past);
+      put4<T, CUT>(bu, at.off[i], at.lo(i), at.hi(i), o, past);
       if (a.uq) {   // blocks of 128 channels: 32 neighbouring lanes
         uint32_t m = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          if (j >= at.left[i]) o[j] = 0.f;
+          if (!at.own(i, j)) o[j] = 0.f;
           m = max(m, __float_as_uint(o[j]) & 0x7FFFFFFFu);
         }
         auto over = [&](auto ctl) {
@@ -339,8 +334,8 @@ __global__ __launch_bounds__(fwd_threads(LPR)) void residual_norm_fwd_kernel(Res
         const float inv = f8_inverse(m, E);
         const int Dp = (D + 127) / 128 * 128, ch = (i * LPR + t) * 4;
         if (on && ch < Dp) {
-          *reinterpret_cast<uint32_t*>(a.uq + row * Dp + ch) =
-              f8_code4(f8_clamp(o[0] * inv), f8_clamp(o[1] * inv), f8_clamp(o[2] * inv), f8_clamp(o[3] * inv));
+          const uint32_t q = f8_code4(f8_clamp(o[0] * inv), f8_clamp(o[1] * inv), f8_clamp(o[2] * inv), f8_clamp(o[3] * inv));
+          *reinterpret_cast<uint32_t*>(a.uq + row * Dp + ch) = CUT == kShifted && ch < D ? q >> (8 * at.lo(i)) : q;
           if ((t & 31) == 0) a.ue[(int64_t)(ch / 128) * ((M + 15) / 16 * 16) + row] = (uint8_t)E;
         }
       }
@@ -351,8 +346,8 @@ __global__ __launch_bounds__(fwd_threads(LPR)) void residual_norm_fwd_kernel(Res
 // Workgroup (b, k): rows k R .. of sample b; its part of the four column sums at part[((b chunks + k) 4 + i) D].  As in
 // the forward the next row is on its way while a row is computed.  Rows and channels that are not there read as zeros in
 // every tensor and statistic, and add nothing.
-template <typename T, typename X, int LPR, int NV, bool VEC>
-__global__ __launch_bounds__(bwd_threads(LPR), 2) void residual_norm_bwd_kernel(ResidualNorm a, bool modvec, int chunks) {
+template <typename T, typename X, int LPR, int NV, int CUT>
+__global__ __launch_bounds__(bwd_threads(LPR), 2) void residual_norm_bwd_kernel(ResidualNorm a, int chunks) {
   constexpr int NT = bwd_threads(LPR), TEAMS = NT / LPR, COLS = LPR * NV * 4;
   __shared__ float slots[2][2][16];
   __shared__ __attribute__((aligned(16))) float cols[TEAMS > 1 ? TEAMS : 1][TEAMS > 1 ? COLS : 4];
@@ -365,15 +360,15 @@ __global__ __launch_bounds__(bwd_threads(LPR), 2) void residual_norm_bwd_kernel(
   const bool past = M * D * (int64_t)sizeof(T) >= kStreamBytes;
   const uint64_t key = drops ? drop_key(a.drop) : 0;
   const float rD = 1.0f / (float)D;
-  const Place<LPR, NV> at(t, team, D);
+  const Place<LPR, NV, CUT> at(t, team, D);
   float acc[4][NV][4], wpre[NV][4], wpost[NV][4];   // sums; (1 + scale) pre_w and gate res_scale post_w of the sample
   {
     const float *scale = a.w.scale ? a.w.scale + b * a.mod_stride : nullptr, *gate = a.w.gate ? a.w.gate + b * a.mod_stride : nullptr;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const Four<T, VEC> pw = param4<T, VEC>(a.w.pre_w, D, at.c[i], at.left[i], 1.f), rs = param4<T, VEC>(a.w.res_scale, D, at.c[i], at.left[i], 1.f);
-      const Four<T, VEC> ow = param4<T, VEC>(a.post ? a.w.post_w : nullptr, D, at.c[i], at.left[i], 1.f);
-      const Four<float, VEC> sc = mod4<VEC>(scale, D, at.c[i], at.left[i], modvec, 0.f), gt = mod4<VEC>(gate, D, at.c[i], at.left[i], modvec, 1.f);
+      const Four<T, CUT> pw = param4<T, CUT>(a.w.pre_w, D, at.c(i), at.hi(i), 1.f), rs = param4<T, CUT>(a.w.res_scale, D, at.c(i), at.hi(i), 1.f);
+      const Four<T, CUT> ow = param4<T, CUT>(a.post ? a.w.post_w : nullptr, D, at.c(i), at.hi(i), 1.f);
+      const Four<float, CUT> sc = param4<float, CUT>(scale, D, at.c(i), at.hi(i), 0.f), gt = param4<float, CUT>(gate, D, at.c(i), at.hi(i), 1.f);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         wpre[i][j] = (1.f + sc.at(j)) * pw.at(j);
@@ -383,8 +378,8 @@ __global__ __launch_bounds__(bwd_threads(LPR), 2) void residual_norm_bwd_kernel(
       }
     }
   }
-  Four<X, VEC> dxr[NV], xr[NV];
-  Four<T, VEC> dur[NV], yr[NV];
+  Four<X, CUT> dxr[NV], xr[NV];
+  Four<T, CUT> dur[NV], yr[NV];
   float mx, rx, my, ry;   // the row's statistics
   const bool has_y = a.y && a.post;
   auto load = [&](int sb) {
@@ -401,10 +396,10 @@ __global__ __launch_bounds__(bwd_threads(LPR), 2) void residual_norm_bwd_kernel(
     ry = stat(1, has_y);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      xr[i].load(bx, at.off[i], at.left[i]);
-      dur[i].load(bdu, at.off[i], at.left[i]);
-      dxr[i].load(bdx, at.off[i], at.left[i]);
-      yr[i].load(by, at.off[i], at.left[i]);
+      xr[i].load(bx, at.off[i], at.hi(i));
+      dur[i].load(bdu, at.off[i], at.hi(i));
+      dxr[i].load(bdx, at.off[i], at.hi(i));
+      yr[i].load(by, at.off[i], at.hi(i));
     }
   };
   if (s0 < s1) load(s0);
@@ -413,7 +408,7 @@ __global__ __launch_bounds__(bwd_threads(LPR), 2) void residual_norm_bwd_kernel(
     const int rows = min(TEAMS, s1 - sb);
     const int64_t row0 = (int64_t)b * a.S + sb;
     float dx[NV][4], v[NV][4], g[NV][4];
-    Four<T, VEC> yc[NV];
+    Four<T, CUT> yc[NV];
     const float rstd = rx, pmean = my, prstd = a.post ? ry : 1.f;
     float c1 = 0.f, c2 = 0.f;
 #pragma unroll
@@ -423,7 +418,7 @@ __global__ __launch_bounds__(bwd_threads(LPR), 2) void residual_norm_bwd_kernel(
       for (int j = 0; j < 4; ++j) {
         dx[i][j] = dxr[i].at(j);
         v[i][j] = (xr[i].at(j) - mx) * rx;
-        g[i][j] = dur[i].at(j);
+        g[i][j] = CUT != kShifted || at.own(i, j) ? dur[i].at(j) : 0.f;
       }
     }
     if (sb + TEAMS < s1) load(sb + TEAMS);
@@ -445,16 +440,16 @@ __global__ __launch_bounds__(bwd_threads(LPR), 2) void residual_norm_bwd_kernel(
     for (int i = 0; i < NV; ++i) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) dx[i][j] = fmaf(rstd, g[i][j] - fmaf(v[i][j], c2, c1), dx[i][j]);
-      put4<X, VEC>(bdx, at.off[i], at.left[i], dx[i], past);
+      put4<X, CUT>(bdx, at.off[i], at.lo(i), at.hi(i), dx[i], past);
     }
     if (!a.y) continue;
     c1 = c2 = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const uint32_t keep = drops ? keep_of(a.drop, key, row0 + team, D, (i * LPR + t) * 4) : 0xFu;
+      const uint32_t keep = drops ? keep_of(a.drop, key, row0 + team, D, (int)at.c(i)) : 0xFu;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const bool in = team < rows && j < at.left[i] && (keep >> j & 1u);
+        const bool in = team < rows && at.own(i, j) && (keep >> j & 1u);
         const float d = in ? dx[i][j] * a.drop.factor : 0.f;
         const float n = (yc[i].at(j) - pmean) * prstd;
         v[i][j] = n;
@@ -476,7 +471,7 @@ __global__ __launch_bounds__(bwd_threads(LPR), 2) void residual_norm_bwd_kernel(
     }
     const __amdgpu_buffer_rsrc_t bdy = rows_of<T>(a.dy, row0, rows, D);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) put4<T, VEC>(bdy, at.off[i], at.left[i], g[i], past);
+    for (int i = 0; i < NV; ++i) put4<T, CUT>(bdy, at.off[i], at.lo(i), at.hi(i), g[i], past);
   }
 
   float* part = a.part + (size_t)blockIdx.x * 4 * D;
@@ -484,12 +479,15 @@ __global__ __launch_bounds__(bwd_threads(LPR), 2) void residual_norm_bwd_kernel(
   for (int q = 0; q < 4; ++q) {
     if constexpr (TEAMS == 1) {
 #pragma unroll
-      for (int i = 0; i < NV; ++i) put4<float, VEC>(rows_of<float>(part, q, 1, D), at.c[i], at.left[i], acc[q][i]);
+      for (int i = 0; i < NV; ++i) put4<float, CUT>(rows_of<float>(part, q, 1, D), at.c(i), at.lo(i), at.hi(i), acc[q][i]);
     } else {
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < NV; ++i)
-        *reinterpret_cast<f32x4*>(&cols[team][(i * LPR + t) * 4]) = f32x4{acc[q][i][0], acc[q][i][1], acc[q][i][2], acc[q][i][3]};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)   // natural order: a shifted run's own channels follow the run before
+          if (CUT != kShifted) cols[team][(i * LPR + t) * 4 + j] = acc[q][i][j];
+          else if (at.own(i, j)) cols[team][at.c(i) + j] = acc[q][i][j];
       __syncthreads();
       for (int d = threadIdx.x; d < D; d += NT) {
         float s = 0.f;
@@ -589,32 +587,35 @@ int bwd_chunks(int B, int S, int D) {
   return chunks_of(B, S, D, threads, 512 * 256 / threads);
 }
 
-template <typename T, typename X, int LPR, int NV, bool VEC>
+template <typename T, typename X, int LPR, int NV, int CUT>
 hipError_t run_rows(const ResidualNorm& a, bool bwd, hipStream_t st) {
-  auto al = [](const void* p) { return ((uintptr_t)p & 15) == 0; };
-  const bool modvec = VEC && al(a.w.gate) && al(a.w.shift) && al(a.w.scale) && a.mod_stride % 4 == 0;
   const int chunks = bwd ? bwd_chunks(a.B, a.S, a.D) : fwd_chunks(a.B, a.S, a.D);
   const dim3 grid((unsigned)a.B * (unsigned)chunks);
-  if (bwd) SR_LAUNCH((residual_norm_bwd_kernel<T, X, LPR, NV, VEC>), grid, dim3(bwd_threads(LPR)), 0, st, a, modvec, chunks);
-  else SR_LAUNCH((residual_norm_fwd_kernel<T, X, LPR, NV, VEC>), grid, dim3(fwd_threads(LPR)), 0, st, a, modvec, chunks);
+  if (bwd) SR_LAUNCH((residual_norm_bwd_kernel<T, X, LPR, NV, CUT>), grid, dim3(bwd_threads(LPR)), 0, st, a, chunks);
+  else SR_LAUNCH((residual_norm_fwd_kernel<T, X, LPR, NV, CUT>), grid, dim3(fwd_threads(LPR)), 0, st, a, chunks);
   return hipGetLastError();
 }
 
-template <typename T, typename X, bool VEC>
+template <typename T, typename X, int LPR, int CUT>
+hipError_t run_runs(const ResidualNorm& a, bool bwd, hipStream_t st) {   // three runs where they hold the row
+  return a.D <= 12 * LPR ? run_rows<T, X, LPR, 3, CUT>(a, bwd, st) : run_rows<T, X, LPR, 4, CUT>(a, bwd, st);
+}
+template <typename T, typename X, int CUT>
 hipError_t run_width(const ResidualNorm& a, bool bwd, hipStream_t st) {
   switch (lanes_of(a.D)) {
-    case 32: return run_rows<T, X, 32, 1, VEC>(a, bwd, st);
+    case 32: return run_rows<T, X, 32, 1, CUT>(a, bwd, st);
     case 64:
-      if (a.D <= 256) return run_rows<T, X, 64, 1, VEC>(a, bwd, st);
-      return a.D <= 512 ? run_rows<T, X, 64, 2, VEC>(a, bwd, st) : run_rows<T, X, 64, 4, VEC>(a, bwd, st);
-    case 128: return run_rows<T, X, 128, 4, VEC>(a, bwd, st);
-    case 256: return run_rows<T, X, 256, 4, VEC>(a, bwd, st);
-    default: return run_rows<T, X, 512, 4, VEC>(a, bwd, st);
+      if (a.D <= 256) return run_rows<T, X, 64, 1, CUT>(a, bwd, st);
+      return a.D <= 512 ? run_rows<T, X, 64, 2, CUT>(a, bwd, st) : run_runs<T, X, 64, CUT>(a, bwd, st);
+    case 128: return run_runs<T, X, 128, CUT>(a, bwd, st);
+    case 256: return run_runs<T, X, 256, CUT>(a, bwd, st);
+    default: return run_runs<T, X, 512, CUT>(a, bwd, st);
   }
 }
 template <typename T, typename X>
-hipError_t run(const ResidualNorm& a, bool bwd, hipStream_t st) {   // the tensors themselves start on 16 bytes
-  return a.D % 4 == 0 ? run_width<T, X, true>(a, bwd, st) : run_width<T, X, false>(a, bwd, st);
+hipError_t run(const ResidualNorm& a, bool bwd, hipStream_t st) {
+  if (a.D < 4) return run_rows<T, X, 32, 1, kSingle>(a, bwd, st);
+  return a.D % 4 == 0 ? run_width<T, X, kWhole>(a, bwd, st) : run_width<T, X, kShifted>(a, bwd, st);
 }
 
 hipError_t run_types(int dtype, int stream_dtype, const ResidualNorm& a, bool bwd, hipStream_t st) {

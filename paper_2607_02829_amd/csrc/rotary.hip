@@ -34,17 +34,11 @@ SR_DEV float2 turn_of(double t) {
 
 constexpr int kThreads = 256, kUnroll = 4;
 
-template <typename T, int V>
-struct Pack {
+// 16 bytes of channels.
+template <typename T>
+struct Vec16 {
+  static constexpr int V = 16 / (int)sizeof(T);
   T v[V];
-};
-template <>
-struct __attribute__((aligned(16))) Pack<bf16_t, 8> {
-  bf16_t v[8];
-};
-template <>
-struct __attribute__((aligned(16))) Pack<float, 4> {
-  float v[4];
 };
 
 // What is left of i after whole d's, and their number; magic = ceil(2^32 / d), exact for i d < 2^32.
@@ -56,24 +50,39 @@ struct Units {
   uint32_t magic_head, magic_token;
 };
 
-// PAIRED: a unit turns V pairs, of channels c0 .. and c1 ..; otherwise V / 2 pairs of neighbours in V channels.
-template <typename T, int V, bool PAIRED>
+// PAIRED: a unit turns V pairs, of channels c0 .. and c1 ..; otherwise V / 2 pairs of neighbours in V channels.  Without
+// WHOLE the last unit of a head's turning channels, and of those that do not turn, may have fewer.
+template <typename T, bool PAIRED, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary a, Units un) {
   extern __shared__ float2 cs[];   // [tokens][P]
+  typedef Vec16<T> Vec;
+  constexpr int V = Vec::V;
   const int P = a.first[3];
   const int64_t rows = (int64_t)a.B * a.S, row0 = (int64_t)blockIdx.x * un.tokens;
   const uint32_t n = (uint32_t)un.tokens * un.per_token;
-  typedef Pack<T, V> Vec;
   const bool past = rows * a.heads * a.hd * (int64_t)sizeof(T) >= kStreamBytes;
-  auto put = [&](T* p, const Vec& v) {
-    if constexpr (V > 1) store16(p, __builtin_bit_cast(i32x4, v), past);
-    else *reinterpret_cast<Vec*>(p) = v;
+  auto get = [&](Vec& v, const T* p, int count) {
+    if (WHOLE || count == V) {
+      v = __builtin_bit_cast(Vec, load16(p));
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) v.v[j] = j < count ? p[j] : T{};
+    }
+  };
+  auto put = [&](T* p, const Vec& v, int count) {
+    if (WHOLE || count == V) {
+      store16(p, __builtin_bit_cast(i32x4, v), past);
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (j < count) p[j] = v.v[j];
+    }
   };
   bool first = true;
   for (uint32_t base = 0; base < n || first; base += kThreads * kUnroll) {
     Vec lo[kUnroll], hi[kUnroll];
     int64_t oy[kUnroll];
-    int c1[kUnroll], at[kUnroll];   // at: first pair in cs, -1: channels that do not turn, -2: nothing
+    int count[kUnroll], at[kUnroll];   // channels of the unit (of one side, PAIRED); first pair in cs, -1: they do not turn, -2: nothing
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k) {
       const uint32_t i = base + threadIdx.x + kThreads * k;
@@ -85,17 +94,17 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary a, Units un) {
         if (u < un.rot) {
           const int p = (int)u * (PAIRED ? V : V / 2);
           at[k] = (int)t * P + p;
-          c0 = a.neighbours ? 2 * p : p;
-          c1[k] = a.neighbours ? 1 : P;   // from c0
+          c0 = PAIRED ? p : 2 * p;
+          count[k] = WHOLE ? V : min(V, PAIRED ? P - p : 2 * (P - p));
         } else {
           at[k] = -1;
           c0 = 2 * P + (int)(u - un.rot) * V;
-          c1[k] = 0;
+          count[k] = WHOLE ? V : min(V, a.hd - c0);
         }
         const T* xp = (const T*)a.x + (row0 + t) * a.ldx + (int64_t)h * a.hd + c0;
         oy[k] = (row0 + t) * a.ldy + (int64_t)h * a.hd + c0;
-        lo[k] = *reinterpret_cast<const Vec*>(xp);
-        if (PAIRED && at[k] >= 0) hi[k] = *reinterpret_cast<const Vec*>(xp + c1[k]);
+        get(lo[k], xp, count[k]);
+        if (PAIRED && at[k] >= 0) get(hi[k], xp + P, count[k]);
       }
     }
     if (first) {
@@ -135,15 +144,17 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary a, Units un) {
         if constexpr (PAIRED) {
 #pragma unroll
           for (int j = 0; j < V; ++j) {
+            if (!WHOLE && j >= count[k]) break;
             const float2 c = cs[at[k] + j];
             const float x0 = to_f32<T>(lo[k].v[j]), x1 = to_f32<T>(hi[k].v[j]);
             lo[k].v[j] = from_f32<T>(fmaf(x0, c.x, -x1 * c.y));
             hi[k].v[j] = from_f32<T>(fmaf(x1, c.x, x0 * c.y));
           }
-          put(yp + c1[k], hi[k]);
+          put(yp + P, hi[k], count[k]);
         } else {
 #pragma unroll
           for (int j = 0; j < V / 2; ++j) {
+            if (!WHOLE && 2 * j >= count[k]) break;
             const float2 c = cs[at[k] + j];
             const float x0 = to_f32<T>(lo[k].v[2 * j]), x1 = to_f32<T>(lo[k].v[2 * j + 1]);
             lo[k].v[2 * j] = from_f32<T>(fmaf(x0, c.x, -x1 * c.y));
@@ -151,18 +162,19 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary a, Units un) {
           }
         }
       }
-      put(yp, lo[k]);
+      put(yp, lo[k], count[k]);
     }
   }
 }
 
-template <typename T, int V, bool PAIRED>
+template <typename T, bool PAIRED>
 hipError_t run(const Rotary& a, hipStream_t st) {
-  const int P = a.first[3];
+  constexpr int V = Vec16<T>::V;
+  const int P = a.first[3], turning = PAIRED ? P : 2 * P, rest = a.hd - 2 * P;
   Units un;
-  un.rot = (uint32_t)(PAIRED ? P / V : 2 * P / V);
+  un.rot = (uint32_t)((turning + V - 1) / V);
   const bool copies = a.x != a.y;   // in place the channels that do not turn stay
-  un.per_head = un.rot + (copies ? (uint32_t)((a.hd - 2 * P) / V) : 0);
+  un.per_head = un.rot + (copies ? (uint32_t)((rest + V - 1) / V) : 0);
   un.per_token = un.per_head * (uint32_t)a.heads;
   if (un.per_token == 0) return hipSuccess;
   // about four units a thread, 16 tokens at most
@@ -170,25 +182,22 @@ hipError_t run(const Rotary& a, hipStream_t st) {
   un.magic_head = (uint32_t)(((1ull << 32) + un.per_head - 1) / un.per_head);
   un.magic_token = (uint32_t)(((1ull << 32) + un.per_token - 1) / un.per_token);
   const int64_t rows = (int64_t)a.B * a.S, wgs = (rows + un.tokens - 1) / un.tokens;
-  SR_LAUNCH((rotary_kernel<T, V, PAIRED>), dim3((unsigned)wgs), dim3(kThreads),
-            (uint32_t)(un.tokens * P * sizeof(float2)), st, a, un);
+  const dim3 grid((unsigned)wgs);
+  const uint32_t lds = (uint32_t)(un.tokens * P * sizeof(float2));
+  if (turning % V == 0 && (!copies || rest % V == 0)) SR_LAUNCH((rotary_kernel<T, PAIRED, true>), grid, dim3(kThreads), lds, st, a, un);
+  else SR_LAUNCH((rotary_kernel<T, PAIRED, false>), grid, dim3(kThreads), lds, st, a, un);
   return hipGetLastError();
 }
 
-template <typename T, int V>
+template <typename T>
 hipError_t run_type(const Rotary& a, hipStream_t st) {
-  const int P = a.first[3];
-  auto whole = [](const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld * sizeof(T) % 16 == 0; };
-  // 16 bytes at a time where rows, heads and the turning channels start and end on them
-  if (whole(a.x, a.ldx) && whole(a.y, a.ldy) && a.hd % V == 0 && (a.neighbours ? 2 * P : P) % V == 0)
-    return a.neighbours ? run<T, V, false>(a, st) : run<T, V, true>(a, st);
-  return run<T, 1, true>(a, st);
+  return a.neighbours ? run<T, false>(a, st) : run<T, true>(a, st);
 }
 
 }  // namespace
 
 hipError_t launch_rotary(int dtype, const Rotary& a, hipStream_t st) {
-  return dtype == kBF16 ? run_type<bf16_t, 8>(a, st) : run_type<float, 4>(a, st);
+  return dtype == kBF16 ? run_type<bf16_t>(a, st) : run_type<float>(a, st);
 }
 
 }  // namespace sr

@@ -47,6 +47,12 @@ def test_dropout(M, N, dtype, resid, p, group):
     _run(M, N, p, dtype, resid, group=group)
 
 
+@pytest.mark.parametrize("group", [0, 9])
+def test_results_past_the_caches(group):
+    _run(2100, 1025, 0.3, "bf16", True, group=group)
+    _run(1100, 1024, 0.3, "f32", False, group=group)
+
+
 @pytest.mark.parametrize("first_row", [1, 2, 3, (1 << 40) + 1, (1 << 62) + 3])   # draws that start inside a word, far ones
 @pytest.mark.parametrize("N", [13, 16, 18])
 def test_first_row(first_row, N):

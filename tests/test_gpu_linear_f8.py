@@ -148,7 +148,7 @@ def _check(got, z, P, K, dtype, act=0):
 
 SIZES = [(1, 1, 1), (1, 16, 128), (1, 4096, 1024), (3, 17, 129), (16, 64, 500), (5, 1024, 4096), (33, 276, 256), (64, 64, 64),
          (100, 130, 300), (128, 128, 128), (129, 257, 1000), (200, 1000, 70), (300, 300, 300), (257, 512, 640),
-         (1000, 276, 256), (512, 1024, 1024), (2013, 1024, 256), (1030, 2050, 384), (4083, 276, 256), (4050, 1024, 512)]
+         (1000, 276, 256), (512, 1024, 1024), (2013, 1024, 256), (1030, 2050, 384), (4083, 276, 256), (4050, 1024, 512), (2111, 1023, 1030), (17000, 1030, 1024)]
 
 
 @pytest.mark.parametrize("M,N,K", SIZES)

@@ -35,6 +35,15 @@ CASES = [
     (2, 9, 4000, False, False, "res_scale pre_w pre_b", 0.1, 0, "bf16", "f32"),
     (1, 5, 8192, False, True, "post_w post_b res_scale pre_w pre_b gate shift scale", 0.1, 0, "bf16", "f32"),
     (1, 3, 8191, True, True, "post_w pre_w", 0.0, 0, "f32", "f32"),
+    (2, 40, 2, False, True, "post_w res_scale gate shift scale", 0.2, 0, "bf16", "f32"),
+    (1, 33, 3, True, True, "post_w post_b pre_w pre_b", 0.2, 0, "f32", "f32"),
+    (3, 21, 5, False, False, "res_scale gate", 0.2, 0, "bf16", "bf16"),
+    (2, 25, 30, True, True, "post_w pre_w scale", 0.1, 0, "bf16", "f32"),
+    (1, 90, 770, False, True, "post_w post_b res_scale pre_w pre_b", 0.1, 0, "bf16", "f32"),
+    (2, 30, 1536, True, True, "post_w pre_w gate", 0.0, 0, "f32", "f32"),
+    (1, 20, 2999, False, True, "res_scale shift scale", 0.1, 0, "bf16", "bf16"),
+    (1, 7, 5001, True, True, "post_w pre_w", 0.1, 0, "bf16", "f32"),
+    (1, 9000, 64, False, True, "post_w post_b gate", 0.1, 0, "bf16", "f32"),             # results past the caches
     (1200, 2, 32, False, True, "res_scale gate shift scale", 0.1, 2, "bf16", "f32"),     # more samples than workgroups
 ]
 
@@ -239,7 +248,7 @@ def test_dropped_nan_and_other_rows():
 
 def test_codes_straight_from_the_norm():
     import torch
-    for D, rms in ((64, False), (128, True), (200, False), (1024, False), (1100, True), (4096, True)):
+    for D, rms in ((64, False), (128, True), (200, False), (1024, False), (1100, True), (4096, True), (1, True), (3, False), (129, False), (255, True), (1022, True)):
         c = (2, 21, D, rms, True, "post_w res_scale pre_w shift scale", 0.1, 0, "bf16", "f32")
         cfg, x, y, w, w64, keep, _ = _setup(c, mod_extra=4 - D % 4)
         M = 42
