@@ -93,8 +93,9 @@ class SrRotary(ctypes.Structure):
                 ("step", ctypes.c_double * 3), ("freqs", ctypes.POINTER(ctypes.c_double))]
 
     def __init__(self, grid, pairs, layout=SR_ROT_HALVES, base=10000.0, origin=None, step=None, freqs=None):
-        n = len(grid)
-        origin, step = origin or [0.0] * n, step or [1.0] * n
+        n, grid, pairs = len(grid), list(grid), list(pairs)
+        origin = [0.0] * n if origin is None else list(origin)
+        step = [1.0] * n if step is None else list(step)
         if not 1 <= n <= 3 or any(len(v) != n for v in (pairs, origin, step)):
             raise ValueError("one to three axes, with an entry of pairs, origin and step for each")
         if freqs is not None and len(freqs) != sum(pairs):

@@ -762,6 +762,7 @@ sr_status check_residual_norm(const sr_residual_norm* c) {
   SR_CHECK(c->B >= 1 && c->S >= 1 && c->D >= 1, SR_EINVAL, "sizes must be positive (B=%d S=%d D=%d)", c->B, c->S, c->D);
   SR_CHECK(c->D <= sr::kMaxNormD, SR_EUNSUPPORTED, "D=%d > %d", c->D, sr::kMaxNormD);
   SR_CHECK((int64_t)c->B * c->S < (1ll << 31), SR_EUNSUPPORTED, "2^31 rows or more are not supported (B=%d S=%d)", c->B, c->S);
+  SR_CHECK(c->B <= 1 << 22, SR_EUNSUPPORTED, "B=%d > 2^22 samples", c->B);   // a workgroup or more each
   SR_CHECK(c->eps > 0.f, SR_EINVAL, "eps must be > 0");
   return check_drop(&c->drop);
 }

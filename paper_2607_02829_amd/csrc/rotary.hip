@@ -58,7 +58,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary a, Units un) {
   typedef Vec16<T> Vec;
   constexpr int V = Vec::V;
   const int P = a.first[3];
-  const int64_t rows = (int64_t)a.B * a.S, row0 = (int64_t)blockIdx.x * un.tokens;
+  const int64_t rows = (int64_t)a.B * a.S, row0 = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * un.tokens;
   const uint32_t n = (uint32_t)un.tokens * un.per_token;
   const bool past = rows * a.heads * a.hd * (int64_t)sizeof(T) >= kStreamBytes;
   auto get = [&](Vec& v, const T* p, int count) {
@@ -182,7 +182,8 @@ hipError_t run(const Rotary& a, hipStream_t st) {
   un.magic_head = (uint32_t)(((1ull << 32) + un.per_head - 1) / un.per_head);
   un.magic_token = (uint32_t)(((1ull << 32) + un.per_token - 1) / un.per_token);
   const int64_t rows = (int64_t)a.B * a.S, wgs = (rows + un.tokens - 1) / un.tokens;
-  const dim3 grid((unsigned)wgs);
+  constexpr int64_t kMaxX = 1 << 22;   // 256 threads each: a launch counts threads along x in 32 bits
+  const dim3 grid((unsigned)std::min(wgs, kMaxX), (unsigned)((wgs + kMaxX - 1) / kMaxX));
   const uint32_t lds = (uint32_t)(un.tokens * P * sizeof(float2));
   if (turning % V == 0 && (!copies || rest % V == 0)) SR_LAUNCH((rotary_kernel<T, PAIRED, true>), grid, dim3(kThreads), lds, st, a, un);
   else SR_LAUNCH((rotary_kernel<T, PAIRED, false>), grid, dim3(kThreads), lds, st, a, un);

@@ -103,6 +103,7 @@ def _norm(**kw):
     (dict(norm=2), abi.SR_EINVAL), (dict(post=3), abi.SR_EINVAL), (dict(B=0), abi.SR_EINVAL), (dict(S=-1), abi.SR_EINVAL),
     (dict(D=0), abi.SR_EINVAL), (dict(eps=0.0), abi.SR_EINVAL), (dict(eps=math.nan), abi.SR_EINVAL),
     (dict(D=8193), abi.SR_EUNSUPPORTED), (dict(B=1 << 16, S=1 << 15), abi.SR_EUNSUPPORTED),
+    (dict(B=(1 << 22) + 1, S=1), abi.SR_EUNSUPPORTED),
 ])
 def test_residual_norm_sizes(kw, status):
     L, c, w, g = _lib(), _norm(**kw), abi.residual_norm_params(), abi.residual_norm_grads()
