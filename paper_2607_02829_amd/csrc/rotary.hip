@@ -32,7 +32,7 @@ SR_DEV float2 turn_of(double t) {
   return float2{(q == 1 || q == 2) ? -a : a, q >= 2 ? -b : b};
 }
 
-constexpr int kThreads = 256, kUnroll = 4;
+constexpr int kThreads = 256, kUnroll = 2, kTokens = 16;   // 65536 x 1024 with two units a thread 50.8 us, four 52.7
 
 // 16 bytes of channels.
 template <typename T>
@@ -45,9 +45,9 @@ struct Vec16 {
 SR_DEV uint32_t quotient(uint32_t i, uint32_t magic, uint32_t d) { return d == 1 ? i : __umulhi(i, magic); }
 
 struct Units {
-  int tokens;         // of a workgroup
+  uint32_t tokens;    // of a workgroup, kTokens at most
   uint32_t per_head, per_token, rot;   // units of a head and of a row; those of a head that turn
-  uint32_t magic_head, magic_token;
+  uint32_t magic_head, magic_token, magic_pairs;
 };
 
 // PAIRED: a unit turns V pairs, of channels c0 .. and c1 ..; otherwise V / 2 pairs of neighbours in V channels.  Without
@@ -55,11 +55,12 @@ struct Units {
 template <typename T, bool PAIRED, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary a, Units un) {
   extern __shared__ float2 cs[];   // [tokens][P]
+  __shared__ double place[kTokens][3];
   typedef Vec16<T> Vec;
   constexpr int V = Vec::V;
   const int P = a.first[3];
-  const int64_t rows = (int64_t)a.B * a.S, row0 = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * un.tokens;
-  const uint32_t n = (uint32_t)un.tokens * un.per_token;
+  const int64_t rows = (int64_t)a.B * a.S, row0 = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (int64_t)un.tokens;
+  const uint32_t n = un.tokens * un.per_token;
   const bool past = rows * a.heads * a.hd * (int64_t)sizeof(T) >= kStreamBytes;
   auto get = [&](Vec& v, const T* p, int count) {
     if (WHOLE || count == V) {
@@ -108,30 +109,24 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary a, Units un) {
       }
     }
     if (first) {
-      for (int i = threadIdx.x; i < un.tokens * P; i += kThreads) {
-        const int t = i / P, p = i - t * P;
-        const int64_t row = row0 + t;
-        if (row < rows) {
-          const int b = (int)(row / a.S), s = (int)(row - (int64_t)b * a.S);
-          int l = a.idx ? a.idx[(size_t)(a.idx_shared ? 0 : b) * a.S + s] : s;
-          int place[3] = {l, 0, 0};
-          if (a.axes == 2) {
-            place[0] = l / a.grid[1];
-            place[1] = l - place[0] * a.grid[1];
-          } else if (a.axes == 3) {
-            const int q = l / a.grid[2];
-            place[2] = l - q * a.grid[2];
-            place[0] = q / a.grid[1];
-            place[1] = q - place[0] * a.grid[1];
-          }
-          const int ax = (p >= a.first[1]) + (p >= a.first[2]);
-          const double at_ax = ax == 0   ? fma(a.step[0], (double)place[0], a.origin[0])
-                               : ax == 1 ? fma(a.step[1], (double)place[1], a.origin[1])
-                                         : fma(a.step[2], (double)place[2], a.origin[2]);
-          float2 c = turn_of(at_ax * a.freq[p]);
-          if (a.inverse) c.y = -c.y;
-          cs[i] = c;
+      // the tokens' coordinates, then the turns of all their pairs
+      if (threadIdx.x < un.tokens && row0 + threadIdx.x < rows) {
+        const uint32_t row = (uint32_t)(row0 + threadIdx.x), b = row / (uint32_t)a.S, s = row - b * (uint32_t)a.S;
+        uint32_t l = a.idx ? (uint32_t)a.idx[(size_t)(a.idx_shared ? 0 : b) * a.S + s] : s;
+#pragma unroll
+        for (int ax = 2; ax >= 0; --ax) {   // axes that there are not have one place
+          const uint32_t g = (uint32_t)a.grid[ax], q = ax > 0 ? l / g : 0u;
+          place[threadIdx.x][ax] = fma(a.step[ax], (double)(l - q * g), a.origin[ax]);
+          l = q;
         }
+      }
+      __syncthreads();
+      for (uint32_t i = threadIdx.x; i < un.tokens * (uint32_t)P; i += kThreads) {
+        const uint32_t t = quotient(i, un.magic_pairs, (uint32_t)P);
+        const int p = (int)(i - t * (uint32_t)P), ax = (p >= a.first[1]) + (p >= a.first[2]);
+        float2 c = turn_of(place[t][ax] * a.freq[p]);
+        if (a.inverse) c.y = -c.y;
+        cs[i] = c;
       }
       __syncthreads();
       first = false;
@@ -177,9 +172,10 @@ hipError_t run(const Rotary& a, hipStream_t st) {
   un.per_head = un.rot + (copies ? (uint32_t)((rest + V - 1) / V) : 0);
   un.per_token = un.per_head * (uint32_t)a.heads;
   if (un.per_token == 0) return hipSuccess;
-  // about four units a thread, 16 tokens at most
-  un.tokens = (int)std::min(16u, std::max(1u, kThreads * kUnroll / un.per_token));
+  // about kUnroll units a thread
+  un.tokens = std::min((uint32_t)kTokens, std::max(1u, kThreads * kUnroll / un.per_token));
   un.magic_head = (uint32_t)(((1ull << 32) + un.per_head - 1) / un.per_head);
+  un.magic_pairs = P ? (uint32_t)(((1ull << 32) + P - 1) / P) : 0;
   un.magic_token = (uint32_t)(((1ull << 32) + un.per_token - 1) / un.per_token);
   const int64_t rows = (int64_t)a.B * a.S, wgs = (rows + un.tokens - 1) / un.tokens;
   constexpr int64_t kMaxX = 1 << 22;   // 256 threads each: a launch counts threads along x in 32 bits
