@@ -68,19 +68,21 @@ SR_DEV void store4(char* p, f32x4 v) {
 
 // ---------------------------------------------------------------- tiles through LDS
 
-constexpr int KB = 128;   // bytes of k in a tile: one block
-
-// Operand tile of R rows x 128 bytes: row r at 128 r, its 16-byte chunks at positions c ^ (r / 2 % 8), so that the 16 rows of a
-// fragment read's quarter wave cover the 64 banks once.  It is filled by whole 1 KB blocks, straight from memory
+// Operand tile of R rows x KB bytes (64 or 128): row r at KB r, its 16-byte chunks at positions c ^ swz(r), so that the 16
+// rows of a fragment read's quarter wave cover the 64 banks once.  It is filled by whole 1 KB blocks, straight from memory
 // (buffer_load ... lds): lane l lands at byte 16 l of its block and fetches the chunk that the swizzle places there.
-SR_DEV int swz(int r) { return (r >> 1) & 7; }
-template <int BPW>
+template <int KB>
+SR_DEV int swz(int r) {
+  return (r / (256 / KB)) & (KB / 16 - 1);
+}
+template <int KB, int BPW>
 struct Fill {
   uint32_t off[BPW];
   SR_DEV void init(int r0, uint32_t Kp, int lane, int wid) {
+    constexpr int CH = KB / 16, RPB = 64 / CH;
 #pragma unroll
     for (int i = 0; i < BPW; ++i) {
-      const int row = (wid * BPW + i) * 8 + lane / 8, c = (lane % 8) ^ swz(row);
+      const int row = (wid * BPW + i) * RPB + lane / CH, c = (lane % CH) ^ swz<KB>(row);
       off[i] = (uint32_t)(r0 + row) * Kp + (uint32_t)(c * 16);
     }
   }
@@ -101,17 +103,18 @@ SR_DEV void fill_tile(const uint32_t* off, __amdgpu_buffer_rsrc_t rs, char* lds,
 // fill it does not need.  Per k-tile: a k-step's products with the next one's fragment reads under them; before the last
 // k-step's the wait for the next tile's fill and the barrier, after which this tile's stage is filled anew and the next
 // tile's first fragments are read.  OCC workgroups per CU.  T float: products in bf16, of 32 values of k in a k-step.
-template <int BM, int BN, int WM, int WN, int KG, int NST, int OCC, typename T>
+template <int BM, int BN, int KB, int WM, int WN, int KG, int NST, int OCC, typename T>
 __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear_f8_tile_kernel(LinearF8 a, int tiles_m, int tiles_n, int splits) {
   constexpr bool WIDE = sizeof(T) == 4;
-  constexpr bool GELU = WIDE || BM * BN < 256 * 256;   // tiles of 256 x 256 on 8-bit products have no registers to spare for it
+  constexpr bool GELU = BM * BN < 256 * 256;   // tiles of 256 x 256 have no registers to spare for it
   constexpr int NW = WM * WN, NT = 64 * NW * KG;
   constexpr int MI = BM / (32 * WM), NJ = BN / (32 * WN);
   constexpr int SB = (BM + BN) * KB;               // bytes of a stage: the token tile, then the weight tile
-  constexpr int APW = BM / 8 / NW, BPW = BN / 8 / NW, LPT = APW + BPW + 2;
-  constexpr int RPF = WIDE ? 1 : 2, KS = 4 / RPF;  // fragment reads of a k-step, k-steps of a tile
+  constexpr int RPB = 1024 / KB, APW = BM / RPB / NW, BPW = BN / RPB / NW, LPT = APW + BPW + 2;
+  constexpr int RPF = WIDE ? 1 : 2, KS = KB / 32 / RPF;   // fragment reads of a k-step, k-steps of a tile
   constexpr int EX = KG * NST * SB;                // the waves' exponents: 256 bytes of rows, 256 of channels, per stage
-  static_assert(MI * 32 * WM == BM && NJ * 32 * WN == BN && APW * 8 * NW == BM && BPW * 8 * NW == BN, "whole tiles");
+  static_assert(MI * 32 * WM == BM && NJ * 32 * WN == BN && APW * RPB * NW == BM && BPW * RPB * NW == BN, "whole tiles");
+  constexpr int PH = NST * KS % 2 ? 2 * NST : NST;   // k-tiles after which stage and set of fragments recur
   static_assert(NST >= 2 && NST <= 4 && (NST - 1) * LPT < 64 && MI * 32 <= 256 && NJ * 32 <= 256, "counter ranges");
   __shared__ __attribute__((aligned(1024))) char smem[EX + NW * KG * NST * 512];
   __shared__ __attribute__((aligned(16))) float bias[BN];
@@ -122,11 +125,12 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear_f8_tile_kernel(
   int tm, tn, split;
   tile_coords(blockIdx.x, gridDim.x, tiles_m, tiles_n, tm, tn, split);
   const int m0 = tm * BM, n0 = tn * BN;
-  const int kb = (a.K + KB - 1) / KB, per = (kb + splits - 1) / splits;
-  const int k0 = min(split * per, kb), all = min(per, kb - k0);   // k-tiles of this run
+  constexpr int TPB = kF8Block / KB;   // k-tiles of a block
+  const int kb = (a.K + kF8Block - 1) / kF8Block, per = (kb + splits - 1) / splits * TPB;
+  const int k0 = min(split * per, kb * TPB), all = min(per, kb * TPB - k0);   // k-tiles of this run
   const int ntile = (per + KG - 1) / KG;                          // every group runs ntile, the missing ones on zeros
   const int t0 = k0 + grp * ntile, nmine = min(ntile, k0 + all - t0);
-  const uint32_t Kp = (uint32_t)kb * KB, Mr = (uint32_t)(a.M + 15) / 16 * 16, Nr = (uint32_t)(a.N + 15) / 16 * 16;
+  const uint32_t Kp = (uint32_t)kb * kF8Block, Mr = (uint32_t)(a.M + 15) / 16 * 16, Nr = (uint32_t)(a.N + 15) / 16 * 16;
   const __amdgpu_buffer_rsrc_t ra = make_rsrc(a.xq, (uint32_t)a.M * Kp);
   const __amdgpu_buffer_rsrc_t rb = make_rsrc(a.wq, (uint32_t)a.N * Kp);
   const __amdgpu_buffer_rsrc_t rea = make_rsrc(a.xe, Mr * (uint32_t)kb);
@@ -141,8 +145,8 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear_f8_tile_kernel(
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
-  Fill<APW> fla;
-  Fill<BPW> flb;
+  Fill<KB, APW> fla;
+  Fill<KB, BPW> flb;
   fla.init(m0, Kp, lane, wid);
   flb.init(n0, Kp, lane, wid);
   const uint32_t oea = (uint32_t)(m0 + wm * (BM / WM) + 4 * lane), oeb = (uint32_t)(n0 + wn * (BN / WN) + 4 * lane);
@@ -153,17 +157,17 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear_f8_tile_kernel(
     const uint32_t kt = (uint32_t)(t0 + t), delta = in ? kt * KB : 0x80000000u;
     fill_tile<APW>(fla.off, ra, st, wid, delta);
     fill_tile<BPW>(flb.off, rb, st + BM * KB, wid, delta);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rea, (lds_ptr_t*)se, 4, in ? oea + kt * Mr : 0x80000000u, 0, 0, 0);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(reb, (lds_ptr_t*)(se + 256), 4, in ? oeb + kt * Nr : 0x80000000u, 0, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rea, (lds_ptr_t*)se, 4, in ? oea + kt / TPB * Mr : 0x80000000u, 0, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(reb, (lds_ptr_t*)(se + 256), 4, in ? oeb + kt / TPB * Nr : 0x80000000u, 0, 0, 0);
   };
   // fragment of rows r .. r + 31, chunk pair c4: lane's row r + lane % 32, chunk 2 c4 + lane / 32; rows 16 apart share
   // the swizzle
   const uint32_t sbase = lds_addr(smem) + (uint32_t)(grp * NST * SB);
   const uint32_t ebase = lds_addr(smem) + (uint32_t)(EX + wave * NST * 512 + (lane & 31));
-  uint32_t fa[4], fb[4];
+  uint32_t fa[KB / 32], fb[KB / 32];
 #pragma unroll
-  for (int c4 = 0; c4 < 4; ++c4) {
-    const int r = lane & 31, c = ((2 * c4 + h) ^ swz(r)) * 16;
+  for (int c4 = 0; c4 < KB / 32; ++c4) {
+    const int r = lane & 31, c = ((2 * c4 + h) ^ swz<KB>(r)) * 16;
     fa[c4] = sbase + (uint32_t)((wm * (BM / WM) + r) * KB + c);
     fb[c4] = sbase + (uint32_t)(BM * KB + (wn * (BN / WN) + r) * KB + c);
   }
@@ -172,24 +176,26 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear_f8_tile_kernel(
   constexpr int NF = (MI + NJ) * RPF;
   // read F of k-step ks of stage S: the MI token fragments, then the NJ weight fragments
   auto read1 = [&](auto sidx, auto ksv, auto fv) {
-    constexpr int S = decltype(sidx)::value, ks = decltype(ksv)::value, F = decltype(fv)::value / RPF, p = decltype(fv)::value % RPF;
-    if constexpr (F < MI) ua[ks & 1][F][p] = rd16<S * SB + F * 32 * KB>(fa[ks * RPF + p]);
-    else ub[ks & 1][F - MI][p] = rd16<S * SB + (F - MI) * 32 * KB>(fb[ks * RPF + p]);
+    constexpr int G = decltype(sidx)::value, S = G % NST, ks = decltype(ksv)::value, F = decltype(fv)::value / RPF, p = decltype(fv)::value % RPF;
+    constexpr int Q = (G * KS + ks) & 1;
+    if constexpr (F < MI) ua[Q][F][p] = rd16<S * SB + F * 32 * KB>(fa[ks * RPF + p]);
+    else ub[Q][F - MI][p] = rd16<S * SB + (F - MI) * 32 * KB>(fb[ks * RPF + p]);
   };
   auto read_ex = [&](auto sidx, auto fv) {
-    constexpr int S = decltype(sidx)::value, F = decltype(fv)::value;
+    constexpr int S = decltype(sidx)::value % NST, F = decltype(fv)::value;
     if constexpr (F < MI) na[F] = rd_u8<S * 512 + F * 32>(ebase);
     else nb[F - MI] = rd_u8<S * 512 + 256 + (F - MI) * 32>(ebase);
   };
-  auto settle = [&](int ks) {
+  auto settle = [&](auto q) {
+    constexpr int Q = decltype(q)::value;
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
-      for (int p = 0; p < RPF; ++p) pin(ua[ks & 1][i][p]);
+      for (int p = 0; p < RPF; ++p) pin(ua[Q][i][p]);
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
 #pragma unroll
-      for (int p = 0; p < RPF; ++p) pin(ub[ks & 1][j][p]);
+      for (int p = 0; p < RPF; ++p) pin(ub[Q][j][p]);
   };
   auto settle_ex = [&]() {
 #pragma unroll
@@ -205,13 +211,13 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear_f8_tile_kernel(
   };
   // the products of one k-step, with issue(X) after product X: what it issues goes out under the products
   constexpr int NX = MI * NJ * (WIDE ? 2 : 1);
-  auto mfmas = [&](auto ksv, auto&& issue) {
-    constexpr int ks = decltype(ksv)::value & 1;
+  auto mfmas = [&](auto qv, auto&& issue) {
+    constexpr int Q = decltype(qv)::value;
     if constexpr (!WIDE) {
       static_for<MI * NJ>([&](auto x) {
         constexpr int i = decltype(x)::value / NJ, j = decltype(x)::value % NJ;
-        const i32x8 xa = __builtin_shufflevector(ua[ks][i][0], ua[ks][i][RPF - 1], 0, 1, 2, 3, 4, 5, 6, 7);
-        const i32x8 xb = __builtin_shufflevector(ub[ks][j][0], ub[ks][j][RPF - 1], 0, 1, 2, 3, 4, 5, 6, 7);
+        const i32x8 xa = __builtin_shufflevector(ua[Q][i][0], ua[Q][i][RPF - 1], 0, 1, 2, 3, 4, 5, 6, 7);
+        const i32x8 xb = __builtin_shufflevector(ub[Q][j][0], ub[Q][j][RPF - 1], 0, 1, 2, 3, 4, 5, 6, 7);
         acc[i][j] = KG == 1 ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(xb, xa, acc[i][j], 0, 0, 0, eb[j], 0, ea[i])
                             : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(xa, xb, acc[i][j], 0, 0, 0, ea[i], 0, eb[j]);
         __builtin_amdgcn_sched_barrier(0);
@@ -219,13 +225,13 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear_f8_tile_kernel(
         __builtin_amdgcn_sched_barrier(0);
       });
     } else {
-      static_for<2>([&](auto qv) {   // 16 values of k each
-        constexpr int q = decltype(qv)::value;
+      static_for<2>([&](auto hv) {   // 16 values of k each
+        constexpr int q = decltype(hv)::value;
         bf16x8 da[MI], db[NJ];
 #pragma unroll
-        for (int i = 0; i < MI; ++i) da[i] = decode8(ua[ks][i][0][2 * q], ua[ks][i][0][2 * q + 1], scale_of(ea[i]));
+        for (int i = 0; i < MI; ++i) da[i] = decode8(ua[Q][i][0][2 * q], ua[Q][i][0][2 * q + 1], scale_of(ea[i]));
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) db[j] = decode8(ub[ks][j][0][2 * q], ub[ks][j][0][2 * q + 1], scale_of(eb[j]));
+        for (int j = 0; j < NJ; ++j) db[j] = decode8(ub[Q][j][0][2 * q], ub[Q][j][0][2 * q + 1], scale_of(eb[j]));
         static_for<MI * NJ>([&](auto x) {
           constexpr int i = decltype(x)::value / NJ, j = decltype(x)::value % NJ;
           acc[i][j] = KG == 1 ? __builtin_amdgcn_mfma_f32_32x32x16_bf16(db[j], da[i], acc[i][j], 0, 0, 0)
@@ -242,14 +248,15 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear_f8_tile_kernel(
   static_for<NF>([&](auto f) { read1(IC<0>{}, IC<0>{}, f); });
   static_for<MI + NJ>([&](auto f) { read_ex(IC<0>{}, f); });
   auto body = [&](int t, auto sidx) {
-    constexpr int S = decltype(sidx)::value;
+    constexpr int G = decltype(sidx)::value, S = G % NST;
     static_for<KS - 1>([&](auto ksv) {
       constexpr int ks = decltype(ksv)::value;
+      constexpr int Q = (G * KS + ks) & 1;
       lgkm_wait<0>();
-      settle(ks);
+      settle(IC<Q>{});
       if constexpr (ks == 0) settle_ex();
       __builtin_amdgcn_sched_barrier(0);
-      mfmas(ksv, [&](auto x) {
+      mfmas(IC<Q>{}, [&](auto x) {
         constexpr int X = decltype(x)::value, F0 = X * NF / NX, F1 = (X + 1) * NF / NX;
         static_for<F1 - F0>([&](auto f) { read1(sidx, IC<ks + 1>{}, IC<F0 + decltype(f)::value>{}); });
       });
@@ -257,25 +264,28 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear_f8_tile_kernel(
     // the next tile is resident (its fill is the oldest in flight), and every wave is done with this one's stage
     wait_vm_lgkm0<(NST - 2) * LPT>();
     lds_barrier();
-    settle(KS - 1);
+    constexpr int Q = (G * KS + KS - 1) & 1;
+    settle(IC<Q>{});
+    if constexpr (KS == 1) settle_ex();
     __builtin_amdgcn_sched_barrier(0);
-    mfmas(IC<KS - 1>{}, [&](auto x) {   // reads of the next tile: unused past the last one
+    mfmas(IC<Q>{}, [&](auto x) {   // reads of the next tile: unused past the last one
       constexpr int X = decltype(x)::value, NA = NF + MI + NJ, F0 = X * NA / NX, F1 = (X + 1) * NA / NX;
       static_for<F1 - F0>([&](auto f) {
         constexpr int F = F0 + decltype(f)::value;
-        if constexpr (F < NF) read1(IC<(S + 1) % NST>{}, IC<0>{}, IC<F>{});
-        else read_ex(IC<(S + 1) % NST>{}, IC<F - NF>{});
+        if constexpr (F < NF) read1(IC<(G + 1) % PH>{}, IC<0>{}, IC<F>{});
+        else read_ex(IC<(G + 1) % PH>{}, IC<F - NF>{});
       });
       if constexpr (X == (NX > 1 ? 1 : 0)) fill(t + NST, S);
     });
   };
-  for (int t = 0; t < ntile; t += NST)
-    static_for<NST>([&](auto s) {
+  for (int t = 0; t < ntile; t += PH)
+    static_for<PH>([&](auto s) {
       if (s.value == 0 || t + s.value < ntile) body(t + s.value, s);
     });
   // the last body's reads and fills land before their registers and stages are used again
   lgkm_wait<0>();
-  settle(0);
+  settle(IC<0>{});
+  settle(IC<1>{});
   settle_ex();
   wait_vm_lgkm0<0>();
   __syncthreads();
@@ -399,8 +409,8 @@ __global__ __launch_bounds__(64 * W) void linear_f8_few_kernel(LinearF8 a) {
   const int lane = threadIdx.x & 63, wave = wave_index(), r = lane & 15, h = lane >> 4;
   const int tiles_n = (a.N + 15) / 16;
   const int m0 = (int)(blockIdx.x / (unsigned)tiles_n) * 16, n0 = (int)(blockIdx.x % (unsigned)tiles_n) * 16;
-  const int kb = (a.K + KB - 1) / KB, per = (kb + W - 1) / W, b1 = min(kb, (wave + 1) * per);
-  const uint32_t Kp = (uint32_t)kb * KB, Mr = (uint32_t)(a.M + 15) / 16 * 16, Nr = (uint32_t)(a.N + 15) / 16 * 16;
+  const int kb = (a.K + kF8Block - 1) / kF8Block, per = (kb + W - 1) / W, b1 = min(kb, (wave + 1) * per);
+  const uint32_t Kp = (uint32_t)kb * kF8Block, Mr = (uint32_t)(a.M + 15) / 16 * 16, Nr = (uint32_t)(a.N + 15) / 16 * 16;
   const __amdgpu_buffer_rsrc_t rx = make_rsrc(a.xq, (uint32_t)a.M * Kp), rw = make_rsrc(a.wq, (uint32_t)a.N * Kp);
   const __amdgpu_buffer_rsrc_t rex = make_rsrc(a.xe, Mr * (uint32_t)kb), rew = make_rsrc(a.we, Nr * (uint32_t)kb);
   const uint32_t ox = (uint32_t)(m0 + r) * Kp + 32u * h, ow = (uint32_t)(n0 + r) * Kp + 32u * h;
@@ -411,7 +421,7 @@ __global__ __launch_bounds__(64 * W) void linear_f8_few_kernel(LinearF8 a) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {   // past the run's end: beyond the operands, zeros
       const bool in = b + u < b1;
-      const uint32_t k = in ? (uint32_t)(b + u) * KB : 0x80000000u;
+      const uint32_t k = in ? (uint32_t)(b + u) * kF8Block : 0x80000000u;
       ex[u] = __builtin_amdgcn_raw_buffer_load_b8(rex, in ? (uint32_t)(b + u) * Mr + m0 + r : 0x80000000u, 0, 0);
       ew[u] = __builtin_amdgcn_raw_buffer_load_b8(rew, in ? (uint32_t)(b + u) * Nr + n0 + r : 0x80000000u, 0, 0);
 #pragma unroll
@@ -474,11 +484,11 @@ int64_t tiles_of(int M, int N, int bm, int bn) { return ((int64_t)(M + bm - 1) /
 //   groups, 1024 x 4096 x 16200 109 (256 x 128 in two runs 117, two workgroups 122), 4096 x 1024 x 4050 34 (39); in four runs
 //   1024 x 1024 x 16200 39 (64 x 64 49, one run 101)
 //   256 x 128:  8192 x 1024 x 1024 13.9 (128 x 128 14.6, 256 x 256 18.9)
-//   256 x 256:  16200 x 4096 x 1024 80 (86), 16200 x 1024 x 4096 57 (67), 4050 x 4096 x 1024 23.7 (24.5), fp32 16200 x 4096 x 1024 134
-//   (146);  with GELU, whose vector work wants a second workgroup's products beside it, 16200 x 4096 x 1024 105 with two of 128 x 128
+//   256 x 256:  16200 x 4096 x 1024 80 (86), 16200 x 1024 x 4096 57 (67), 4050 x 4096 x 1024 23.7 (24.5);  with GELU or fp32 results two
+//   workgroups of 256 x 128 in three stages of 64 bytes: 16200 x 4096 x 1024 with GELU 95 (128 x 128 101), fp32 122 (256 x 256 130)
 Plan plan_of(int M, int N, int K) {
   auto tiles = [&](int bm, int bn) { return tiles_of(M, N, bm, bn); };
-  const int kb = (K + KB - 1) / KB;
+  const int kb = (K + kF8Block - 1) / kF8Block;
   const int64_t t16 = tiles(16, 16), t32 = tiles(32, 32), t64 = tiles(64, 64), t128 = tiles(128, 128);
   // runs of a row: as many as fill the CUs, of 20 blocks or more
   auto runs = [&](int64_t t) { return (int)std::max<int64_t>(1, std::min<int64_t>(256 / t, kb / 20)); };
@@ -492,10 +502,10 @@ Plan plan_of(int M, int N, int K) {
   return {k128x2, 1};
 }
 
-template <int BM, int BN, int WM, int WN, int KG, int NST, int OCC, typename T>
+template <int BM, int BN, int KB, int WM, int WN, int KG, int NST, int OCC, typename T>
 hipError_t run_tile(const LinearF8& a, int splits, hipStream_t st) {
   const int tm = (a.M + BM - 1) / BM, tn = (a.N + BN - 1) / BN;
-  SR_LAUNCH((linear_f8_tile_kernel<BM, BN, WM, WN, KG, NST, OCC, T>), dim3((unsigned)tm * (unsigned)tn * (unsigned)splits),
+  SR_LAUNCH((linear_f8_tile_kernel<BM, BN, KB, WM, WN, KG, NST, OCC, T>), dim3((unsigned)tm * (unsigned)tn * (unsigned)splits),
             dim3(64 * WM * WN * KG), 0, st, a, tm, tn, splits);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || splits == 1) return e;
@@ -513,20 +523,22 @@ hipError_t run(const LinearF8& a, hipStream_t st) {
       SR_LAUNCH((linear_f8_few_kernel<8, T>), dim3((unsigned)tiles_of(a.M, a.N, 16, 16)), dim3(512), 0, st, a);
       return hipGetLastError();
     }
-    case k32: return run_tile<32, 32, 1, 1, 8, 2, 1, T>(a, s, st);
+    case k32: return run_tile<32, 32, 128, 1, 1, 8, 2, 1, T>(a, s, st);
     case k64:   // longer rows in more stages, or groups (512 x 1024 x 4096 13.2 -> 9.9 us; x 1024 5.1, 5.4)
-      if (a.K <= 2048) return run_tile<64, 64, 2, 2, 2, 2, 2, T>(a, s, st);
-      if constexpr (WIDE) return run_tile<64, 64, 2, 2, 4, 2, 1, T>(a, s, st);
-      else return run_tile<64, 64, 2, 2, 2, 4, 1, T>(a, s, st);
-    case k64x128: return run_tile<64, 128, 2, 4, 1, 4, 1, T>(a, s, st);
+      if (a.K <= 2048) return run_tile<64, 64, 128, 2, 2, 2, 2, 2, T>(a, s, st);
+      if constexpr (WIDE) return run_tile<64, 64, 128, 2, 2, 4, 2, 1, T>(a, s, st);
+      else return run_tile<64, 64, 128, 2, 2, 2, 4, 1, T>(a, s, st);
+    case k64x128: return run_tile<64, 128, 128, 2, 4, 1, 4, 1, T>(a, s, st);
     case k128:
-      if constexpr (WIDE) return run_tile<128, 128, 2, 2, 2, 2, 1, T>(a, s, st);
-      else return run_tile<128, 128, 2, 4, 1, 4, 1, T>(a, s, st);
-    case k128x2: return run_tile<128, 128, 2, 4, 1, 2, 2, T>(a, s, st);
-    case k256x128: return run_tile<256, 128, 4, 2, 1, 3, 1, T>(a, s, st);
+      if constexpr (WIDE) return run_tile<128, 128, 128, 2, 2, 2, 2, 1, T>(a, s, st);
+      else return run_tile<128, 128, 128, 2, 4, 1, 4, 1, T>(a, s, st);
+    case k128x2: return run_tile<128, 128, 128, 2, 4, 1, 2, 2, T>(a, s, st);
+    case k256x128: return run_tile<256, 128, 128, 4, 2, 1, 3, 1, T>(a, s, st);
     case k256:
-      if (!WIDE && a.act == SR_ACT_GELU) return run_tile<128, 128, 2, 2, 1, 2, 2, T>(a, s, st);
-      return run_tile<256, 256, 2, 4, 1, 2, 1, T>(a, s, st);
+      // decoding and GELU are vector work, under which a second workgroup's products run
+      if (WIDE || a.act == SR_ACT_GELU) return run_tile<256, 128, 64, 2, 2, 1, 3, 2, T>(a, s, st);
+      if constexpr (!WIDE) return run_tile<256, 256, 128, 2, 4, 1, 2, 1, T>(a, s, st);
+      break;
   }
   return hipErrorInvalidValue;
 }

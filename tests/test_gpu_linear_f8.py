@@ -158,7 +158,7 @@ def test_products(M, N, K, dtype):
     _check(got, z, P, K, dtype)
 
 
-@pytest.mark.parametrize("M,N,K", [(1, 4096, 1024), (40, 100, 200), (300, 512, 256), (2000, 1024, 256), (129, 257, 130)])
+@pytest.mark.parametrize("M,N,K", [(1, 4096, 1024), (40, 100, 200), (300, 512, 256), (2000, 1024, 256), (129, 257, 130), (6500, 2100, 1024)])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_gelu_and_no_bias(M, N, K, dtype):
     got, z, P = _product(M, N, K, dtype, act=abi.SR_ACT_GELU, spread=0.2)
