@@ -14,7 +14,7 @@ namespace sr {
 
 // Results of this many bytes and more are stored past the caches (non-temporal): they would be evicted before anything reads
 // them, and until then push out what the kernel still reads (16200 x 4096 x 1024 on 8-bit codes 92 -> 73 us, 16200 x 4096
-// dropout 45.2 -> 43.5, 65536 x 1024 rotary 55 -> 52); smaller ones stay for their reader (1024 x 1024 x 1024 with its
+// dropout 45.2 -> 43.5, 65536 x 1024 rotary 50 -> 46); smaller ones stay for their reader (1024 x 1024 x 1024 with its
 // tokens' codes 9.7 us, past the caches 10.2).
 constexpr int64_t kStreamBytes = 4 << 20;
 // Runs of 8 and 16 bytes that start at any element: global accesses need no more alignment than that here, so rows of odd
