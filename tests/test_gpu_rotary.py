@@ -25,6 +25,9 @@ CASES = [
     (1, 700, 1, 8, [700], [4], True, False, 0, "bf16", 0, 0),                # many tokens of few channels
     (2, 30, 3, 110, [5, 6], [27, 28], False, False, 0, "bf16", 6, 0),        # units that are cut short
     (2, 30, 3, 110, [5, 6], [20, 28], True, True, 1, "f32", 1, 0),
+    (2, 21, 3, 24, [21], [11], False, False, 0, "bf16", 1, 0),               # fewer that do not turn than 16 bytes hold
+    (2, 21, 3, 24, [21], [3], False, True, 1, "bf16", 0, 0),                 # fewer that turn
+    (1, 4500, 9, 46, [50, 90], [11, 12], True, False, 0, "bf16", 0, 0),      # units that overlap, past the caches
     (1, 4500, 8, 64, [50, 90], [16, 16], False, False, 0, "bf16", 0, 0),     # results past the caches
     (4, 6, 3, 64, [2, 3], [0, 32], False, False, 0, "bf16", 0, 0),           # an axis without pairs
     (1, 5, 3, 64, [5], [0], False, False, 0, "bf16", 0, 0),                  # nothing turns
