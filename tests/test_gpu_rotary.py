@@ -92,6 +92,19 @@ def test_shared_indices_repeats_and_given_frequencies():
            origin=[-0.5, 2.25], step=[0.25, -3.0], freqs=freqs)
 
 
+@pytest.mark.parametrize("base", [1e-4, 2.0, 5e5, 1e30])
+def test_frequencies_of_a_base(base):
+    # far from the origin each frequency's error shows; against powers of 64 bits of mantissa
+    import torch
+    c = (1, 12, 2, 64, [3, 4], [11, 21], False, False, 0, "f32", 0, 0)
+    g = torch.Generator().manual_seed(8)
+    x, y = torch.randn((12, 128), generator=g), torch.empty((12, 128), device="cuda")
+    org = [2.0 ** 24, -3.0 * 2 ** 20]
+    abi.sr_rotary(abi.SrRotary([3, 4], [11, 21], base=base, origin=org), 0, abi.SR_F32, 1, 12, 2, 64, x.cuda(), 128, None, 0, y, 128)
+    freqs = [float(np.longdouble(base) ** (-np.longdouble(j) / n)) for n in (11, 21) for j in range(n)]
+    _check(y.cpu().double().numpy().reshape(1, 12, 2, 64), x.double().numpy().reshape(1, 12, 2, 64), None, c, origin=org, freqs=freqs)
+
+
 def test_unaligned_rows_and_a_window_of_qkv():
     # the queries and keys of q | k | v rows in place, and a view that starts off 16 bytes
     import torch
