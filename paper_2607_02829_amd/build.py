@@ -26,6 +26,9 @@ NO_NANS = {"attention.hip"}
 # Files whose kernels read LDS fragments with inline assembly: their gfx950 assembly is kept
 # and checked (isa_scan) for registers touched while such a read is in flight.
 ASYNC_READS = {"attention.hip", "gemm.hip", "linear8.hip", "linear_f8.hip"}
+# Files whose kernels draw from 64-bit generators: their assembly is kept too and checked for 64-bit shifts by an amount in a kernel's
+# last register (isa_scan.high_shifts).
+SHIFTS = {"select.hip", "dropout.hip", "residual_norm.hip"}
 
 HIPCC = os.environ.get("HIPCC", shutil.which("hipcc") or "/opt/rocm/bin/hipcc")
 FLAGS = [
@@ -43,7 +46,7 @@ def _compile(src: str) -> str:
         cmd.insert(1, "-ffp-contract=off")
     if src in NO_NANS:
         cmd.insert(1, "-fno-honor-nans")
-    if src in ASYNC_READS:
+    if src in ASYNC_READS | SHIFTS:
         cmd.insert(1, "-save-temps=obj")
     if src.endswith(".cpp"):
         cmd[1:1] = ["-x", "hip"]
@@ -54,7 +57,7 @@ def _compile(src: str) -> str:
 
 
 def device_asm_path(src: str) -> str:
-    """Where build() keeps the gfx950 assembly of an ASYNC_READS source."""
+    """Where build() keeps the gfx950 assembly of an ASYNC_READS or SHIFTS source."""
     return os.path.join(BUILD, os.path.splitext(src)[0] + "-hip-amdgcn-amd-amdhsa-gfx950.s")
 
 
@@ -69,6 +72,16 @@ def check_async_reads() -> dict:
     return bad
 
 
+def check_shifts() -> dict:
+    """Kernels of the sources with kept assembly that shift 64 bits by an amount in their last register (none when sound)."""
+    from .isa_scan import high_shifts
+    bad = {}
+    for src in sorted(ASYNC_READS | SHIFTS):
+        with open(device_asm_path(src)) as f:
+            bad.update(high_shifts(f.read()))
+    return bad
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     with ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as ex:
@@ -76,6 +89,9 @@ def build(verbose: bool = False) -> str:
     bad = check_async_reads()
     if bad:
         raise RuntimeError(f"registers touched while their LDS reads are in flight: {bad}")
+    bad = check_shifts()
+    if bad:
+        raise RuntimeError(f"64-bit shifts by an amount in the last register: {bad}")
     tmp = OUT + ".tmp"
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)

@@ -36,15 +36,37 @@ SR_DEV uint64_t drop_key(const DropArgs& a) {
   return drop_mix(a.seed + (step + 1ull) * kDropGamma);
 }
 SR_DEV uint64_t drop_word(uint64_t key, uint64_t w) { return drop_mix(key + (w + 1ull) * kDropGamma); }
+// A word is taken apart in halves of 32 bits: a 64-bit shift by a lane's own amount is not safe here in every register (the
+// build's scan of the assembly has the case).
 SR_DEV bool drop_keep1(uint64_t key, uint64_t e, uint32_t thresh) {
-  return ((uint32_t)(drop_word(key, e >> 2) >> (16 * (uint32_t)(e & 3))) & 0xFFFFu) >= thresh;
+  const uint64_t v = drop_word(key, e >> 2);
+  uint32_t lo = (uint32_t)v, hi = (uint32_t)(v >> 32);
+  asm("" : "+v"(lo), "+v"(hi));   // or the compiler makes the choice such a shift again
+  const uint32_t w = e & 2 ? hi : lo;
+  return ((e & 1 ? w >> 16 : w) & 0xFFFFu) >= thresh;
+}
+// n words of 32 bits from draw e on, of n + 2 that start at a multiple of four draws.
+template <int n>
+SR_DEV void drop_align(uint32_t (&w)[n + 2], uint64_t e) {
+  if (e & 2) {
+#pragma unroll
+    for (int j = 0; j <= n; ++j) w[j] = w[j + 1];
+  }
+  if (e & 1) {
+#pragma unroll
+    for (int j = 0; j < n; ++j) w[j] = __builtin_amdgcn_alignbit(w[j + 1], w[j], 16);
+  }
 }
 // Bit j: draw e + j is kept, j = 0 .. 3.  One word of the generator where e is a multiple of four, else two.
 SR_DEV uint32_t drop_keep4(uint64_t key, uint64_t e, uint32_t thresh) {
-  uint64_t v = drop_word(key, e >> 2);
-  const uint32_t sh = 16 * (uint32_t)(e & 3);
-  if (sh) v = v >> sh | drop_word(key, (e >> 2) + 1) << (64 - sh);
-  const uint32_t w[2] = {(uint32_t)v, (uint32_t)(v >> 32)};
+  const uint64_t v = drop_word(key, e >> 2);
+  uint32_t w[4] = {(uint32_t)v, (uint32_t)(v >> 32), 0, 0};
+  if (e & 3) {
+    const uint64_t top = drop_word(key, (e >> 2) + 1);
+    w[2] = (uint32_t)top;
+    w[3] = (uint32_t)(top >> 32);
+    drop_align<2>(w, e);
+  }
   uint32_t keep = 0;
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
@@ -55,14 +77,14 @@ SR_DEV uint32_t drop_keep4(uint64_t key, uint64_t e, uint32_t thresh) {
 }
 // Bit j: draw e + j is kept, j = 0 .. 7.  Two words of the generator where e is a multiple of four, else three.
 SR_DEV uint32_t drop_keep8(uint64_t key, uint64_t e, uint32_t thresh) {
-  uint64_t lo = drop_word(key, e >> 2), hi = drop_word(key, (e >> 2) + 1);
-  const uint32_t sh = 16 * (uint32_t)(e & 3);
-  if (sh) {
+  const uint64_t lo = drop_word(key, e >> 2), hi = drop_word(key, (e >> 2) + 1);
+  uint32_t w[6] = {(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32), 0, 0};
+  if (e & 3) {
     const uint64_t top = drop_word(key, (e >> 2) + 2);
-    lo = lo >> sh | hi << (64 - sh);
-    hi = hi >> sh | top << (64 - sh);
+    w[4] = (uint32_t)top;
+    w[5] = (uint32_t)(top >> 32);
+    drop_align<4>(w, e);
   }
-  const uint32_t w[4] = {(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
   uint32_t keep = 0;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
