@@ -142,61 +142,90 @@ SR_DEV float lanes_sum(float v) {
 constexpr int fwd_threads(int lpr) { return lpr > 256 ? lpr : 256; }
 constexpr int bwd_threads(int lpr) { return lpr <= 64 || lpr > 256 ? 512 : 256; }
 
-// Two sums at once over a team.  Teams of several waves meet in LDS: the slots alternate, so that one barrier a sum
-// is enough (a slot is written again only behind the other one's barrier).
-template <int LPR>
+// N sums at once over a team, of the sum of a thread's runs: the runs that lie CL lanes apart are added up first, in their order
+// (add_run), then the lanes of a wave, then the waves.  CL follows D alone, so a row has the same sums, bit for bit, on a team of CL lanes with NV
+// runs and on one with a lane for every run (NV = 1), whose runs meet in LDS.  Several waves meet there too: the slots
+// alternate, so that one barrier a sum is enough (a slot is written again only behind the other one's barrier).
+constexpr int lanes_apart(int lpr, int nv) { return nv > 1 || lpr <= 64 ? lpr : lpr == 512 ? 128 : 64; }
+SR_DEV void add_run(float& all, int i, float run) { all = i ? all + run : run; }
+template <int LPR, int NV>
 struct TeamSum {
-  static constexpr int W = LPR / 64;   // waves of a team (0: less than one)
-  float (*slot)[2][16];
-  int parity = 0;
-  SR_DEV void operator()(float& a, float& b) {
-    a = lanes_sum<LPR>(a);
-    b = lanes_sum<LPR>(b);
-    if constexpr (W > 1) {
-      const int wave = wave_index(), first = wave / W * W;
-      slot[parity][0][wave] = a;
-      slot[parity][1][wave] = b;
-      __syncthreads();
-      a = b = 0.f;
+  static constexpr int CL = lanes_apart(LPR, NV), W = LPR / 64;   // waves of a team (0: less than one)
+  static constexpr int SLOTS = CL < LPR ? 512 : 16;
+  float (*slot)[2][SLOTS];
+  int team, parity = 0;
+  template <int N>
+  SR_DEV void operator()(float (&q)[N]) {
+    if constexpr (CL < LPR) {
+      const int t = threadIdx.x % LPR;
 #pragma unroll
-      for (int k = 0; k < W; ++k) {
-        a += slot[parity][0][first + k];
-        b += slot[parity][1][first + k];
+      for (int n = 0; n < N; ++n) slot[parity][n][team * LPR + t] = q[n];
+      __syncthreads();
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        const float* at = slot[parity][n] + team * LPR + (t & 63);
+        q[n] = 0.f;
+#pragma unroll
+        for (int w = 0; w < CL / 64; ++w) {
+          float s = at[64 * w];
+#pragma unroll
+          for (int i = 1; i < LPR / CL; ++i) s += at[64 * w + CL * i];
+          q[n] += wave_sum(s);
+        }
       }
       parity ^= 1;
+    } else {
+#pragma unroll
+      for (int n = 0; n < N; ++n) q[n] = lanes_sum<LPR>(q[n]);
+      if constexpr (W > 1) {
+        const int wave = wave_index(), first = wave / W * W;
+#pragma unroll
+        for (int n = 0; n < N; ++n) slot[parity][n][wave] = q[n];
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+          q[n] = 0.f;
+#pragma unroll
+          for (int k = 0; k < W; ++k) q[n] += slot[parity][n][first + k];
+        }
+        parity ^= 1;
+      }
     }
-  }
-  SR_DEV void operator()(float& a) {
-    float b = 0.f;
-    (*this)(a, b);
   }
 };
 
 // z -> Norm(z) in place, with the row's mean and reciprocal deviation; channels past D come out as zeros.
 template <int LPR, int NV, int CUT>
-SR_DEV void norm_row(float (&z)[NV][4], const Place<LPR, NV, CUT>& at, float rD, bool layer, float eps, TeamSum<LPR>& sum,
+SR_DEV void norm_row(float (&z)[NV][4], const Place<LPR, NV, CUT>& at, float rD, bool layer, float eps, TeamSum<LPR, NV>& sum,
                      float& mean, float& rstd) {
+#pragma clang fp contract(off)
   mean = 0.f;
   if (layer) {
-    float s = 0.f;
+    float s[1];
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < NV; ++i) {
+      float r = 0.f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) s += z[i][j];
+      for (int j = 0; j < 4; ++j) r += z[i][j];
+      add_run(s[0], i, r);
+    }
     sum(s);
-    mean = s * rD;
+    mean = s[0] * rD;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) z[i][j] = at.own(i, j) ? z[i][j] - mean : 0.f;
   }
-  float q = 0.f;
+  float q[1];
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
+  for (int i = 0; i < NV; ++i) {
+    float r = 0.f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) q = fmaf(z[i][j], z[i][j], q);
+    for (int j = 0; j < 4; ++j) r = fmaf(z[i][j], z[i][j], r);
+    add_run(q[0], i, r);
+  }
   sum(q);
-  rstd = 1.0f / sqrtf(fmaf(q, rD, eps));
+  rstd = 1.0f / sqrtf(fmaf(q[0], rD, eps));
 #pragma unroll
   for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -215,10 +244,11 @@ SR_DEV uint32_t keep_of(const DropArgs& d, uint64_t key, int64_t row, int D, int
 //   x1 = x + keep (n w1 + b1),  w1 = f gate res_scale post_w, b1 alike;   u = v w2 + b2,  w2 = (1 + scale) pre_w, ..
 template <typename T, typename X, int LPR, int NV, int CUT>
 __global__ __launch_bounds__(fwd_threads(LPR)) void residual_norm_fwd_kernel(ResidualNorm a, int chunks) {
+#pragma clang fp contract(off)   // a row's bits do not depend on the team that takes it: every fma is written out
   constexpr int NT = fwd_threads(LPR), TEAMS = NT / LPR;
-  __shared__ float slots[2][2][16];
-  TeamSum<LPR> sum{slots};
+  __shared__ float slots[2][2][TeamSum<LPR, NV>::SLOTS];
   const int t = threadIdx.x % LPR, team = LPR < 64 ? (int)threadIdx.x / LPR : wave_index() / (LPR / 64 > 0 ? LPR / 64 : 1), D = a.D;
+  TeamSum<LPR, NV> sum{slots, team};
   const int64_t M = (int64_t)a.B * a.S;
   const int b = (int)(blockIdx.x / (unsigned)chunks), k = (int)(blockIdx.x - (unsigned)b * (unsigned)chunks);
   const int R = (a.S + chunks - 1) / chunks, s0 = (int)min((long)k * R, (long)a.S), s1 = min(a.S - s0, R) + s0;
@@ -348,11 +378,12 @@ __global__ __launch_bounds__(fwd_threads(LPR)) void residual_norm_fwd_kernel(Res
 // every tensor and statistic, and add nothing.
 template <typename T, typename X, int LPR, int NV, int CUT>
 __global__ __launch_bounds__(bwd_threads(LPR), 2) void residual_norm_bwd_kernel(ResidualNorm a, int chunks) {
+#pragma clang fp contract(off)   // as in the forward
   constexpr int NT = bwd_threads(LPR), TEAMS = NT / LPR, COLS = LPR * NV * 4;
-  __shared__ float slots[2][2][16];
+  __shared__ float slots[2][2][TeamSum<LPR, NV>::SLOTS];
   __shared__ __attribute__((aligned(16))) float cols[TEAMS > 1 ? TEAMS : 1][TEAMS > 1 ? COLS : 4];
-  TeamSum<LPR> sum{slots};
   const int t = threadIdx.x % LPR, team = LPR < 64 ? (int)threadIdx.x / LPR : wave_index() / (LPR / 64 > 0 ? LPR / 64 : 1), D = a.D;
+  TeamSum<LPR, NV> sum{slots, team};
   const int64_t M = (int64_t)a.B * a.S;
   const int b = (int)(blockIdx.x / (unsigned)chunks), k = (int)(blockIdx.x - (unsigned)b * (unsigned)chunks);
   const int R = (a.S + chunks - 1) / chunks, s0 = (int)min((long)k * R, (long)a.S), s1 = min(a.S - s0, R) + s0;
@@ -386,7 +417,7 @@ __global__ __launch_bounds__(bwd_threads(LPR), 2) void residual_norm_bwd_kernel(
     const int rows = min(TEAMS, s1 - sb);
     const int64_t row0 = (int64_t)b * a.S + sb;
     const __amdgpu_buffer_rsrc_t bdx = rows_of<X>(a.dx1, row0, rows, D), bx = rows_of<X>(a.du ? a.x : nullptr, row0, rows, D);
-    const __amdgpu_buffer_rsrc_t bdu = rows_of<T>(a.du, row0, rows, D), by = rows_of<T>(a.y, row0, rows, D);
+    const __amdgpu_buffer_rsrc_t bdu = rows_of<T>(a.du, row0, rows, D);
     auto stat = [&](int q, bool has) {
       return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rows_of<float>(has ? a.stats + q * M : nullptr, row0, rows, 1), (uint32_t)team * 4, 0, 0));
     };
@@ -399,21 +430,26 @@ __global__ __launch_bounds__(bwd_threads(LPR), 2) void residual_norm_bwd_kernel(
       xr[i].load(bx, at.off[i], at.hi(i));
       dur[i].load(bdu, at.off[i], at.hi(i));
       dxr[i].load(bdx, at.off[i], at.hi(i));
-      yr[i].load(by, at.off[i], at.hi(i));
     }
   };
-  if (s0 < s1) load(s0);
+  auto load_y = [&](int sb) {   // read half a row later than the others, so its registers are free that much longer
+    const __amdgpu_buffer_rsrc_t by = rows_of<T>(a.y, (int64_t)b * a.S + sb, min(TEAMS, s1 - sb), D);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) yr[i].load(by, at.off[i], at.hi(i));
+  };
+  if (s0 < s1) {
+    load(s0);
+    load_y(s0);
+  }
 
   for (int sb = s0; sb < s1; sb += TEAMS) {
     const int rows = min(TEAMS, s1 - sb);
     const int64_t row0 = (int64_t)b * a.S + sb;
     float dx[NV][4], v[NV][4], g[NV][4];
-    Four<T, CUT> yc[NV];
     const float rstd = rx, pmean = my, prstd = a.post ? ry : 1.f;
-    float c1 = 0.f, c2 = 0.f;
+    float c[2];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      yc[i] = yr[i];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         dx[i][j] = dxr[i].at(j);
@@ -423,18 +459,21 @@ __global__ __launch_bounds__(bwd_threads(LPR), 2) void residual_norm_bwd_kernel(
     }
     if (sb + TEAMS < s1) load(sb + TEAMS);
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < NV; ++i) {
+      float r0 = 0.f, r1 = 0.f;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         acc[0][i][j] += g[i][j];
         acc[1][i][j] = fmaf(g[i][j], v[i][j], acc[1][i][j]);
         g[i][j] *= wpre[i][j];
-        c1 += g[i][j];
-        c2 = fmaf(g[i][j], v[i][j], c2);
+        r0 += g[i][j];
+        r1 = fmaf(g[i][j], v[i][j], r1);
       }
-    sum(c1, c2);
-    c1 = layer ? c1 * rD : 0.f;
-    c2 *= rD;
+      add_run(c[0], i, r0);
+      add_run(c[1], i, r1);
+    }
+    sum(c);
+    float c1 = layer ? c[0] * rD : 0.f, c2 = c[1] * rD;
     const __amdgpu_buffer_rsrc_t bdx = rows_of<X>(a.dx, row0, rows, D);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -443,27 +482,30 @@ __global__ __launch_bounds__(bwd_threads(LPR), 2) void residual_norm_bwd_kernel(
       put4<X, CUT>(bdx, at.off[i], at.lo(i), at.hi(i), dx[i], past);
     }
     if (!a.y) continue;
-    c1 = c2 = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const uint32_t keep = drops ? keep_of(a.drop, key, row0 + team, D, (int)at.c(i)) : 0xFu;
+      float r0 = 0.f, r1 = 0.f;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const bool in = team < rows && at.own(i, j) && (keep >> j & 1u);
         const float d = in ? dx[i][j] * a.drop.factor : 0.f;
-        const float n = (yc[i].at(j) - pmean) * prstd;
+        const float n = (yr[i].at(j) - pmean) * prstd;
         v[i][j] = n;
         acc[2][i][j] += d;
         acc[3][i][j] = in ? fmaf(d, n, acc[3][i][j]) : acc[3][i][j];   // a dropped value does not count, not even a NaN
         g[i][j] = d * wpost[i][j];
-        c1 += g[i][j];
-        c2 = fmaf(g[i][j], n, c2);
+        r0 += g[i][j];
+        r1 = fmaf(g[i][j], n, r1);
       }
+      add_run(c[0], i, r0);
+      add_run(c[1], i, r1);
     }
+    if (sb + TEAMS < s1) load_y(sb + TEAMS);
     if (a.post) {
-      sum(c1, c2);
-      c1 = layer ? c1 * rD : 0.f;
-      c2 *= rD;
+      sum(c);
+      c1 = layer ? c[0] * rD : 0.f;
+      c2 = c[1] * rD;
 #pragma unroll
       for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -570,20 +612,27 @@ __global__ __launch_bounds__(1024) void residual_norm_grads_kernel(ResidualNorm 
   }
 }
 
-int lanes_of(int D) { return D <= 128 ? 32 : D <= 1024 ? 64 : D <= 2048 ? 128 : D <= 4096 ? 256 : 512; }
+// Lanes of a row.  Few rows of up to 2048 channels take as many as have a run of four channels: each row has a CU of its own, and
+// what counts is the length of a wave's instructions (1 x 1024 forward 5.5 -> 4.3 us, of which the call is 4.2; both directions
+// 18.8 -> 12.0, 256 x 1024 20.9 -> 14.6).
+constexpr int kFewRows = 256;
+int lanes_of(int64_t M, int D) {
+  if (M <= kFewRows && D > 256 && D <= 2048) return D <= 512 ? 128 : D <= 1024 ? 256 : 512;
+  return D <= 128 ? 32 : D <= 1024 ? 64 : D <= 2048 ? 128 : D <= 4096 ? 256 : 512;
+}
 
 // Workgroups per sample, so that there are about `wgs` of them: in the backward 512 threads per CU, all that its registers leave room for; in the forward, where three fit,
 // a little more (16200 x 1024: 768 42.3 us, 1024 41.0, 1536 42.0).
 int chunks_of(int B, int S, int D, int threads, int wgs) {
-  const int teams = threads / lanes_of(D);
   const int64_t M = (int64_t)B * S;
+  const int teams = threads / lanes_of(M, D);
   // rows of a team: two at least once every CU has a workgroup, so that one loads under the other (8 x 512 x 1024 forward 14.1 -> 12.1 us)
   const int64_t rows = std::max<int64_t>(M > 256 * teams ? 2 : 1, (M + (int64_t)wgs * teams - 1) / ((int64_t)wgs * teams));
   return (int)((S + rows * teams - 1) / (rows * teams));
 }
-int fwd_chunks(int B, int S, int D) { return chunks_of(B, S, D, fwd_threads(lanes_of(D)), 1024); }
+int fwd_chunks(int B, int S, int D) { return chunks_of(B, S, D, fwd_threads(lanes_of((int64_t)B * S, D)), 1024); }
 int bwd_chunks(int B, int S, int D) {
-  const int threads = bwd_threads(lanes_of(D));
+  const int threads = bwd_threads(lanes_of((int64_t)B * S, D));
   return chunks_of(B, S, D, threads, 512 * 256 / threads);
 }
 
@@ -597,12 +646,15 @@ hipError_t run_rows(const ResidualNorm& a, bool bwd, hipStream_t st) {
 }
 
 template <typename T, typename X, int LPR, int CUT>
-hipError_t run_runs(const ResidualNorm& a, bool bwd, hipStream_t st) {   // three runs where they hold the row
+hipError_t run_runs(const ResidualNorm& a, bool bwd, hipStream_t st) {   // one where few rows have a lane for each; three where they hold the row
+  if constexpr (LPR > 64) {
+    if (a.D <= 4 * LPR) return run_rows<T, X, LPR, 1, CUT>(a, bwd, st);
+  }
   return a.D <= 12 * LPR ? run_rows<T, X, LPR, 3, CUT>(a, bwd, st) : run_rows<T, X, LPR, 4, CUT>(a, bwd, st);
 }
 template <typename T, typename X, int CUT>
 hipError_t run_width(const ResidualNorm& a, bool bwd, hipStream_t st) {
-  switch (lanes_of(a.D)) {
+  switch (lanes_of((int64_t)a.B * a.S, a.D)) {
     case 32: return run_rows<T, X, 32, 1, CUT>(a, bwd, st);
     case 64:
       if (a.D <= 256) return run_rows<T, X, 64, 1, CUT>(a, bwd, st);

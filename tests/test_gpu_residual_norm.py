@@ -268,3 +268,45 @@ def test_codes_straight_from_the_norm():
         wq, we, _ = ob.f8_quantize(u.cpu().double().numpy())
         assert np.array_equal(q.cpu().numpy(), wq) and np.array_equal(e.cpu().numpy()[:, :M], we)
         assert (e[:, M:] == 0xEE).all()
+
+
+@pytest.mark.parametrize("D", [257, 300, 512, 513, 700, 1000, 1024, 1025, 1536, 1537, 2047, 2048])
+@pytest.mark.parametrize("rms,dtype", [(False, "bf16"), (True, "f32")])
+def test_a_row_does_not_depend_on_how_many_there_are(D, rms, dtype):
+    # 40 rows are taken by wider teams than 600; their results are those rows' of the larger call, bit for bit
+    import torch
+    c = (1, 600, D, rms, True, "post_w post_b res_scale pre_w pre_b", 0.1, 0, dtype, "f32")
+    cfg, x, y, w, _, _, g = _setup(c, mod_extra=0)
+    dt = _dt(dtype)
+    dx1, du = torch.randn((600, D), generator=g).cuda(), torch.randn((600, D), generator=g).to(dt).cuda()
+    xd, yd, first = x.view(600, D).cuda(), y.view(600, D).cuda(), cfg.drop.first_row
+    params = abi.residual_norm_params(**w)
+    out = []
+    for lo, hi in ((0, 600), (560, 600)):
+        n = hi - lo
+        cfg.S, cfg.drop.first_row = n, first + lo
+        x1, u, st = torch.empty((n, D), device="cuda"), torch.empty((n, D), dtype=dt, device="cuda"), torch.empty((4, n), device="cuda")
+        dx, dy = torch.empty((n, D), device="cuda"), torch.empty((n, D), dtype=dt, device="cuda")
+        a = [t[lo:hi].clone() for t in (xd, yd, dx1, du)]
+        abi.sr_residual_norm_fwd(cfg, params, a[0], a[1], x1, u, None, None, st)
+        scratch = torch.empty(abi.sr_residual_norm_scratch_bytes(cfg), dtype=torch.uint8, device="cuda")
+        abi.sr_residual_norm_bwd(cfg, params, x1, a[1], st, a[2], a[3], dx, dy, abi.residual_norm_grads(), scratch)
+        out.append((x1, u, dx, dy, st.T))
+    for p, q in zip(*out):
+        assert torch.equal(p[560:], q)
+
+
+def test_many_calls_of_few_rows_agree():
+    # waves of one workgroup share their SIMDs here: every wave draws its own words, in every call
+    import torch
+    for D in (1100, 1500, 2048):
+        c = (2, 21, D, False, True, "post_w res_scale", 0.1, 0, "f32", "f32")
+        cfg, x, y, w, w64, keep, _ = _setup(c, mod_extra=0)
+        params, xd, yd = abi.residual_norm_params(**w), x.cuda(), y.cuda()
+        n = (42 * D + 3) // 4 * 4
+        x1, u = torch.zeros((300, n), device="cuda"), torch.zeros((300, n), device="cuda")
+        for i in range(300):
+            abi.sr_residual_norm_fwd(cfg, params, xd, yd, x1[i], u[i])
+        assert bool((x1 == x1[0]).all()) and bool((u == u[0]).all())
+        moved = (x1[0, :42 * D].view(2, 21, D).cpu() != x).numpy()
+        assert np.array_equal(moved & ~keep, np.zeros_like(keep)) and moved.mean() > 0.8
