@@ -232,6 +232,16 @@ SR_DEV void norm_row(float (&z)[NV][4], const Place<LPR, NV, CUT>& at, float rD,
     for (int j = 0; j < 4; ++j) z[i][j] *= rstd;
 }
 
+// Rows of part k of a sample's S, cut into `chunks` parts.  Unsigned: S and the parts' number pass 2^31 together, and so does the
+// row that a team is to take next.  (chunks - 1) R < S + chunks stays below 2^32.
+struct Rows {
+  uint32_t begin, end;
+};
+SR_DEV Rows rows_of_part(int S, int chunks, int k) {
+  const uint32_t n = (uint32_t)S, R = (n + (uint32_t)chunks - 1) / (uint32_t)chunks, begin = min((uint32_t)k * R, n);
+  return {begin, begin + min(n - begin, R)};
+}
+
 // Bit j: channel c + j of the row keeps its value.
 SR_DEV uint32_t keep_of(const DropArgs& d, uint64_t key, int64_t row, int D, int c) {
   const uint64_t r = d.first_row + (uint64_t)row;
@@ -251,7 +261,8 @@ __global__ __launch_bounds__(fwd_threads(LPR)) void residual_norm_fwd_kernel(Res
   TeamSum<LPR, NV> sum{slots, team};
   const int64_t M = (int64_t)a.B * a.S;
   const int b = (int)(blockIdx.x / (unsigned)chunks), k = (int)(blockIdx.x - (unsigned)b * (unsigned)chunks);
-  const int R = (a.S + chunks - 1) / chunks, s0 = (int)min((long)k * R, (long)a.S), s1 = min(a.S - s0, R) + s0;
+  const Rows mine = rows_of_part(a.S, chunks, k);
+  const uint32_t s0 = mine.begin, s1 = mine.end;
   const bool layer = a.norm == SR_NORM_LAYER, drops = a.y && a.drop.thresh, next = a.u || a.uq;
   // x1 stays in the caches where a backward is to read it (16200 x 1024, both directions: 96 us, with x1 past them 103; forward alone 41, 38)
   const bool past = M * D * (int64_t)sizeof(T) >= kStreamBytes, past_x1 = past && !a.stats;
@@ -259,8 +270,8 @@ __global__ __launch_bounds__(fwd_threads(LPR)) void residual_norm_fwd_kernel(Res
   const Place<LPR, NV, CUT> at(t, team, D);
   Four<X, CUT> xr[NV];
   Four<T, CUT> yr[NV];
-  auto load = [&](int sb) {
-    const int rows = min(TEAMS, s1 - sb);
+  auto load = [&](uint32_t sb) {
+    const int rows = (int)min((uint32_t)TEAMS, s1 - sb);
     const int64_t row0 = (int64_t)b * a.S + sb;
     const __amdgpu_buffer_rsrc_t bx = rows_of<X>(a.x, row0, rows, D), by = rows_of<T>(a.y, row0, rows, D);
 #pragma unroll
@@ -296,8 +307,8 @@ __global__ __launch_bounds__(fwd_threads(LPR)) void residual_norm_fwd_kernel(Res
     }
   }
 
-  for (int sb = s0; sb < s1; sb += TEAMS) {
-    const int rows = min(TEAMS, s1 - sb);
+  for (uint32_t sb = s0; sb < s1; sb += TEAMS) {
+    const int rows = (int)min((uint32_t)TEAMS, s1 - sb);
     const int64_t row0 = (int64_t)b * a.S + sb, row = row0 + team;
     const bool on = team < rows;
     float x[NV][4], n[NV][4];
@@ -386,7 +397,8 @@ __global__ __launch_bounds__(bwd_threads(LPR), 2) void residual_norm_bwd_kernel(
   TeamSum<LPR, NV> sum{slots, team};
   const int64_t M = (int64_t)a.B * a.S;
   const int b = (int)(blockIdx.x / (unsigned)chunks), k = (int)(blockIdx.x - (unsigned)b * (unsigned)chunks);
-  const int R = (a.S + chunks - 1) / chunks, s0 = (int)min((long)k * R, (long)a.S), s1 = min(a.S - s0, R) + s0;
+  const Rows mine = rows_of_part(a.S, chunks, k);
+  const uint32_t s0 = mine.begin, s1 = mine.end;
   const bool layer = a.norm == SR_NORM_LAYER, drops = a.y && a.drop.thresh;
   const bool past = M * D * (int64_t)sizeof(T) >= kStreamBytes;
   const uint64_t key = drops ? drop_key(a.drop) : 0;
@@ -413,8 +425,8 @@ __global__ __launch_bounds__(bwd_threads(LPR), 2) void residual_norm_bwd_kernel(
   Four<T, CUT> dur[NV], yr[NV];
   float mx, rx, my, ry;   // the row's statistics
   const bool has_y = a.y && a.post;
-  auto load = [&](int sb) {
-    const int rows = min(TEAMS, s1 - sb);
+  auto load = [&](uint32_t sb) {
+    const int rows = (int)min((uint32_t)TEAMS, s1 - sb);
     const int64_t row0 = (int64_t)b * a.S + sb;
     const __amdgpu_buffer_rsrc_t bdx = rows_of<X>(a.dx1, row0, rows, D), bx = rows_of<X>(a.du ? a.x : nullptr, row0, rows, D);
     const __amdgpu_buffer_rsrc_t bdu = rows_of<T>(a.du, row0, rows, D);
@@ -432,8 +444,8 @@ __global__ __launch_bounds__(bwd_threads(LPR), 2) void residual_norm_bwd_kernel(
       dxr[i].load(bdx, at.off[i], at.hi(i));
     }
   };
-  auto load_y = [&](int sb) {   // read half a row later than the others, so its registers are free that much longer
-    const __amdgpu_buffer_rsrc_t by = rows_of<T>(a.y, (int64_t)b * a.S + sb, min(TEAMS, s1 - sb), D);
+  auto load_y = [&](uint32_t sb) {   // read half a row later than the others, so its registers are free that much longer
+    const __amdgpu_buffer_rsrc_t by = rows_of<T>(a.y, (int64_t)b * a.S + sb, (int)min((uint32_t)TEAMS, s1 - sb), D);
 #pragma unroll
     for (int i = 0; i < NV; ++i) yr[i].load(by, at.off[i], at.hi(i));
   };
@@ -442,8 +454,8 @@ __global__ __launch_bounds__(bwd_threads(LPR), 2) void residual_norm_bwd_kernel(
     load_y(s0);
   }
 
-  for (int sb = s0; sb < s1; sb += TEAMS) {
-    const int rows = min(TEAMS, s1 - sb);
+  for (uint32_t sb = s0; sb < s1; sb += TEAMS) {
+    const int rows = (int)min((uint32_t)TEAMS, s1 - sb);
     const int64_t row0 = (int64_t)b * a.S + sb;
     float dx[NV][4], v[NV][4], g[NV][4];
     const float rstd = rx, pmean = my, prstd = a.post ? ry : 1.f;
