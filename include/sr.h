@@ -444,7 +444,8 @@ SR_API sr_status sr_blocks8_fwd(const sr_config* cfg, int32_t S, const sr_block_
 /* Rotary positions with several axes.  A token stands on a grid of up to three axes (time, height, width; the last one
  * runs fastest: token l = (i_0 * grid[1] + i_1) * grid[2] + i_2) and every head turns `pairs` pairs of its channels by
  *   angle(token, p) = (origin[a] + step[a] * i_a) * f_p      p = 0 .. P-1, a the axis that owns pair p,
- * in 64 bits (a far position keeps its angle).  Axis 0 owns the first pairs[0] pairs, axis 1 the next, and so on;
+ * in 64 bits (a far position keeps its angle); no place of the grid may turn a pair by more than 2^45 either way, where 64 bits
+ * hold an angle to 2^-8 (SR_EUNSUPPORTED).  Axis 0 owns the first pairs[0] pairs, axis 1 the next, and so on;
  * P = their sum, 2 P <= head_dim.  f_p = base^(-j / pairs[a]) for the axis's j-th pair, or freqs[p].
  *   SR_ROT_HALVES: pair p is channels (p, P + p) of the head;  SR_ROT_NEIGHBOURS: channels (2 p, 2 p + 1).
  *   (c0, c1) -> (c0 cos - c1 sin, c1 cos + c0 sin), in fp32 and rounded once; channels from 2 P on are unchanged. */

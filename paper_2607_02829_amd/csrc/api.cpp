@@ -842,10 +842,13 @@ sr_status sr_rotary(const sr_rotary_cfg* rot, int32_t inverse, int32_t dtype, in
     a.first[i] = p;
     const int n = i < rot->axes ? rot->pairs[i] : 0;
     const long double ratio = n && !rot->freqs ? std::exp2(-lb / n) : 1.0L;
+    const double far = n ? std::max(std::fabs(rot->origin[i]), std::fabs(rot->origin[i] + rot->step[i] * (rot->grid[i] - 1))) : 0.0;
     long double f = 1.0L;
     for (int j = 0; j < n; ++j, ++p, f *= ratio) {
       a.freq[p] = rot->freqs ? rot->freqs[p] : (double)f;
       SR_CHECK(std::isfinite(a.freq[p]), SR_EINVAL, "the frequency of pair %d is not finite", p);
+      SR_CHECK(far * std::fabs(a.freq[p]) <= sr::kMaxRotAngle, SR_EUNSUPPORTED, "pair %d turns by up to %g, more than 2^45", p,
+               far * std::fabs(a.freq[p]));
     }
   }
   a.first[3] = p;

@@ -35,6 +35,8 @@ SR_DEV void store16(void* p, i32x4 v, bool past = false) {
 SR_DEV void store8(void* p, i32x2 v) { *(i32x2_any*)p = __builtin_bit_cast(i32x2_any, v); }
 
 constexpr int kMaxRotPairs = 128;   // head dims up to 256
+// Largest angle: its rounding in 64 bits is 2^-8 there, and the quarter turns in it are still counted to 2^-7 (turn_of).
+constexpr double kMaxRotAngle = 0x1p45;
 struct Rotary {
   int B = 0, S = 0, heads = 0, hd = 0;
   int axes = 1, grid[3] = {1, 1, 1}, first[4] = {0, 0, 0, 0};   // axis a owns pairs first[a] .. first[a + 1] - 1
