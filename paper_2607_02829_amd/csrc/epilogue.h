@@ -56,11 +56,10 @@ SR_DEV float gelu_f(float z) {
   return z * norm_cdf<DEG>(z, z * z);
 }
 // z Phi(z) as max(z, 0) - |z| Phi(-|z|), with the limits at the infinities (a finite |z| times a Phi of 0), for layers
-// that round z and GELU(z) once together.
-template <int DEG>
+// that round z and GELU(z) once together: fp32's fit for any type of the results.
 SR_DEV float gelu_lim(float z) {
   // the median leaves out the canonicalisations of fminf and fmaxf; of a NaN it is a number, but its Phi is NaN
-  return fmaf(-__builtin_amdgcn_fmed3f(fabsf(z), 0.f, 3.4028234663852886e38f), half_erfc_of<DEG>(z, z * z),
+  return fmaf(-__builtin_amdgcn_fmed3f(fabsf(z), 0.f, 3.4028234663852886e38f), half_erfc_of<9>(z, z * z),
               __builtin_amdgcn_fmed3f(z, 0.f, __builtin_inff()));
 }
 template <int DEG>
