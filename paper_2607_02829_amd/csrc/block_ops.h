@@ -12,11 +12,16 @@
 
 namespace sr {
 
-// Results of this many bytes and more are stored past the caches (non-temporal): they would be evicted before anything reads
-// them, and until then push out what the kernel still reads (16200 x 4096 x 1024 on 8-bit codes 92 -> 73 us, 16200 x 4096
-// dropout 45.2 -> 43.5, 65536 x 1024 rotary 50 -> 46); smaller ones stay for their reader (1024 x 1024 x 1024 with its
-// tokens' codes 9.7 us, past the caches 10.2).
+// Results of this many bytes and more, in rows of whole lines, are stored past the caches (non-temporal) by the kernels that come back to
+// what they have read: the products, whose operands other workgroups read again, and the residual step, whose backward reads x1
+// and y again.  us, past and in the caches, with the call that reads the results (sr_quantize_f8, or the residual step):
+//   8-bit codes, 16200 x 4096 x 1024 124.5 and 131.0, with GELU 140 and 152, 16200 x 1024 x 4096 100.1 and 100.8
+//   residual step, both directions, 8 x 512 x 1024 50.2 and 49.4 (without readers 33.5 and 36.5), 16200 x 1024 132.0 and 132.7
+// Partial lines lose: 16200 x 1030 x 1024 56.6 and 52.7, the residual step of 16200 x 1023 175 and 168.  So do kernels that read everything
+// once and have nothing to keep in the caches; there the reader pays more than the call gains: rotary of 65536 x 1024 88.6 and 84.9
+// (alone 47.2 and 50.9), dropout of 16200 x 1024 added to a residual 30.0 and 28.1 (alone 15.3 and 17.7).
 constexpr int64_t kStreamBytes = 4 << 20;
+SR_DEV bool past_caches(int64_t rows, int64_t cols, int elt) { return cols * elt % 128 == 0 && rows * cols * elt >= kStreamBytes; }
 // Runs of 8 and 16 bytes that start at any element: global accesses need no more alignment than that here, so rows of odd
 // lengths take the same wide accesses (16200 x 4093 dropout of whole rows 103 -> 55 us, 8192 x 1023 x 1000 on 8-bit codes with theirs 34 -> 26).
 typedef int i32x4_any __attribute__((ext_vector_type(4), aligned(2), may_alias));

@@ -31,16 +31,16 @@ struct Eight {
       }
     }
   }
-  SR_DEV void store(T* p, bool past) const {
+  SR_DEV void store(T* p) const {
     if constexpr (sizeof(T) == 2) {
       i32x4 w;
 #pragma unroll
       for (int j = 0; j < 4; ++j) w[j] = (int)f2bf2(v[2 * j], v[2 * j + 1]);
-      store16(p, w, past);
+      store16(p, w);
     } else {
 #pragma unroll
       for (int j = 0; j < 2; ++j)
-        store16(p + 4 * j, __builtin_bit_cast(i32x4, f32x4{v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]}), past);
+        store16(p + 4 * j, __builtin_bit_cast(i32x4, f32x4{v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]}));
     }
   }
 };
@@ -49,7 +49,6 @@ struct Eight {
 template <typename T>
 __global__ __launch_bounds__(kThreads) void dropout_kernel(Dropout a) {
   const int64_t n = a.M * a.N, whole = n / 8;
-  const bool past = n * (int64_t)sizeof(T) >= kStreamBytes;
   const uint64_t key = drop_key(a.drop), e0 = a.drop.first_row * (uint64_t)a.N;
   const T *x = (const T*)a.x, *r = (const T*)a.resid;
   T* y = (T*)a.y;
@@ -63,7 +62,7 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(Dropout a) {
       const float t = keep >> j & 1u ? v.v[j] * a.drop.factor : 0.f;
       v.v[j] = r ? w.v[j] + t : t;
     }
-    v.store(y + 8 * i, past);
+    v.store(y + 8 * i);
   }
   const int64_t i = 8 * whole + threadIdx.x;
   if (blockIdx.x == 0 && i < n) {
@@ -78,7 +77,6 @@ template <typename T>
 __global__ __launch_bounds__(kThreads) void dropout_rows_kernel(Dropout a) {
   const uint64_t key = drop_key(a.drop);
   const int lane = threadIdx.x & 63;
-  const bool past = a.M * a.N * (int64_t)sizeof(T) >= kStreamBytes;
   const int64_t step = (int64_t)gridDim.x * (kThreads / 64);
   for (int64_t row = (int64_t)blockIdx.x * (kThreads / 64) + wave_index(); row < a.M; row += step) {
     const bool keep = drop_keep1(key, (a.drop.first_row + (uint64_t)row) / (uint64_t)a.drop.group, a.drop.thresh);
@@ -94,7 +92,7 @@ __global__ __launch_bounds__(kThreads) void dropout_rows_kernel(Dropout a) {
         const float t = keep ? v.v[j] * a.drop.factor : 0.f;
         v.v[j] = r ? w.v[j] + t : t;
       }
-      v.store(y + c, past);
+      v.store(y + c);
     }
     for (int64_t c = whole + lane; c < a.N; c += 64) {
       const float t = keep ? to_f32<T>(x[c]) * a.drop.factor : 0.f;

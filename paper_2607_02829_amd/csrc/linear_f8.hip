@@ -296,7 +296,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG, OCC) void linear_f8_tile_kernel(
     typedef decltype(otype) O;
     constexpr int ACT = decltype(actv)::value;
     O* out = (O*)dst;
-    const bool past = splits == 1 && (int64_t)a.M * a.N * (int64_t)sizeof(O) >= kStreamBytes;
+    const bool past = splits == 1 && past_caches(a.M, a.N, sizeof(O));
     if constexpr (KG == 1) {
       // one group: the weight is the first operand, so that a lane has four consecutive channels of one token in each
       // register quad (register r: channel 8 (r/4) + 4 h + r%4, token lane % 32).  The results go through LDS, IPP blocks of

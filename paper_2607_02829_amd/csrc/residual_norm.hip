@@ -265,7 +265,7 @@ __global__ __launch_bounds__(fwd_threads(LPR)) void residual_norm_fwd_kernel(Res
   const uint32_t s0 = mine.begin, s1 = mine.end;
   const bool layer = a.norm == SR_NORM_LAYER, drops = a.y && a.drop.thresh, next = a.u || a.uq;
   // x1 stays in the caches where a backward is to read it (16200 x 1024, both directions: 96 us, with x1 past them 103; forward alone 41, 38)
-  const bool past = M * D * (int64_t)sizeof(T) >= kStreamBytes, past_x1 = past && !a.stats;
+  const bool past = CUT == kWhole && past_caches(M, D, sizeof(T)), past_x1 = past && !a.stats;
   const float rD = 1.0f / (float)D;
   const Place<LPR, NV, CUT> at(t, team, D);
   Four<X, CUT> xr[NV];
@@ -400,7 +400,7 @@ __global__ __launch_bounds__(bwd_threads(LPR), 2) void residual_norm_bwd_kernel(
   const Rows mine = rows_of_part(a.S, chunks, k);
   const uint32_t s0 = mine.begin, s1 = mine.end;
   const bool layer = a.norm == SR_NORM_LAYER, drops = a.y && a.drop.thresh;
-  const bool past = M * D * (int64_t)sizeof(T) >= kStreamBytes;
+  const bool past = CUT == kWhole && past_caches(M, D, sizeof(T));
   const uint64_t key = drops ? drop_key(a.drop) : 0;
   const float rD = 1.0f / (float)D;
   const Place<LPR, NV, CUT> at(t, team, D);

@@ -63,9 +63,6 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary a, Units un) {
   const int P = a.first[3];
   const int64_t rows = (int64_t)a.B * a.S, row0 = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (int64_t)un.tokens;
   const uint32_t n = un.tokens * un.per_token;
-  // past the caches only in whole lines: 16384 rows of 32 heads of 32 channels, whose halves are 32 bytes, 30 us past them, 13 not
-  const bool lines = WHOLE && (!PAIRED || (P * sizeof(T) % 128 == 0 && a.hd * sizeof(T) % 128 == 0));
-  const bool past = lines && rows * a.heads * a.hd * (int64_t)sizeof(T) >= kStreamBytes;
   auto get = [&](Vec& v, const T* p, int count) {
     if (WHOLE || count == V) {
       v = __builtin_bit_cast(Vec, load16(p));
@@ -76,7 +73,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(Rotary a, Units un) {
   };
   auto put = [&](T* p, const Vec& v, int count) {
     if (WHOLE || count == V) {
-      store16(p, __builtin_bit_cast(i32x4, v), past);
+      store16(p, __builtin_bit_cast(i32x4, v));
     } else {
 #pragma unroll
       for (int j = 0; j < V; ++j)
