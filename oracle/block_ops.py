@@ -181,5 +181,6 @@ def f8_quantize(x, tile=False):
     with np.errstate(invalid="ignore"):
         q = np.where(bad, 0x7F, e4m3_codes(np.clip(np.nan_to_num(b * 2.0 ** -e.astype(float)), -448, 448))).astype(np.uint8)
     vals = e4m3_values()[q] * 2.0 ** e.astype(float)
+    q.reshape(Rt // 128, 128, Cp)[:, :, C:] = 0      # past a row's end, also in a block of NaN codes
     back = lambda t: t.reshape(Rt, -1)[:R]  # noqa: E731
     return back(q), (back(e) + 127).astype(np.uint8).T, back(vals)[:, :C]

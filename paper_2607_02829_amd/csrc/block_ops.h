@@ -102,6 +102,8 @@ SR_DEV uint32_t f8_code4(float a, float b, float c, float d) {
   int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
 }
+// The first n of four codes, zeros behind them: in a block with an Inf or NaN the values past a row's end would be NaN too.
+SR_DEV uint32_t f8_first(uint32_t w, int n) { return n >= 4 ? w : n <= 0 ? 0u : w & ((1u << (8 * n)) - 1u); }
 SR_DEV float f8_clamp(float v) { return __builtin_isnan(v) ? v : fminf(fmaxf(v, -448.f), 448.f); }
 
 hipError_t launch_quantize_f8(int kind, int dtype, int M, int N, const void* x, int64_t ldx, uint8_t* q, uint8_t* e,

@@ -75,8 +75,8 @@ SR_DEV uint32_t dpp_max16(uint32_t m) {   // over 16 neighbouring lanes
   return m;
 }
 
-// Codes of eight values, of one block or of one each.
-SR_DEV i32x2 codes8(const float (&v)[8], const float (&inv)[8], bool clamps) {
+// Codes of eight values, of one block or of one each; in a tile at the matrix's edge `left` of them are its own.
+SR_DEV i32x2 codes8(const float (&v)[8], const float (&inv)[8], bool clamps, bool edge, int left) {
   float c[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) c[j] = v[j] * inv[j];
@@ -87,6 +87,10 @@ SR_DEV i32x2 codes8(const float (&v)[8], const float (&inv)[8], bool clamps) {
   i32x2 w;
   w[0] = (int)f8_code4(c[0], c[1], c[2], c[3]);
   w[1] = (int)f8_code4(c[4], c[5], c[6], c[7]);
+  if (edge) {
+    w[0] = (int)f8_first((uint32_t)w[0], left);
+    w[1] = (int)f8_first((uint32_t)w[1], left - 4);
+  }
   return w;
 }
 
@@ -155,7 +159,7 @@ __global__ __launch_bounds__(256) void quantize_f8_kernel(QuantF8 a) {
         inv[j] = s;
       }
       if (m < a.M) {
-        *reinterpret_cast<i32x2*>(a.q + m * Np + n) = codes8(c, inv, E == 246u);
+        *reinterpret_cast<i32x2*>(a.q + m * Np + n) = codes8(c, inv, E == 246u, n0 + 128 > a.N, a.N - n);
         if (l == 0) a.e[tn * Mr + m] = (uint8_t)E;
       }
     }
@@ -191,7 +195,7 @@ __global__ __launch_bounds__(256) void quantize_f8_kernel(QuantF8 a) {
         c[i] = v[i].at(j);
         inv[i] = s;
       }
-      *reinterpret_cast<i32x2*>(tr + (8 * l + j) * kPitch + 8 * g) = codes8(c, inv, E == 246u);
+      *reinterpret_cast<i32x2*>(tr + (8 * l + j) * kPitch + 8 * g) = codes8(c, inv, E == 246u, m0 + 128 > a.M, a.M - (m0 + 8 * g));
       if (g == 0) ex[8 * l + j] = (uint8_t)E;
     }
     __syncthreads();

@@ -372,11 +372,13 @@ __global__ __launch_bounds__(fwd_threads(LPR)) void residual_norm_fwd_kernel(Res
         const auto r = __builtin_amdgcn_permlane16_swap(m, m, false, false);
         m = max(r[0], r[1]);
         const uint32_t E = f8_exponent(m);
-        const float inv = f8_inverse(m, E);
+        const float inv = at.off[i] < kPast ? f8_inverse(m, E) : 0.f;   // codes past D are zeros in any block
         const int Dp = (D + 127) / 128 * 128, ch = (i * LPR + t) * 4;
         if (on && ch < Dp) {
-          const uint32_t q = f8_code4(f8_clamp(o[0] * inv), f8_clamp(o[1] * inv), f8_clamp(o[2] * inv), f8_clamp(o[3] * inv));
-          *reinterpret_cast<uint32_t*>(a.uq + row * Dp + ch) = CUT == kShifted && ch < D ? q >> (8 * at.lo(i)) : q;
+          uint32_t q = f8_code4(f8_clamp(o[0] * inv), f8_clamp(o[1] * inv), f8_clamp(o[2] * inv), f8_clamp(o[3] * inv));
+          if (CUT == kShifted && ch < D) q >>= 8 * at.lo(i);
+          if constexpr (CUT == kSingle) q = f8_first(q, D - ch);
+          *reinterpret_cast<uint32_t*>(a.uq + row * Dp + ch) = q;
           if ((t & 31) == 0) a.ue[(int64_t)(ch / 128) * ((M + 15) / 16 * 16) + row] = (uint8_t)E;
         }
       }
