@@ -529,7 +529,8 @@ SR_API sr_status sr_residual_norm_fwd(const sr_residual_norm* cfg, const sr_resi
 
 /* Its vector-Jacobian product.  x1: the forward's (x where y was NULL).  dx1: gradient of x1 by what else reads it, or NULL
  * for none; du: gradient of u, or NULL if the forward had no u (one of the two is needed).  dx (may be dx1) and dy out; dy, y NULL together.
- * Column sums run in a fixed order (deterministic).  scratch: sr_residual_norm_scratch_bytes bytes. */
+ * Column sums run in a fixed order (deterministic).  scratch: sr_residual_norm_scratch_bytes bytes (never less for more of B, S or D, so
+ * that of the largest call serves them all). */
 SR_API sr_status sr_residual_norm_scratch_bytes(const sr_residual_norm* cfg, size_t* scratch_bytes);
 SR_API sr_status sr_residual_norm_bwd(const sr_residual_norm* cfg, const sr_residual_norm_params* params, const void* x1,
                                const void* y, const float* stats, const void* dx1, const void* du, void* dx, void* dy,
@@ -560,7 +561,8 @@ SR_API sr_status sr_quantize_f8(int32_t f8_kind, int32_t dtype, int32_t M, int32
  *   (M, N, K) on x and w;   dx: (M, K, N) on dy and the transposed codes of w;
  *   dw: (N, K, M), SR_F32, on the transposed codes of dy and of x.
  *   dtype: of bias (or NULL) and y [M,N];  act: sr_act.
- *   scratch: sr_linear_f8_scratch_bytes bytes (NULL when 0), for the partial sums of long rows with few results.
+ *   scratch: sr_linear_f8_scratch_bytes bytes (NULL when 0; never less for more of M, N or K, so that of the largest call serves them
+ *     all), for the partial sums of long rows with few results.
  * M, N >= 1; 1 <= K <= 2^24; M*Kp, N*Kp and M*N*elt < 2^31 bytes (Kp: K rounded up to 128). */
 SR_API sr_status sr_linear_f8_scratch_bytes(int32_t M, int32_t N, int32_t K, size_t* scratch_bytes);
 SR_API sr_status sr_linear_f8(int32_t dtype, int32_t act, int32_t M, int32_t N, int32_t K, const uint8_t* xq, const uint8_t* xe,

@@ -928,7 +928,7 @@ sr_status sr_residual_norm_bwd(const sr_residual_norm* cfg, const sr_residual_no
   for (const float* p : {grads->post_w, grads->post_b, grads->res_scale, grads->pre_w, grads->pre_b, grads->gate,
                          grads->shift, grads->scale})
     SR_CHECK(aligned16(p), SR_EALIGN, "a gradient pointer is not 16-byte aligned");
-  const size_t need = sr::residual_norm_scratch(a.B, a.S, a.D);
+  const size_t need = sr::residual_norm_need(a.B, a.S, a.D);
   SR_PTR(scratch, "scratch");
   SR_CHECK(scratch_bytes >= need, SR_EWORKSPACE, "scratch buffer has %zu bytes, needs %zu", scratch_bytes, need);
   a.x = x1; a.y = y; a.stats = const_cast<float*>(stats);
@@ -985,7 +985,7 @@ sr_status sr_linear_f8(int32_t dtype, int32_t act, int32_t M, int32_t N, int32_t
   SR_PTR(we, "we");
   SR_OPT(bias, "bias");
   SR_PTR(y, "y");
-  const size_t need = sr::linear_f8_scratch(M, N, K);
+  const size_t need = sr::linear_f8_need(M, N, K);
   if (need) {
     SR_PTR(scratch, "scratch");
     SR_CHECK(scratch_bytes >= need, SR_EWORKSPACE, "scratch buffer has %zu bytes, needs %zu", scratch_bytes, need);

@@ -80,7 +80,8 @@ struct ResidualNorm {
   float* part = nullptr;
 };
 constexpr int kMaxNormD = 8192;
-size_t residual_norm_scratch(int B, int S, int D);   // bytes
+size_t residual_norm_need(int B, int S, int D);      // bytes that the backward of these sizes uses
+size_t residual_norm_scratch(int B, int S, int D);   // bytes for these sizes and all smaller ones
 hipError_t launch_residual_norm_fwd(int dtype, int stream_dtype, const ResidualNorm& a, hipStream_t st);
 hipError_t launch_residual_norm_bwd(int dtype, int stream_dtype, const ResidualNorm& a, hipStream_t st);
 
@@ -117,7 +118,8 @@ struct LinearF8 {
   int act = SR_ACT_NONE;
   float* scratch = nullptr;
 };
-size_t linear_f8_scratch(int M, int N, int K);   // bytes
+size_t linear_f8_need(int M, int N, int K);      // bytes that a product of these sizes uses
+size_t linear_f8_scratch(int M, int N, int K);   // bytes for these sizes and all smaller ones
 hipError_t launch_linear_f8(int dtype, const LinearF8& a, hipStream_t st);
 
 }  // namespace sr

@@ -546,9 +546,16 @@ hipError_t run(const LinearF8& a, hipStream_t st) {
 
 }  // namespace
 
-size_t linear_f8_scratch(int M, int N, int K) {
+size_t linear_f8_need(int M, int N, int K) {
   const Plan p = plan_of(M, N, K);
   return p.splits == 1 ? 0 : (size_t)p.splits * M * N * sizeof(float);
+}
+
+// The most that a product of these sizes or smaller ones needs (more tiles leave fewer runs, and none past a tile per CU): runs of 20
+// blocks or more, on 256 tiles at most with all runs, of 32 x 32 up to 128 of these and of 128 x 128 at most beyond.
+size_t linear_f8_scratch(int M, int N, int K) {
+  const int64_t runs = (K + kF8Block - 1) / kF8Block / 20, side = tiles_of(M, N, 32, 32) <= 128 ? 32 : 128;
+  return runs < 2 ? 0 : (size_t)std::min(runs * M * N, 256 * side * side) * sizeof(float);
 }
 
 hipError_t launch_linear_f8(int dtype, const LinearF8& a, hipStream_t st) {

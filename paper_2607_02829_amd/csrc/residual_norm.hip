@@ -691,7 +691,16 @@ hipError_t run_types(int dtype, int stream_dtype, const ResidualNorm& a, bool bw
 
 }  // namespace
 
-size_t residual_norm_scratch(int B, int S, int D) { return (size_t)B * bwd_chunks(B, S, D) * 4 * D * sizeof(float); }
+size_t residual_norm_need(int B, int S, int D) { return (size_t)B * bwd_chunks(B, S, D) * 4 * D * sizeof(float); }
+
+// The most that a call of this many samples, rows and channels or fewer needs (more rows take fewer lanes each, and then fewer
+// workgroups).  Of W workgroups aimed at (chunks_of; 512 from 1025 channels on, and where few rows take more lanes, but these are 256 rows at
+// most), a sample has (W - 1) / B + 1 at most, and no more than rows / T of whole teams.
+size_t residual_norm_scratch(int B, int S, int D) {
+  const int64_t W = D <= 1024 ? 256 : 512, T = D <= 128 ? 16 : D <= 256 ? 8 : 1;
+  const int64_t parts = std::max<int64_t>(B, std::min(B * ((S + T - 1) / T), std::min<int64_t>(B, W) + W - 1));
+  return (size_t)parts * 4 * D * sizeof(float);
+}
 
 hipError_t launch_residual_norm_fwd(int dtype, int stream_dtype, const ResidualNorm& a, hipStream_t st) {
   return run_types(dtype, stream_dtype, a, false, st);
