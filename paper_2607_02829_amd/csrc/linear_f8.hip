@@ -4,7 +4,8 @@
 // as an exponent byte, so blocks of 128 cost no instruction of their own.  Its sums are fp32, but of eight products that
 // it adds at a time it drops what lies 14 bits below the largest: 1.5e-5 of the results' deviation, a hundredth of a
 // bf16 result's rounding.  So bf16 results come from it, and fp32 results from products in bf16, which holds codes times
-// their powers of two exactly (v_cvt_scalef32_pk_bf16_fp8), at half its rate.
+// their powers of two exactly (v_cvt_scalef32_pk_bf16_fp8; 2^-9 of a code times 2^-124 is bf16's smallest number, and in the two
+// lower exponents a block can have, values round to its multiples), at half its rate.
 //
 // Which tile, group or run a product belongs to follows the sizes alone, and every sum has a fixed order.
 #include <algorithm>
@@ -20,7 +21,7 @@ namespace {
 typedef __attribute__((__vector_size__(8 * sizeof(int)))) int i32x8;
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-// Eight codes times 2^e as bf16 (exact).
+// Eight codes times 2^e as bf16 (exact down to e = -124).
 SR_DEV bf16x8 decode8(int lo, int hi, float scale) {
   union {
     bf16x2 h[4];
