@@ -26,9 +26,9 @@ NO_NANS = {"attention.hip"}
 # Files whose kernels read LDS fragments with inline assembly: their gfx950 assembly is kept
 # and checked (isa_scan) for registers touched while such a read is in flight.
 ASYNC_READS = {"attention.hip", "gemm.hip", "linear8.hip", "linear_f8.hip"}
-# Files whose kernels draw from 64-bit generators: their assembly is kept too and checked for 64-bit shifts by an amount in a kernel's
-# last register (isa_scan.high_shifts).
-SHIFTS = {"select.hip", "dropout.hip", "residual_norm.hip"}
+# Files with kernels: the assembly of all of them is kept and checked for 64-bit shifts by an amount in a kernel's last register
+# (isa_scan.high_shifts).
+SHIFTS = {s for s in SOURCES if s.endswith(".hip")} | {"profile.cpp"}
 
 HIPCC = os.environ.get("HIPCC", shutil.which("hipcc") or "/opt/rocm/bin/hipcc")
 FLAGS = [
@@ -46,7 +46,7 @@ def _compile(src: str) -> str:
         cmd.insert(1, "-ffp-contract=off")
     if src in NO_NANS:
         cmd.insert(1, "-fno-honor-nans")
-    if src in ASYNC_READS | SHIFTS:
+    if src in SHIFTS:
         cmd.insert(1, "-save-temps=obj")
     if src.endswith(".cpp"):
         cmd[1:1] = ["-x", "hip"]
@@ -57,7 +57,7 @@ def _compile(src: str) -> str:
 
 
 def device_asm_path(src: str) -> str:
-    """Where build() keeps the gfx950 assembly of an ASYNC_READS or SHIFTS source."""
+    """Where build() keeps the gfx950 assembly of a source with kernels."""
     return os.path.join(BUILD, os.path.splitext(src)[0] + "-hip-amdgcn-amd-amdhsa-gfx950.s")
 
 
@@ -73,10 +73,10 @@ def check_async_reads() -> dict:
 
 
 def check_shifts() -> dict:
-    """Kernels of the sources with kept assembly that shift 64 bits by an amount in their last register (none when sound)."""
+    """Kernels of the library that shift 64 bits by an amount in their last register (none when sound)."""
     from .isa_scan import high_shifts
     bad = {}
-    for src in sorted(ASYNC_READS | SHIFTS):
+    for src in sorted(SHIFTS):
         with open(device_asm_path(src)) as f:
             bad.update(high_shifts(f.read()))
     return bad
