@@ -477,6 +477,8 @@ SR_API sr_status sr_rotary(const sr_rotary_cfg* rot, int32_t inverse, int32_t dt
  *   group = 0: element (row, n) of N columns is draw (first_row + row) * N + n;
  *   group > 0: the values of a row share the draw (first_row + row) / group (1: tokens; S: samples, that is
  *              stochastic depth).
+ * Calls with the same seed and step draw the same: give every dropout of a model (both branches of a block, and each block) a seed of its
+ * own, kept from its forward to its backward, and count the training steps in step.
  * first_row lets the ranks or pieces of a batch draw as the whole batch would.  step_dev (a device address, 8-byte
  * aligned, or NULL) is read by the kernel and added to step, so that every replay of a captured graph can have a draw of its own. */
 typedef struct {
@@ -497,7 +499,9 @@ SR_API sr_status sr_dropout(const sr_drop* drop, int32_t dtype, int32_t M, int32
  *   n  = post ? Norm(y) post_w + post_b : y
  *   x1 = x + gate_b res_scale drop(n)                              rounded to the stream's type
  *   u  = (Norm(x1) pre_w + pre_b) (1 + scale_b) + shift_b          rounded to the storage type
- * SR_NORM_LAYER: Norm(z) = (z - mean) / sqrt(var + eps);  SR_NORM_RMS: z / sqrt(mean z^2 + eps).  fp32 throughout. */
+ * SR_NORM_LAYER: Norm(z) = (z - mean) / sqrt(var + eps);  SR_NORM_RMS: z / sqrt(mean z^2 + eps).  fp32 throughout; what a sample's
+ * channels are multiplied with (gate, res_scale, the factor of what dropout keeps, post_w; 1 + scale, pre_w) is first multiplied together,
+ * and post_b and pre_b alike, so a result has up to three roundings of 2^-24 more than step by step. */
 typedef enum { SR_NORM_LAYER = 0, SR_NORM_RMS = 1 } sr_norm;
 typedef struct {
   int32_t B, S, D;             /* samples (<= 2^22), rows per sample, channels (D <= 8192) */

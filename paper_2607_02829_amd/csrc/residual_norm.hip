@@ -627,8 +627,12 @@ __global__ __launch_bounds__(1024) void residual_norm_grads_kernel(ResidualNorm 
 }
 
 // Lanes of a row.  Few rows of up to 2048 channels take as many as have a run of four channels: each row has a CU of its own, and
-// what counts is the length of a wave's instructions (1 x 1024 forward 5.5 -> 4.3 us, of which the call is 4.2; both directions
-// 18.8 -> 12.0, 256 x 1024 20.9 -> 14.6).
+// what counts is the length of a wave's instructions.  us of a kernel in a graph, forward and backward with its join, a lane for every
+// run against four or fewer runs a lane:
+//   1024 channels: 1 row 3.0 + 6.7 (4.6 + 11.2), 256 rows 3.5 + 10.0 (5.2 + 12.2), 257 4.3 + 10.4 (5.2 + 12.2), 512 4.6 + 11.1 (5.5 + 13.1),
+//   1024 5.5 + 13.9 (5.9 + 15.4), 2048 7.3 + 16.5 (8.7 + 16.8);  512: 256 rows 3.4 + 9.0 (3.7 + 9.0), 384 3.4 + 9.9 (3.8 + 9.3), 2048
+//   5.4 + 13.8 (5.6 + 12.3);  2048: 256 rows 4.5 + 11.8 (5.4 + 14.8), 512 6.0 + 13.7 (5.9 + 16.4).
+// The border is where a CU has one row; 513 to 1024 channels would still gain at eight times as many rows.
 constexpr int kFewRows = 256;
 int lanes_of(int64_t M, int D) {
   if (M <= kFewRows && D > 256 && D <= 2048) return D <= 512 ? 128 : D <= 1024 ? 256 : 512;
