@@ -489,8 +489,7 @@ int64_t tiles_of(int M, int N, int bm, int bn) { return ((int64_t)(M + bm - 1) /
 //   1024 x 1024 x 16200 39 (64 x 64 49, one run 101)
 //   256 x 128:  8192 x 1024 x 1024 13.9 (128 x 128 14.6, 256 x 256 18.9)
 //   256 x 256:  16200 x 4096 x 1024 80 (86), 16200 x 1024 x 4096 57 (67), 4050 x 4096 x 1024 23.7 (24.5);  with GELU or fp32 results two
-//   workgroups of 256 x 128 in three stages of 64 bytes: 16200 x 4096 x 1024 with GELU 99 (128 x 128 101 with a shorter
-//   fit of GELU that took 95 here), fp32 122 (256 x 256 130)
+//   workgroups of 256 x 128 in three stages of 64 bytes: 16200 x 4096 x 1024 with GELU 97 - 100 (128 x 128 110), fp32 122 (256 x 256 130)
 Plan plan_of(int M, int N, int K) {
   auto tiles = [&](int bm, int bn) { return tiles_of(M, N, bm, bn); };
   const int kb = (K + kF8Block - 1) / kF8Block;
